@@ -75,7 +75,8 @@ typedef enum {
     SBN_ERR_WORKSPACE = 5,   /* workspace missing or smaller than sbn_workspace_bytes() */
     SBN_ERR_CUDA = 6,        /* a CUDA runtime/driver call failed (launch, tensor map, ...) */
     SBN_ERR_TIMEOUT = 7,     /* a bounded device-side wait ran out (see sbn_check_status) */
-    SBN_ERR_TOO_LARGE = 8    /* problem exceeds what the library's built-in scratch can serve */
+    SBN_ERR_TOO_LARGE = 8,   /* problem exceeds what the library's built-in scratch can serve */
+    SBN_ERR_INDEX = 9        /* a label or a teacher's index is not in the vocabulary (see sbn_check_status) */
 } sbn_status;
 
 typedef enum { SBN_OUT_F32 = 0, SBN_OUT_BF16 = 1 } sbn_out_dtype;
@@ -421,9 +422,70 @@ sbn_status sbn_unpack_canonical(const int8_t *vals, const uint8_t *meta, int N, 
 sbn_status sbn_tile_canonical(const int8_t *vals_plain, const uint8_t *meta_plain, int N, int K,
                               int8_t *vals, uint8_t *meta, void *stream);
 
+/*
+ * The losses at a model's output head, with their gradients -- what a training step needs around the layers above: the
+ * paper trains with the language-modelling loss and reports perplexity (Sec. 3), ternary models are also distilled
+ * from a full-precision teacher.  The head stays dense bf16 (only the linear layers are ternary, Sec. 2.1):
+ *   x     device, bf16 [T][K], the last hidden states; K % 128 == 0
+ *   head  device, bf16 [N][K], N = vocabulary, any N >= 1;  z = x head^T are the logits, T x N of them
+ * The logits and their gradient are never kept: the forward calls keep one maximum and sum per row and tile, the backward
+ * calls compute z again, a piece of the vocabulary at a time.  Products are exact, sums are held in fp32 on the tensor
+ * cores; the gradient of the logits is rounded to bf16 (as a bf16 run holds it) before it is multiplied with x and head.
+ *
+ * sbn_head_cross_entropy: softmax cross entropy of every token,
+ *   lse[t] = log sum_i exp z[t][i],   loss[t] = lse[t] - z[t][labels[t]]
+ *   labels    device, int64 [T].  A negative label leaves the row out (loss 0, lse 0, no gradient): such rows are not
+ *             multiplied at all, and what x holds there reaches nothing.  A label >= N: loss NaN, otherwise as if left out,
+ *             and sbn_check_status reports SBN_ERR_INDEX
+ *   loss, lse device out, fp32 [T]; lse is needed by the backward call
+ * sbn_head_cross_entropy_backward, with dloss[t] = the gradient of loss[t] (1 / count for a mean):
+ *   dz[t][i] = dloss[t] (exp(z[t][i] - lse[t]) - [i = labels[t]]),   dx = dz head,   dhead = dz^T x
+ *   lse       device, fp32 [T], from the forward call with the same x, head and labels
+ *   dloss     device, fp32 [T]; not read in rows left out
+ *   dx_bf16   device out, bf16 [T][K], or NULL to skip;  dhead_bf16  device out, bf16 [N][K], or NULL to skip (both are
+ *             overwritten, not accumulated; neither may be its input's buffer, SBN_ERR_UNSUPPORTED)
+ *
+ * sbn_head_distill: distillation from a teacher's `top` largest logits per token, over the whole vocabulary of the student:
+ *   q_j = exp(top_logits[t][j] / tau) / sum over the entries that are there,   p_i = exp(z[t][i] / tau - lse[0][t]),
+ *   lse[0][t] = log sum_i exp(z[t][i] / tau),
+ *   distill_loss[t] = sum_j q_j (log q_j - log p_{top_index[t][j]})            (0 log 0 = 0; no factor tau^2)
+ *   top_index   device, int64 [T][top], in any order.  A negative index is an entry that is not there (its logit is not looked
+ *               at); a row with none, or with none but logits of -infinity, is left out: loss 0, no gradient.  An index
+ *               that comes twice counts twice.  An index >= N: distill_loss NaN, no gradient of it, SBN_ERR_INDEX as above
+ *   top_logits  device, [T][top] of top_dtype (SBN_OUT_F32 or SBN_OUT_BF16);  top from 1 to 256, else SBN_ERR_UNSUPPORTED
+ *   temperature tau, positive and finite, and so is 1 / tau (else SBN_ERR_UNSUPPORTED)
+ *   labels, ce_loss  both or neither: the cross entropy of the same logits (at temperature 1) in the same pass over the
+ *               head, as above; a row is left out of the products if neither loss asks for it
+ *   lse         device out, fp32 [T], with labels [2][T]: lse[1] is that of temperature 1; 0 where its loss is left out
+ * sbn_head_distill_backward, with the losses' gradients d_distill and (with labels) d_ce, fp32 [T]:
+ *   dz[t][i] = d_distill[t] / tau (p_i - sum of q_j with top_index[t][j] = i) + d_ce[t] (softmax(z[t])_i - [i = labels[t]])
+ *   and dx, dhead as above.
+ *
+ *   ws          device workspace of sbn_head_workspace_bytes(backward, T, N, K, top) bytes, 256-byte aligned, top = 0 for
+ *               the cross entropy; contents need no initialisation; not to be shared by calls that may run concurrently
+ * Results are the same, bit for bit, from call to call.  All four calls only enqueue; they may be captured into a graph.
+ */
+size_t sbn_head_workspace_bytes(int backward, int T, int N, int K, int top);   /* 0 for sizes that the calls refuse */
+sbn_status sbn_head_cross_entropy(const void *x_bf16, int T, int K, const void *head_bf16, int N,
+                                  const int64_t *labels, float *loss, float *lse, void *ws,
+                                  size_t ws_bytes, void *stream);
+sbn_status sbn_head_cross_entropy_backward(const void *x_bf16, int T, int K, const void *head_bf16, int N,
+                                           const int64_t *labels, const float *lse, const float *dloss,
+                                           void *dx_bf16, void *dhead_bf16, void *ws, size_t ws_bytes,
+                                           void *stream);
+sbn_status sbn_head_distill(const void *x_bf16, int T, int K, const void *head_bf16, int N,
+                            const int64_t *top_index, const void *top_logits, sbn_out_dtype top_dtype, int top,
+                            float temperature, const int64_t *labels, float *distill_loss, float *ce_loss,
+                            float *lse, void *ws, size_t ws_bytes, void *stream);
+sbn_status sbn_head_distill_backward(const void *x_bf16, int T, int K, const void *head_bf16, int N,
+                                     const int64_t *top_index, const void *top_logits, sbn_out_dtype top_dtype,
+                                     int top, float temperature, const int64_t *labels, const float *lse,
+                                     const float *d_distill, const float *d_ce, void *dx_bf16,
+                                     void *dhead_bf16, void *ws, size_t ws_bytes, void *stream);
+
 /* Synchronises `stream`, returns SBN_ERR_TIMEOUT if any kernel since the last call gave up on a
- * bounded wait (and clears that record), SBN_ERR_CUDA if the stream reports an error, else
- * SBN_OK. */
+ * bounded wait, SBN_ERR_INDEX if one met a label or a teacher's index outside the vocabulary (and
+ * clears that record), SBN_ERR_CUDA if the stream reports an error, else SBN_OK. */
 sbn_status sbn_check_status(void *stream);
 
 /* Static string for a status code. */

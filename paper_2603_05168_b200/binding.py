@@ -30,6 +30,7 @@ EXPORTS = [
     "sbn_bitlinear", "sbn_layer_forward_host", "sbn_check_status", "sbn_status_string",
     "sbn_set_gemm_tuning", "sbn_plan_gemm", "sbn_launch_count", "sbn_unpack_canonical", "sbn_tile_canonical",
     "sbn_set_wait_test", "sbn_set_gemm_probe", "sbn_bitlinear_backward",
+    "sbn_head_workspace_bytes", "sbn_head_cross_entropy", "sbn_head_cross_entropy_backward", "sbn_head_distill", "sbn_head_distill_backward",
 ]
 
 _lib = None
@@ -104,6 +105,17 @@ def lib() -> ctypes.CDLL:
         L.sbn_tile_canonical.argtypes = [vp, vp, i32, i32, vp, vp, vp]
         L.sbn_bitlinear_backward.restype = i32
         L.sbn_bitlinear_backward.argtypes = [vp, i32, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, sz, vp]
+        f32 = ctypes.c_float
+        L.sbn_head_workspace_bytes.restype = sz
+        L.sbn_head_workspace_bytes.argtypes = [i32, i32, i32, i32, i32]
+        L.sbn_head_cross_entropy.restype = i32
+        L.sbn_head_cross_entropy.argtypes = [vp, i32, i32, vp, i32, vp, vp, vp, vp, sz, vp]
+        L.sbn_head_cross_entropy_backward.restype = i32
+        L.sbn_head_cross_entropy_backward.argtypes = [vp, i32, i32, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.sbn_head_distill.restype = i32
+        L.sbn_head_distill.argtypes = [vp, i32, i32, vp, i32, vp, vp, i32, i32, f32, vp, vp, vp, vp, vp, sz, vp]
+        L.sbn_head_distill_backward.restype = i32
+        L.sbn_head_distill_backward.argtypes = [vp, i32, i32, vp, i32, vp, vp, i32, i32, f32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.sbn_set_gemm_probe.restype = None
         L.sbn_set_gemm_probe.argtypes = [i32]
         L.sbn_set_wait_test.restype = i32
@@ -311,6 +323,85 @@ def sbn_bitlinear_backward(dY, xq, a_scale, vals, meta, w_scale, N: int, K: int,
            "sbn_bitlinear_backward")
 
 
+def sbn_head_workspace_bytes(T: int, N: int, K: int, top: int = 0, backward: bool = False) -> int:
+    return int(lib().sbn_head_workspace_bytes(1 if backward else 0, T, N, K, top))
+
+
+def _head_tensor(name, t, dtype, shape, device):
+    """The C ABI takes pointers: what a tensor is has to be right here.  Raises ValueError."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} "
+                         f"on {t.device}{'' if t.is_contiguous() else ', not contiguous'}")
+    return t.data_ptr()
+
+
+def _head_inputs(x, head, labels):
+    if x.dim() != 2 or head.dim() != 2:
+        raise ValueError("x and head are two-dimensional")
+    (T, K), N, dev = x.shape, head.shape[0], x.device
+    if dev.type != "cuda" or dev.index != torch._C._cuda_getDevice():
+        raise ValueError(f"x is on {dev}, which is not the current CUDA device")
+    return (T, N, K, dev, _head_tensor("x", x, torch.bfloat16, (T, K), dev), _head_tensor("head", head, torch.bfloat16, (N, K), dev),
+            _head_tensor("labels", labels, torch.int64, (T,), dev))
+
+
+def _head_teacher(T, dev, top_index, top_logits):
+    if top_index.dim() != 2 or top_logits.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("top_index is two-dimensional, top_logits are float32 or bfloat16")
+    top = top_index.shape[1]
+    return (_head_tensor("top_index", top_index, torch.int64, (T, top), dev), _head_tensor("top_logits", top_logits, top_logits.dtype, (T, top), dev),
+            OUT_BF16 if top_logits.dtype == torch.bfloat16 else OUT_F32, top)
+
+
+def _head_ws(ws, dev):
+    if ws is None:
+        return None, 0
+    if ws.device != dev or not ws.is_contiguous():
+        raise ValueError(f"ws: expected a contiguous tensor on {dev}")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
+def sbn_head_cross_entropy(x, head, labels, loss, lse, ws=None):
+    """x bf16 [T][K], head bf16 [N][K], labels int64 [T] (negative: left out); writes loss and lse, fp32 [T]."""
+    T, N, K, dev, px, ph, pl = _head_inputs(x, head, labels)
+    _check(lib().sbn_head_cross_entropy(px, T, K, ph, N, pl, _head_tensor("loss", loss, torch.float32, (T,), dev),
+                                        _head_tensor("lse", lse, torch.float32, (T,), dev), *_head_ws(ws, dev), _stream()),
+           "sbn_head_cross_entropy")
+
+
+def sbn_head_cross_entropy_backward(x, head, labels, lse, dloss, dx=None, dhead=None, ws=None):
+    """lse from the forward call, dloss fp32 [T]; writes dx (bf16, as x) and / or dhead (bf16, as head)."""
+    T, N, K, dev, px, ph, pl = _head_inputs(x, head, labels)
+    _check(lib().sbn_head_cross_entropy_backward(px, T, K, ph, N, pl, _head_tensor("lse", lse, torch.float32, (T,), dev),
+                                                 _head_tensor("dloss", dloss, torch.float32, (T,), dev),
+                                                 _head_tensor("dx", dx, torch.bfloat16, (T, K), dev),
+                                                 _head_tensor("dhead", dhead, torch.bfloat16, (N, K), dev), *_head_ws(ws, dev), _stream()),
+           "sbn_head_cross_entropy_backward")
+
+
+def sbn_head_distill(x, head, top_index, top_logits, temperature, loss, lse, labels=None, ce_loss=None, ws=None):
+    """top_index int64, top_logits fp32 or bf16 [T][top] (negative index: not there); writes loss fp32 [T] and lse fp32 [1][T], or
+    with labels and ce_loss [2][T]."""
+    T, N, K, dev, px, ph, pl = _head_inputs(x, head, labels)
+    _check(lib().sbn_head_distill(px, T, K, ph, N, *_head_teacher(T, dev, top_index, top_logits), float(temperature), pl,
+                                  _head_tensor("loss", loss, torch.float32, (T,), dev), _head_tensor("ce_loss", ce_loss, torch.float32, (T,), dev),
+                                  _head_tensor("lse", lse, torch.float32, (1 if labels is None else 2, T), dev), *_head_ws(ws, dev), _stream()),
+           "sbn_head_distill")
+
+
+def sbn_head_distill_backward(x, head, top_index, top_logits, temperature, lse, d_loss, labels=None, d_ce=None, dx=None, dhead=None, ws=None):
+    """lse from the forward call; d_loss and (with labels) d_ce fp32 [T]; writes dx and / or dhead."""
+    T, N, K, dev, px, ph, pl = _head_inputs(x, head, labels)
+    _check(lib().sbn_head_distill_backward(px, T, K, ph, N, *_head_teacher(T, dev, top_index, top_logits), float(temperature), pl,
+                                           _head_tensor("lse", lse, torch.float32, (1 if labels is None else 2, T), dev),
+                                           _head_tensor("d_loss", d_loss, torch.float32, (T,), dev), _head_tensor("d_ce", d_ce, torch.float32, (T,), dev),
+                                           _head_tensor("dx", dx, torch.bfloat16, (T, K), dev),
+                                           _head_tensor("dhead", dhead, torch.bfloat16, (N, K), dev), *_head_ws(ws, dev), _stream()),
+           "sbn_head_distill_backward")
+
+
 def sbn_set_gemm_probe(flags: int = 0):
     """Timing experiments on the CTA-pair GEMM (results are wrong while flags != 0); see sbn.h."""
     lib().sbn_set_gemm_probe(int(flags))
@@ -360,3 +451,11 @@ def alloc_xq(T: int, K: int, device="cuda"):
 def alloc_gemm_ws(op: int, T: int, N: int, K: int, device="cuda"):
     n = sbn_workspace_bytes(op, T, N, K)
     return torch.zeros(max(n, 16), dtype=torch.uint8, device=device)      # zero-filled once, kept zero by the library
+
+
+def alloc_head_ws(T: int, N: int, K: int, top: int = 0, backward: bool = False, device="cuda"):
+    """Workspace of a call at the output head (top = 0: cross entropy); its contents need no initialisation."""
+    n = sbn_head_workspace_bytes(T, N, K, top, backward)
+    if n == 0:
+        raise ValueError(f"unsupported sizes T = {T}, N = {N}, K = {K}, top = {top}")
+    return torch.empty(n, dtype=torch.uint8, device=device)

@@ -1,0 +1,402 @@
+// The products at the output head, z = x W^T [T][N] (N = vocabulary), dx = dz W and dW = dz^T x, without z or dz ever being
+// kept whole, on the CTA-pair loop of gemm_bf16_pair_loop.cuh:
+//
+//   head_logits_kernel<stats>   tiles of 256 rows x BN columns of z whose epilogue leaves, per row and half of a tile's columns,
+//                               the maximum m and sum exp((z - m) / tau), and the logits at the row's targets
+//   head_logits_kernel<grad>    the same tiles of one piece of the vocabulary (as many columns as the workspace holds):
+//                               dz = g (exp(z / tau - lse) - target), rounded to bf16 into the piece
+//   head_grads_kernel           both gradients of a piece in one launch: dW rows of the piece (contraction over the rows that
+//                               count, bf16 out), and the piece's part of dx, added up in fp32
+//
+// Tokens are on the lanes of tensor memory, so an epilogue thread owns a token's row of the tile: its maximum, its sum and its
+// targets need no exchange.  dz is rounded to bf16 because the tensor cores' operands are; sums are in fp32 throughout.
+// Forward 2 T N K operations, a training step four times that (z is computed twice, it costs less than keeping it).
+#pragma once
+
+#include "gemm_bf16_pair_loop.cuh"
+#include "head_rows.cuh"
+
+namespace sbn {
+
+__device__ __forceinline__ float ex2_approx(float v) {        // relative error 2^-22
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+
+struct HeadMaps {
+    CUtensorMap x, xc;            // K-major: the tokens' rows, or the rows that count moved together
+    CUtensorMap w;                // K-major, BN / 2 rows per box
+};
+struct HeadLogitsParams {
+    HeadTargets tg;
+    const int* count;
+    const int* row_src;
+    int T, N, K;
+    int v0, v1;                   // columns of z: the whole vocabulary, or a piece
+    int bn;
+    float c0;                     // log2(e) / tau
+    // stats
+    float2* part;                 // [rows][parts]
+    float* part1;                 // [rows][parts], sums at temperature 1 (with labels)
+    float* z_ev;                  // [rows][events]
+    int parts;
+    // grad
+    const float *lse0, *lse1;     // per token
+    const float *g0, *g1;         // gradients of the two losses per token (g1: label beside a teacher)
+    float inv_tau;
+    uint16_t* dz;                 // [T up to a multiple of 256][ldz]
+    int ldz;
+    int skip_loads;
+};
+
+// MODE 0 stats, 1 grad.  LIST: targets are sorted events (distillation), else the label alone.  DUAL: the label's loss at
+// temperature 1 beside the teacher's.
+template <int MODE, bool LIST, bool DUAL>
+struct HeadLogitsWork {
+    const HeadMaps& maps;
+    const HeadLogitsParams& p;
+    int rows, tiles_m, tiles_v;
+    bool moved;
+
+    __device__ HeadLogitsWork(const HeadMaps& m, const HeadLogitsParams& q) : maps(m), p(q) {}
+    __device__ void start() {
+        rows = *p.count;
+        moved = rows < p.T;
+        tiles_m = (max(rows, 1) + 255) / 256;              // no row counts: one tile of zeros, which dW then contracts over
+        tiles_v = (p.v1 - p.v0 + p.bn - 1) / p.bn;
+    }
+
+    struct Tile { int m0, n0, bn, k_stages; };
+    // Row tiles fastest, in groups of 16 (a group's rows stay in the L2 while the vocabulary streams by once).
+    struct Tiles {
+        const HeadLogitsWork& w;
+        long long i;
+        long long all;
+        __device__ Tiles(const HeadLogitsWork& work, int pair) : w(work), i(pair), all(static_cast<long long>(work.tiles_m) * work.tiles_v) {}
+        __device__ bool next(Tile& t) {
+            if (i >= all) return false;
+            const int group = static_cast<int>(i / (16ll * w.tiles_v));
+            const int in_group = min(16, w.tiles_m - 16 * group);
+            const int rem = static_cast<int>(i - 16ll * group * w.tiles_v);
+            t.m0 = (16 * group + rem % in_group) * 256;
+            t.n0 = w.p.v0 + (rem / in_group) * w.p.bn;
+            t.bn = w.p.bn;
+            t.k_stages = w.p.K >> 6;
+            i += kBackwardPairs;
+            return true;
+        }
+    };
+
+    __device__ void load(const Tile& t, int ks, uint32_t rank, uint32_t st, uint32_t bar) const {
+        tma_load_2d_pair(st, moved ? &maps.xc : &maps.x, ks * 64, t.m0 + static_cast<int>(rank) * 128, bar);
+        tma_load_2d_pair(st + kPairLoopStageA, &maps.w, ks * 64, t.n0 + static_cast<int>(rank) * (t.bn >> 1), bar);
+    }
+    __device__ uint32_t idesc(const Tile& t) const { return make_idesc_bf16_any(256, t.bn, false, false); }
+    __device__ uint64_t a_step(const Tile&) const { return 32 >> 4; }
+    __device__ uint64_t b_step(const Tile&) const { return 32 >> 4; }
+    __device__ uint64_t a_desc(const Tile&, uint32_t s) const { return make_smem_desc(s, 16, 1024, kSwz128); }
+    __device__ uint64_t b_desc(const Tile&, uint32_t s) const { return make_smem_desc(s, 16, 1024, kSwz128); }
+
+    struct Epilogue {
+        const HeadLogitsWork& w;
+        int rank, quarter, parity, lane;
+        int r, t;                 // row that counts, its token
+        int next_col, e;          // the next target at or behind the current column
+        const int* ev_col;
+        float l0, l1, g0, g1;     // grad: -lse log2(e) and gradient per loss
+
+        __device__ Epilogue(const HeadLogitsWork& work, int rk, int q, int par, int ln) : w(work), rank(rk), quarter(q), parity(par), lane(ln) {}
+
+        __device__ void advance(int col) {                 // to the first target at or behind `col`
+            if constexpr (LIST) {
+                while (next_col < col) {
+                    ++e;
+                    next_col = e < w.p.tg.events ? ev_col[e] : kNoColumn;
+                }
+            } else {
+                if (next_col < col) next_col = kNoColumn;
+            }
+        }
+
+        __device__ void begin(const Tile& tile) {
+            const HeadLogitsParams& p = w.p;
+            r = tile.m0 + rank * 128 + quarter * 32 + lane;
+            t = 0;
+            next_col = kNoColumn;
+            e = 0;
+            l0 = l1 = -INFINITY;
+            g0 = g1 = 0.0f;
+            if (r >= w.rows) return;
+            t = p.row_src[r];
+            if constexpr (LIST) {
+                ev_col = p.tg.ev_col + static_cast<size_t>(t) * p.tg.events;
+                int lo = 0, hi = p.tg.events;              // first event at or behind the tile's columns
+                while (lo < hi) {
+                    const int mid = (lo + hi) >> 1;
+                    if (ev_col[mid] < tile.n0) lo = mid + 1; else hi = mid;
+                }
+                e = lo;
+                next_col = e < p.tg.events ? ev_col[e] : kNoColumn;
+            } else {
+                next_col = static_cast<int>(p.tg.labels[t]);
+                if (next_col < tile.n0) next_col = kNoColumn;
+            }
+            if constexpr (MODE == 1) {
+                constexpr float kLog2e = 1.4426950408889634f;
+                const int flags = LIST ? p.tg.flags[t] : kRowDistill;
+                if (flags & kRowDistill) {
+                    l0 = -p.lse0[t] * kLog2e;
+                    g0 = p.g0[t] * p.inv_tau;
+                }
+                if (DUAL && (flags & kRowLabel)) {
+                    l1 = -p.lse1[t] * kLog2e;
+                    g1 = p.g1[t];
+                }
+            }
+        }
+
+        template <class Release>
+        __device__ void run(const Tile& tile, uint32_t taddr, Release&& release) {
+            const HeadLogitsParams& p = w.p;
+            const int chunks = tile.bn >> 5;
+            const bool here = r < w.rows;
+            const int first_row = tile.m0 + rank * 128 + quarter * 32;
+            // rows that nobody reads: behind the last that counts (grad: behind the last stage that dW reads)
+            const bool idle = first_row >= (MODE == 0 ? w.rows : ((max(w.rows, 1) + 63) & ~63));
+            if (idle) {
+                release();
+                return;
+            }
+            float m = -INFINITY, s0 = 0.0f, s1 = 0.0f;
+#pragma unroll 1
+            for (int c = parity; c < chunks; c += 2) {
+                uint32_t z[32];
+                __syncwarp();                              // the lanes may have parted over their targets
+                tmem_ld_32x32b_x32(taddr + static_cast<uint32_t>(c * 32), z);
+                tmem_ld_wait();
+                if (c + 2 >= chunks) release();
+                const int n = tile.n0 + c * 32;
+                advance(n);
+                if constexpr (MODE == 0) {
+                    while (next_col < n + 32) {            // rare: a row has a handful of targets in the whole vocabulary
+                        float v = 0.0f;
+#pragma unroll
+                        for (int q = 0; q < 32; ++q) v = next_col - n == q ? __uint_as_float(z[q]) : v;
+                        if constexpr (LIST) {
+                            p.z_ev[static_cast<size_t>(r) * p.tg.events + e] = v;
+                            ++e;
+                            next_col = e < p.tg.events ? ev_col[e] : kNoColumn;
+                        } else {
+                            p.z_ev[r] = v;
+                            next_col = kNoColumn;
+                        }
+                    }
+                    if (n >= p.N) continue;
+                    if (n + 32 > p.N) {                    // behind the vocabulary: nothing
+#pragma unroll
+                        for (int q = 0; q < 32; ++q) z[q] = n + q < p.N ? z[q] : 0xFF800000u;
+                    }
+                    float mc = __uint_as_float(z[0]);
+#pragma unroll
+                    for (int q = 1; q < 32; ++q) mc = fmaxf(mc, __uint_as_float(z[q]));
+                    const float m_new = fmaxf(m, mc);
+                    s0 *= ex2_approx((m - m_new) * p.c0);
+                    if (DUAL) s1 *= ex2_approx((m - m_new) * 1.4426950408889634f);
+                    m = m_new;
+#pragma unroll
+                    for (int q = 0; q < 32; ++q) {
+                        const float d = __uint_as_float(z[q]) - m;      // the difference first: exact where it matters
+                        s0 += ex2_approx(d * p.c0);
+                        if (DUAL) s1 += ex2_approx(d * 1.4426950408889634f);
+                    }
+                } else {
+                    float v[32];
+#pragma unroll
+                    for (int q = 0; q < 32; ++q) {
+                        v[q] = ex2_approx(fmaf(__uint_as_float(z[q]), p.c0, l0)) * g0;
+                        if (DUAL) v[q] = fmaf(ex2_approx(fmaf(__uint_as_float(z[q]), 1.4426950408889634f, l1)), g1, v[q]);
+                    }
+                    while (next_col < n + 32) {
+                        float off = g0;
+                        if constexpr (LIST) {
+                            const float q = p.tg.ev_w[static_cast<size_t>(t) * p.tg.events + e];
+                            off = q < 0.0f ? g1 : q * g0;
+                        }
+#pragma unroll
+                        for (int q = 0; q < 32; ++q) v[q] -= next_col - n == q ? off : 0.0f;
+                        if constexpr (LIST) {
+                            ++e;
+                            next_col = e < p.tg.events ? ev_col[e] : kNoColumn;
+                        } else {
+                            next_col = kNoColumn;
+                        }
+                    }
+                    uint32_t o[16];
+#pragma unroll
+                    for (int q = 0; q < 16; ++q) {
+                        const bool in0 = here && n + 2 * q < p.N, in1 = here && n + 2 * q + 1 < p.N;
+                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[q]) : "f"(in1 ? v[2 * q + 1] : 0.0f), "f"(in0 ? v[2 * q] : 0.0f));
+                    }
+                    uint4* to = reinterpret_cast<uint4*>(p.dz + static_cast<size_t>(r) * p.ldz + (n - p.v0));
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) to[q] = make_uint4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
+                }
+            }
+            if constexpr (MODE == 0) {
+                if (here) store_part(tile, m, s0, s1);
+            }
+        }
+        __device__ void store_part(const Tile& tile, float m, float s0, float s1) const {
+            const size_t at = static_cast<size_t>(r) * w.p.parts + 2 * ((tile.n0 - w.p.v0) / tile.bn) + parity;
+            w.p.part[at] = make_float2(m, s0);
+            if (DUAL) w.p.part1[at] = s1;
+        }
+    };
+};
+
+template <int MODE, bool LIST, bool DUAL>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairLoopThreads, 1)
+head_logits_kernel(const __grid_constant__ HeadMaps maps, const __grid_constant__ HeadLogitsParams p) {
+    pdl_launch_dependents();
+    HeadLogitsWork<MODE, LIST, DUAL> work(maps, p);
+    bf16_pair_loop(work, p.skip_loads != 0);
+}
+
+// ---- gradients of a piece --------------------------------------------------------------------------
+struct HeadGradMaps {
+    CUtensorMap aw;               // dz piece for dW: MN-major, two blocks of 64 columns
+    CUtensorMap ax;               // dz piece for dx: K-major
+    CUtensorMap bx[2], bxc[2];    // x, or the rows that count moved together: MN-major, two blocks, one block (half tiles)
+    CUtensorMap bw[2];            // the piece's rows of W
+};
+struct HeadGradParams {
+    const int* count;
+    int T, K;
+    int cols;                     // vocabulary rows of the piece
+    uint16_t* dw;                 // [cols][K], or null with no tiles of part 0
+    float* acc;                   // dx sums: [slots][T][K]
+    int slot_stages;              // dx's contraction is cut into slices of that many stages, each with a slot of its own
+    int add;                      // not the first piece: add to acc
+    BackwardPlan plan;            // part 0: dW, part 1: dx (tile index = slice * tiles of dx + tile)
+    int skip_loads;
+};
+
+struct HeadGradsWork {
+    const HeadGradMaps& maps;
+    const HeadGradParams& p;
+    int rows;
+    bool moved;
+
+    __device__ HeadGradsWork(const HeadGradMaps& m, const HeadGradParams& q) : maps(m), p(q) {}
+    __device__ void start() {
+        rows = *p.count;
+        moved = rows < p.T;
+    }
+
+    struct Tile { int part, m0, n0, bn, k_stages, k_first, slot; };
+    struct Tiles {
+        const HeadGradsWork& w;
+        int pair, g, i;
+        __device__ Tiles(const HeadGradsWork& work, int pr) : w(work), pair(pr), g(0), i(0) {}
+        __device__ bool next(Tile& t) {
+            const HeadGradParams& p = w.p;
+            for (; g < p.plan.segments; ++g, i = 0) {
+                const BackwardSegment& sg = p.plan.seg[g];
+                while (i < sg.count(pair)) {
+                    const int u = sg.index(pair, i++);
+                    t.part = sg.part;
+                    t.bn = sg.half ? 128 : 256;
+                    const int tiles_m = ((t.part == 0 ? p.cols : p.T) + 255) / 256;
+                    int tile = sg.half ? sg.first_tile + (u >> 1) : u;
+                    t.slot = 0;
+                    t.k_first = 0;
+                    if (t.part == 0) {
+                        t.k_stages = (max(w.rows, 1) + 63) / 64;
+                    } else {
+                        const int tiles = tiles_m * ((p.K + 255) / 256);
+                        t.slot = tile / tiles;
+                        tile -= t.slot * tiles;
+                        t.k_first = t.slot * p.slot_stages;
+                        t.k_stages = min(p.slot_stages, (p.cols + 63) / 64 - t.k_first);
+                    }
+                    t.m0 = (tile % tiles_m) * 256;
+                    t.n0 = (tile / tiles_m) * 256 + (sg.half ? (u & 1) * 128 : 0);
+                    if (t.part == 1 && t.m0 >= w.rows) continue;            // rows left out
+                    return true;
+                }
+            }
+            return false;
+        }
+    };
+
+    __device__ void load(const Tile& t, int ks, uint32_t rank, uint32_t st, uint32_t bar) const {
+        const int m0 = t.m0 + static_cast<int>(rank) * 128, n0 = t.n0 + static_cast<int>(rank) * (t.bn >> 1);
+        const int half = t.bn == 128, k = (t.k_first + ks) * 64;
+        if (t.part == 0) tma_load_3d_pair(st, &maps.aw, 0, k, m0 >> 6, bar);
+        else tma_load_2d_pair(st, &maps.ax, k, m0, bar);
+        const CUtensorMap* b = t.part == 1 ? &maps.bw[half] : (moved ? &maps.bxc[half] : &maps.bx[half]);
+        tma_load_3d_pair(st + kPairLoopStageA, b, 0, k, n0 >> 6, bar);
+    }
+    // K = 16 elements per instruction: 16 rows of an MN-major operand, 32 B along a row of a K-major one
+    __device__ uint32_t idesc(const Tile& t) const { return make_idesc_bf16_any(256, t.bn, t.part == 0, true); }
+    __device__ uint64_t a_step(const Tile& t) const { return t.part == 0 ? (2048 >> 4) : (32 >> 4); }
+    __device__ uint64_t b_step(const Tile&) const { return 2048 >> 4; }
+    __device__ uint64_t a_desc(const Tile& t, uint32_t s) const { return make_smem_desc(s, t.part == 0 ? 8192 : 16, 1024, kSwz128); }
+    __device__ uint64_t b_desc(const Tile&, uint32_t s) const { return make_smem_desc(s, 8192, 1024, kSwz128); }
+
+    struct Epilogue {
+        const HeadGradsWork& w;
+        int rank, quarter, parity, lane;
+        __device__ Epilogue(const HeadGradsWork& work, int rk, int q, int par, int ln) : w(work), rank(rk), quarter(q), parity(par), lane(ln) {}
+        __device__ void begin(const Tile&) {}
+
+        template <class Release>
+        __device__ void run(const Tile& t, uint32_t taddr, Release&& release) {
+            const HeadGradParams& p = w.p;
+            const int m = t.m0 + rank * 128 + quarter * 32 + lane;
+            const int chunks = t.bn >> 5;
+            const bool mine = m < (t.part == 0 ? p.cols : w.rows);
+#pragma unroll 1
+            for (int c = parity; c < chunks; c += 2) {
+                uint32_t v[32];
+                __syncwarp();
+                tmem_ld_32x32b_x32(taddr + static_cast<uint32_t>(c * 32), v);
+                tmem_ld_wait();
+                if (c + 2 >= chunks) release();
+                const int n = t.n0 + c * 32;
+                if (!mine || n >= p.K) continue;            // K % 32 == 0: a chunk is in or out as a whole
+                if (t.part == 0) {
+                    uint32_t o[16];
+#pragma unroll
+                    for (int q = 0; q < 16; ++q)
+                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[q]) : "f"(__uint_as_float(v[2 * q + 1])), "f"(__uint_as_float(v[2 * q])));
+                    uint4* to = reinterpret_cast<uint4*>(p.dw + static_cast<size_t>(m) * p.K + n);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) to[q] = make_uint4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
+                } else {
+                    float* to = p.acc + (static_cast<size_t>(t.slot) * p.T + m) * p.K + n;
+                    // One tile of a launch writes an element, and launches follow one another: the sum's order is fixed
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) {
+                        if (p.add)
+                            asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};"
+                                         ::"l"(to + 4 * q), "f"(__uint_as_float(v[4 * q])), "f"(__uint_as_float(v[4 * q + 1])),
+                                           "f"(__uint_as_float(v[4 * q + 2])), "f"(__uint_as_float(v[4 * q + 3])) : "memory");
+                        else
+                            *reinterpret_cast<uint4*>(to + 4 * q) = make_uint4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+                    }
+                }
+            }
+        }
+    };
+};
+
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairLoopThreads, 1)
+head_grads_kernel(const __grid_constant__ HeadGradMaps maps, const __grid_constant__ HeadGradParams p) {
+    pdl_launch_dependents();
+    HeadGradsWork work(maps, p);
+    bf16_pair_loop(work, p.skip_loads != 0);
+}
+
+}  // namespace sbn

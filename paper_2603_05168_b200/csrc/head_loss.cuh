@@ -1,0 +1,247 @@
+// Host side of the losses at the output head: workspaces, pieces of the vocabulary, launches.  Included by libsbn.cu.
+#pragma once
+
+#include "head_gemm_tcgen05.cuh"
+
+namespace sbn {
+
+// How a call is cut up, from its sizes alone.
+struct HeadPlan {
+    int bn, parts;                // forward: columns per tile, partial sums per row
+    int piece;                    // backward: columns of dz at a time (a multiple of 256)
+    int bn_piece;                 // columns per tile of the pieces' logits
+    int slots, slot_stages;       // slices of dx's contraction over a piece, and 64-column stages of each
+    long long rows64, rows256;    // T up to a multiple
+};
+
+static inline long long head_up(long long v, long long to) { return (v + to - 1) / to * to; }
+
+// Columns per tile of z: as wide as possible (a wide tile reads its rows for more columns), narrower where the tiles would
+// not go round.  Time per stage in us: the MMAs of 256 columns take 0.36; a narrow tile's two loads 0.19.
+static int head_tile_columns(int T, int cols, int K) {
+    int best = 256;
+    double best_cost = 1e300;
+    for (int bn = 256; bn >= 64; bn >>= 1) {
+        const double tiles = static_cast<double>(head_up(T, 256) / 256) * ((cols + bn - 1) / bn);
+        const double rounds = std::ceil(tiles / kBackwardPairs);
+        const double cost = rounds * (std::max(0.36 * bn / 256, 0.19) * (K / 64) + 1.0);
+        if (cost < best_cost * 0.99) { best_cost = cost; best = bn; }
+    }
+    return best;
+}
+
+static HeadPlan head_plan(int T, int N, int K) {
+    HeadPlan h;
+    h.rows64 = head_up(T, 64);
+    h.rows256 = head_up(T, 256);
+    h.bn = head_tile_columns(T, N, K);
+    h.parts = 2 * ((N + h.bn - 1) / h.bn);
+    long long cols = (128ll << 20) / (2 * h.rows256);
+    if (T <= 512) cols = std::min(cols, (40ll << 20) / (2ll * K));      // few tokens: the piece's rows of W stay in the L2 for dx
+    cols = std::max(1024ll, cols / 256 * 256);
+    const long long pieces = (N + cols - 1) / cols;
+    h.piece = static_cast<int>(head_up((N + pieces - 1) / pieces, 256));
+    h.bn_piece = head_tile_columns(T, std::min(N, h.piece), K);
+    const int dx_tiles = static_cast<int>(h.rows256 / 256) * ((K + 255) / 256);
+    const int stages = (std::min(h.piece, N) + 63) / 64, slots = std::max(1, std::min((kBackwardPairs + dx_tiles / 2) / dx_tiles, stages));
+    h.slot_stages = (stages + slots - 1) / slots;
+    h.slots = (stages + h.slot_stages - 1) / h.slot_stages;             // all of them are written by the first piece
+    return h;
+}
+
+// Workspace of a call, in bytes from its start.
+struct HeadWs {
+    size_t count, row_src, row_of, flags, ev_col, ev_w, xc, z_ev, part, part1, dz, acc, total;
+};
+static HeadWs head_ws_layout(const HeadPlan& h, bool backward, int T, int K, int top) {
+    HeadWs w{};
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) & ~static_cast<size_t>(255); return here; };
+    const size_t t = static_cast<size_t>(T), events = top ? static_cast<size_t>(top) + 1 : 1;
+    w.count = take(4);
+    w.row_src = take(4 * t);
+    w.row_of = take(4 * t);
+    if (top) {
+        w.flags = take(t);
+        w.ev_col = take(4 * t * events);
+        w.ev_w = take(4 * t * events);
+    }
+    w.xc = take(2 * static_cast<size_t>(h.rows64) * K);
+    if (!backward) {
+        w.z_ev = take(4 * t * events);
+        w.part = take(8 * t * h.parts);
+        if (top) w.part1 = take(4 * t * h.parts);
+    } else {
+        w.dz = take(2 * static_cast<size_t>(h.rows256) * h.piece);
+        w.acc = take(4 * static_cast<size_t>(h.slots) * t * K);
+    }
+    w.total = at;
+    return w;
+}
+
+// One call of either operator: top == 0 is the cross entropy.
+struct HeadCall {
+    const void* x;
+    int T, K;
+    const void* head;
+    int N;
+    const long long* labels;
+    const long long* top_index;
+    const void* top_logits;
+    int top_bf16, top;
+    float tau;
+    char* ws;
+};
+
+static bool head_encode(const HeadCall& c, const HeadPlan& h, const HeadWs& w, int bn, HeadMaps* maps) {
+    const uint64_t k = static_cast<uint64_t>(c.K);
+    return encode_2d_bf16_sw128(&maps->x, c.x, k, c.T, k, 128) && encode_2d_bf16_sw128(&maps->xc, c.ws + w.xc, k, h.rows64, k, 128) &&
+           encode_2d_bf16_sw128(&maps->w, c.head, k, c.N, k, bn / 2);
+}
+
+template <int MODE, bool LIST, bool DUAL>
+static sbn_status launch_head_logits_as(const HeadMaps& maps, const HeadLogitsParams& p, cudaStream_t stream) {
+    if (!ensure_dynamic_smem<head_logits_kernel<MODE, LIST, DUAL>>(kPairLoopSmemBytes)) return SBN_ERR_CUDA;
+    const long long tiles = head_up(p.T, 256) / 256 * ((p.v1 - p.v0 + p.bn - 1) / p.bn);
+    const unsigned pairs = static_cast<unsigned>(std::min<long long>(tiles, kBackwardPairs));
+    if (launch_kernel(head_logits_kernel<MODE, LIST, DUAL>, dim3(2 * pairs), dim3(kPairLoopThreads), kPairLoopSmemBytes, stream, maps, p) != cudaSuccess)
+        return SBN_ERR_CUDA;
+    ++g_launch_count;
+    return SBN_OK;
+}
+template <int MODE>
+static sbn_status launch_head_logits(const HeadMaps& maps, const HeadLogitsParams& p, bool list, bool dual, cudaStream_t stream) {
+    if (!list) return launch_head_logits_as<MODE, false, false>(maps, p, stream);
+    return dual ? launch_head_logits_as<MODE, true, true>(maps, p, stream) : launch_head_logits_as<MODE, true, false>(maps, p, stream);
+}
+
+// What both directions begin with: targets (distillation) and the rows that count.
+static sbn_status launch_head_rows(const HeadCall& c, const HeadWs& w, HeadRowsJob rows, HeadTargets* tg, cudaStream_t stream) {
+    tg->labels = c.labels;
+    tg->flags = nullptr;
+    tg->ev_col = nullptr;
+    tg->ev_w = nullptr;
+    tg->events = 1;
+    if (c.top) {
+        HeadTargetsJob t{c.top_index, c.top_logits, c.top_bf16, c.top, c.T, c.N, static_cast<float>(1.0 / static_cast<double>(c.tau)), c.labels,
+                         reinterpret_cast<unsigned char*>(c.ws + w.flags), reinterpret_cast<int*>(c.ws + w.ev_col),
+                         reinterpret_cast<float*>(c.ws + w.ev_w)};
+        const int blocks = std::min((c.T + kTargetWarps - 1) / kTargetWarps, 16 * device_sm_count());
+        if (launch_kernel(head_targets_kernel, dim3(blocks), dim3(32 * kTargetWarps), 0, stream, t) != cudaSuccess) return SBN_ERR_CUDA;
+        ++g_launch_count;
+        tg->flags = t.flags;
+        tg->ev_col = t.ev_col;
+        tg->ev_w = t.ev_w;
+        tg->events = c.top + (c.labels ? 1 : 0);
+    }
+    rows.labels = c.labels;
+    rows.flags = tg->flags;
+    rows.x = static_cast<const uint16_t*>(c.x);
+    rows.T = c.T;
+    rows.K = c.K;
+    rows.N = c.N;
+    rows.count = reinterpret_cast<int*>(c.ws + w.count);
+    rows.row_src = reinterpret_cast<int*>(c.ws + w.row_src);
+    rows.xc = reinterpret_cast<uint16_t*>(c.ws + w.xc);
+    const int blocks = std::min(c.T, 2 * device_sm_count()), per = (c.T + blocks - 1) / blocks;
+    if (launch_kernel(head_rows_kernel, dim3((c.T + per - 1) / per), dim3(kRowsThreads), 0, stream, rows, per) != cudaSuccess) return SBN_ERR_CUDA;
+    ++g_launch_count;
+    return SBN_OK;
+}
+
+static sbn_status head_forward(const HeadCall& c, float* loss0, float* loss1, float* lse0, float* lse1, cudaStream_t stream) {
+    const HeadPlan h = head_plan(c.T, c.N, c.K);
+    const HeadWs w = head_ws_layout(h, false, c.T, c.K, c.top);
+    HeadMaps maps;
+    if (!head_encode(c, h, w, h.bn, &maps)) return SBN_ERR_CUDA;
+    HeadRowsJob rows{};
+    rows.loss0 = loss0; rows.loss1 = loss1; rows.lse0 = lse0; rows.lse1 = lse1;
+    HeadLogitsParams p{};
+    sbn_status st = launch_head_rows(c, w, rows, &p.tg, stream);
+    if (st != SBN_OK) return st;
+    const bool list = c.top != 0, dual = list && c.labels;
+    p.count = reinterpret_cast<int*>(c.ws + w.count);
+    p.row_src = reinterpret_cast<int*>(c.ws + w.row_src);
+    p.T = c.T; p.N = c.N; p.K = c.K;
+    p.v0 = 0; p.v1 = c.N; p.bn = h.bn;
+    p.c0 = static_cast<float>(1.4426950408889634 / static_cast<double>(c.tau));
+    p.part = reinterpret_cast<float2*>(c.ws + w.part);
+    p.part1 = dual ? reinterpret_cast<float*>(c.ws + w.part1) : nullptr;
+    p.z_ev = reinterpret_cast<float*>(c.ws + w.z_ev);
+    p.parts = h.parts;
+    p.skip_loads = g_test_break_waits;
+    st = launch_head_logits<0>(maps, p, list, dual, stream);
+    if (st != SBN_OK) return st;
+    const HeadLossJob j{p.tg, p.count, p.row_src, p.part, p.part1, p.z_ev, h.parts, 1.0 / static_cast<double>(c.tau), loss0, loss1, lse0, lse1};
+    const int blocks = std::min((c.T + kLossWarps - 1) / kLossWarps, 8 * device_sm_count());
+    if (launch_kernel(head_losses_kernel, dim3(blocks), dim3(32 * kLossWarps), 0, stream, j) != cudaSuccess) return SBN_ERR_CUDA;
+    ++g_launch_count;
+    return SBN_OK;
+}
+
+static sbn_status head_backward(const HeadCall& c, const float* lse0, const float* lse1, const float* g0, const float* g1, void* dx, void* dhead,
+                                cudaStream_t stream) {
+    const HeadPlan h = head_plan(c.T, c.N, c.K);
+    const HeadWs w = head_ws_layout(h, true, c.T, c.K, c.top);
+    const uint64_t k = static_cast<uint64_t>(c.K), t = static_cast<uint64_t>(c.T);
+    HeadMaps maps;
+    HeadGradMaps gm;
+    if (!head_encode(c, h, w, h.bn_piece, &maps)) return SBN_ERR_CUDA;
+    bool ok = encode_3d_bf16_blocks(&gm.aw, c.ws + w.dz, h.piece, h.rows256, 2) && encode_2d_bf16_sw128(&gm.ax, c.ws + w.dz, h.piece, h.rows256, h.piece, 128);
+    for (int half = 0; ok && half < 2; ++half)
+        ok = encode_3d_bf16_blocks(&gm.bx[half], c.x, k, t, half ? 1 : 2) && encode_3d_bf16_blocks(&gm.bxc[half], c.ws + w.xc, k, h.rows64, half ? 1 : 2);
+    if (!ok || !ensure_dynamic_smem<head_grads_kernel>(kPairLoopSmemBytes)) return SBN_ERR_CUDA;
+    HeadRowsJob rows{};
+    rows.row_of = reinterpret_cast<int*>(c.ws + w.row_of);
+    HeadLogitsParams p{};
+    sbn_status st = launch_head_rows(c, w, rows, &p.tg, stream);
+    if (st != SBN_OK) return st;
+    const bool list = c.top != 0, dual = list && c.labels;
+    p.count = reinterpret_cast<int*>(c.ws + w.count);
+    p.row_src = reinterpret_cast<int*>(c.ws + w.row_src);
+    p.T = c.T; p.N = c.N; p.K = c.K;
+    p.bn = h.bn_piece;
+    p.c0 = static_cast<float>(1.4426950408889634 / static_cast<double>(c.tau));
+    p.inv_tau = static_cast<float>(1.0 / static_cast<double>(c.tau));
+    p.lse0 = lse0; p.lse1 = lse1; p.g0 = g0; p.g1 = g1;
+    p.dz = reinterpret_cast<uint16_t*>(c.ws + w.dz);
+    p.ldz = h.piece;
+    p.skip_loads = g_test_break_waits;
+    HeadGradParams q{};
+    q.count = p.count;
+    q.T = c.T; q.K = c.K;
+    q.acc = reinterpret_cast<float*>(c.ws + w.acc);
+    q.slot_stages = h.slot_stages;
+    q.skip_loads = g_test_break_waits;
+    const int tiles_k = (c.K + 255) / 256;
+    for (int v0 = 0; v0 < c.N; v0 += h.piece) {
+        const int cols = std::min(h.piece, c.N - v0);
+        p.v0 = v0; p.v1 = v0 + cols;
+        st = launch_head_logits<1>(maps, p, list, dual, stream);
+        if (st != SBN_OK) return st;
+        const char* w_rows = static_cast<const char*>(c.head) + static_cast<size_t>(v0) * c.K * 2;
+        for (int half = 0; half < 2; ++half)
+            if (!encode_3d_bf16_blocks(&gm.bw[half], w_rows, k, cols, half ? 1 : 2)) return SBN_ERR_CUDA;
+        const int all_stages = (cols + 63) / 64;
+        q.cols = cols;
+        q.dw = dhead ? static_cast<uint16_t*>(dhead) + static_cast<size_t>(v0) * c.K : nullptr;
+        q.add = v0 > 0;
+        const int slices = (all_stages + h.slot_stages - 1) / h.slot_stages;     // fewer in a short last piece
+        const int tiles[2] = {dhead ? (cols + 255) / 256 * tiles_k : 0, dx ? static_cast<int>(h.rows256 / 256) * tiles_k * slices : 0};
+        const int stages[2] = {(c.T + 63) / 64, h.slot_stages};
+        q.plan = plan_backward(tiles, stages, -1);
+        if (launch_kernel(head_grads_kernel, dim3(2 * kBackwardPairs), dim3(kPairLoopThreads), kPairLoopSmemBytes, stream, gm, q) != cudaSuccess)
+            return SBN_ERR_CUDA;
+        ++g_launch_count;
+    }
+    if (dx) {
+        const HeadDxJob j{rows.row_of, q.acc, h.slots, c.T, c.K, static_cast<uint16_t*>(dx)};
+        const long long steps = (static_cast<long long>(c.T) * (c.K / 8) + kDxThreads - 1) / kDxThreads;
+        const int blocks = static_cast<int>(std::min<long long>(steps, 16ll * device_sm_count()));
+        if (launch_kernel(head_dx_kernel, dim3(blocks), dim3(kDxThreads), 0, stream, j) != cudaSuccess) return SBN_ERR_CUDA;
+        ++g_launch_count;
+    }
+    return SBN_OK;
+}
+
+}  // namespace sbn

@@ -1,0 +1,321 @@
+// Losses at the output head, what is done per token (the products are in head_gemm_tcgen05.cuh):
+//
+//   head_targets_kernel   distillation: the teacher's entries of a row become probabilities q = softmax(l / tau), sorted by
+//                         index together with the label, so that a GEMM tile finds those that fall into its columns
+//   head_rows_kernel      which rows count at all.  Rows that nothing is asked of (label < 0, no teacher entries: padding,
+//                         prompts) are left out of every product: the rows that count move together, in their order, when
+//                         any is left out, so such rows cost no work and whatever they hold -- NaN, infinities -- reaches
+//                         nothing.  The count stays on the device; the GEMM kernels read it
+//   head_losses_kernel    log-sum-exp and losses from the partial maxima and sums of the logits kernel
+//   head_dx_kernel        sums of dx in fp32 -> bf16, back at the tokens' own rows, zeros in rows left out
+//
+// All memory-bound or latency-bound and small beside the products (4096 tokens: 2 to 10 us each).  No atomics: every result
+// is the same from run to run.
+#pragma once
+
+#include "sbn_common.cuh"
+
+namespace sbn {
+
+constexpr int kHeadMaxTop = 256;                  // teacher entries per token
+constexpr int kNoColumn = 0x7FFFFFFF;             // an event that is not there: behind every column
+
+// Per-row flags of a distillation (head_targets_kernel).
+constexpr int kRowDistill = 1, kRowLabel = 2, kRowBadTeacher = 4, kRowBadLabel = 8;
+
+// What a row's gradient or loss refers to.  Cross entropy: the label.  Distillation: `events` entries per row, sorted by
+// column; weight >= 0 is a teacher probability, -1 marks the label's entry.
+struct HeadTargets {
+    const long long* labels;                      // [T] or null
+    const unsigned char* flags;                   // [T], distillation only
+    const int* ev_col;                            // [T][events]
+    const float* ev_w;
+    int events;
+};
+
+struct HeadTargetsJob {
+    const long long* index;                       // [T][top]
+    const void* logits;                           // [T][top] fp32 or bf16
+    int logits_bf16, top, T, N;
+    float inv_tau;
+    const long long* labels;                      // or null
+    unsigned char* flags;
+    int* ev_col;
+    float* ev_w;
+};
+
+constexpr int kTargetWarps = 4;
+
+// A warp per token.  The rank of an entry is the number of entries before it (column, then position): top is at most 256,
+// so counting costs less than a sorting network's exchanges would.
+__global__ void __launch_bounds__(32 * kTargetWarps)
+head_targets_kernel(const HeadTargetsJob j) {
+    __shared__ int s_col[kTargetWarps][kHeadMaxTop + 1];
+    __shared__ float s_val[kTargetWarps][kHeadMaxTop];
+    pdl_launch_dependents();
+    pdl_wait();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    int* col = s_col[warp];
+    float* val = s_val[warp];
+    const int events = j.top + (j.labels != nullptr ? 1 : 0);
+    for (long long t = static_cast<long long>(blockIdx.x) * kTargetWarps + warp; t < j.T; t += static_cast<long long>(gridDim.x) * kTargetWarps) {
+        const long long* index = j.index + t * j.top;
+        float top_val = -INFINITY;
+        int bad = 0, any = 0;
+        for (int i = lane; i < j.top; i += 32) {
+            const long long c = index[i];
+            const float l = j.logits_bf16 ? __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t*>(j.logits)[t * j.top + i]) << 16)
+                                          : static_cast<const float*>(j.logits)[t * j.top + i];
+            const bool there = c >= 0 && c < j.N;
+            bad |= c >= j.N;
+            any |= there && !(l == -INFINITY);               // a NaN counts, and shows in the loss
+            col[i] = there ? static_cast<int>(c) : kNoColumn;
+            val[i] = there ? l : -INFINITY;
+            if (there) top_val = fmaxf(top_val, l);
+        }
+        top_val = warp_max(top_val);
+        bad = __any_sync(0xFFFFFFFFu, bad);
+        any = __any_sync(0xFFFFFFFFu, any) && !bad;
+        float sum = 0.0f;
+        for (int i = lane; i < j.top; i += 32) {
+            // the difference first: the type's lowest value, divided by a small temperature, would become -inf
+            const float e = val[i] == -INFINITY ? 0.0f : expf((val[i] - top_val) * j.inv_tau);
+            val[i] = e;
+            sum += e;
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+        unsigned char flags = static_cast<unsigned char>((any ? kRowDistill : 0) | (bad ? kRowBadTeacher : 0));
+        if (j.labels != nullptr) {
+            const long long y = j.labels[t];
+            if (y >= 0 && y < j.N) flags |= kRowLabel;
+            if (y >= j.N) flags |= kRowBadLabel;
+            if (lane == 0) col[j.top] = (flags & kRowLabel) ? static_cast<int>(y) : kNoColumn;
+        }
+        __syncwarp();
+        for (int i = lane; i < j.top; i += 32)
+            if (!any) col[i] = kNoColumn;
+        __syncwarp();
+        for (int i = lane; i < events; i += 32) {
+            const int c = col[i];
+            int rank = 0;
+            for (int o = 0; o < events; ++o) rank += (col[o] < c || (col[o] == c && o < i)) ? 1 : 0;
+            j.ev_col[t * events + rank] = c;
+            j.ev_w[t * events + rank] = i == j.top ? -1.0f : (c == kNoColumn ? 0.0f : val[i] / sum);
+        }
+        if (lane == 0) {
+            j.flags[t] = flags;
+            if (flags & (kRowBadTeacher | kRowBadLabel)) atomicExch(&g_device_status, static_cast<int>(SBN_ERR_INDEX));
+        }
+        __syncwarp();
+    }
+}
+
+struct HeadRowsJob {
+    const long long* labels;                      // cross entropy (flags null)
+    const unsigned char* flags;                   // distillation
+    const uint16_t* x;                            // [T][K]
+    int T, K, N;
+    int* count;                                   // out: number of rows that count
+    int* row_src;                                 // out [T]: token of row r
+    int* row_of;                                  // out [T] or null: row of token t, -1 if left out
+    uint16_t* xc;                                 // out [T up to a multiple of 64][K], written only if rows are left out
+    float *loss0, *loss1, *lse0, *lse1;           // forward: outputs of rows left out (any may be null): distillation / label
+};
+
+constexpr int kRowsThreads = 256;
+
+__device__ __forceinline__ int head_row_flags(const HeadRowsJob& j, int t) {
+    if (j.flags != nullptr) return j.flags[t];
+    const long long y = j.labels[t];
+    return y < 0 ? 0 : (y < j.N ? kRowLabel : kRowBadLabel);
+}
+
+// Sum of v over the block; every thread gets it.
+__device__ __forceinline__ int block_sum(int v, int* scratch) {
+    v = __reduce_add_sync(0xFFFFFFFFu, v);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
+    __syncthreads();
+    int s = 0;
+#pragma unroll
+    for (int w = 0; w < kRowsThreads / 32; ++w) s += scratch[w];
+    return s;
+}
+
+// CTA b has tokens [b per, (b + 1) per).  Every CTA counts all tokens itself (8 or 1 bytes each, from the L2) instead of
+// waiting for the others' counts: one launch, nothing to order.
+__global__ void __launch_bounds__(kRowsThreads)
+head_rows_kernel(const HeadRowsJob j, const int per) {
+    __shared__ int s_scratch[kRowsThreads / 32];
+    pdl_launch_dependents();
+    pdl_wait();
+    const int first = blockIdx.x * per, last = min(j.T, first + per);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    int before = 0, total = 0;
+    for (int t = tid; t < j.T; t += kRowsThreads) {
+        const int c = (head_row_flags(j, t) & (kRowDistill | kRowLabel)) ? 1 : 0;
+        total += c;
+        before += t < first ? c : 0;
+    }
+    total = block_sum(total, s_scratch);
+    before = block_sum(before, s_scratch);
+    if (blockIdx.x == 0 && tid == 0) *j.count = total;
+    for (int t0 = first; t0 < last; t0 += kRowsThreads) {
+        const int t = t0 + tid;
+        const int flags = t < last ? head_row_flags(j, t) : 0;
+        const bool counts = (flags & (kRowDistill | kRowLabel)) != 0;
+        const unsigned ballot = __ballot_sync(0xFFFFFFFFu, counts);
+        __syncthreads();
+        if (lane == 0) s_scratch[warp] = __popc(ballot);
+        __syncthreads();
+        int r = before, all = 0;
+#pragma unroll
+        for (int w = 0; w < kRowsThreads / 32; ++w) {
+            r += w < warp ? s_scratch[w] : 0;
+            all += s_scratch[w];
+        }
+        r += __popc(ballot & ((1u << lane) - 1u));
+        if (counts) j.row_src[r] = t;
+        if (t < last) {
+            if (j.row_of != nullptr) j.row_of[t] = counts ? r : -1;
+            if (j.flags == nullptr && (flags & kRowBadLabel)) atomicExch(&g_device_status, static_cast<int>(SBN_ERR_INDEX));
+            if (!counts) {
+                const float nan = __uint_as_float(0x7FC00000u);
+                if (j.loss0 != nullptr) j.loss0[t] = (flags & kRowBadTeacher) ? nan : 0.0f;
+                if (j.loss1 != nullptr) j.loss1[t] = (flags & kRowBadLabel) ? nan : 0.0f;
+                if (j.lse0 != nullptr) j.lse0[t] = 0.0f;
+                if (j.lse1 != nullptr) j.lse1[t] = 0.0f;
+            }
+        }
+        if (total < j.T) {
+            // the rows that count, 16 bytes at a time, one row after another
+            __syncthreads();
+            const int vecs = j.K >> 3;
+            for (int i = 0; i < all; ++i) {
+                const int src = j.row_src[before + i];
+                const uint4* from = reinterpret_cast<const uint4*>(j.x + static_cast<size_t>(src) * j.K);
+                uint4* to = reinterpret_cast<uint4*>(j.xc + static_cast<size_t>(before + i) * j.K);
+                for (int v = tid; v < vecs; v += kRowsThreads) to[v] = __ldg(from + v);
+            }
+        }
+        before += all;
+    }
+    if (total < j.T && blockIdx.x == gridDim.x - 1) {
+        // dW contracts over whole stages of 64 rows: zeros behind the last row that counts
+        const int rows = ((max(total, 1) + 63) & ~63) - total, vecs = j.K >> 3;
+        uint4* to = reinterpret_cast<uint4*>(j.xc + static_cast<size_t>(total) * j.K);
+        for (long long v = tid; v < static_cast<long long>(rows) * vecs; v += kRowsThreads) to[v] = make_uint4(0u, 0u, 0u, 0u);
+    }
+}
+
+struct HeadLossJob {
+    HeadTargets tg;
+    const int* count;
+    const int* row_src;
+    const float2* part;                           // [rows][parts]: maximum m of the raw logits, sum of exp((z - m) / tau)
+    const float* part1;                           // [rows][parts] or null: sum of exp(z - m)
+    const float* z_ev;                            // [rows][events]: logits at the events
+    int parts;
+    double inv_tau;
+    float *loss0, *loss1, *lse0, *lse1;           // at the tokens' own rows: distillation, label.  Cross entropy: loss1 and lse0
+};
+
+constexpr int kLossWarps = 4;
+
+// A warp per row.  In double: a loss is the small difference of two numbers near each other, and this is a few hundred
+// operations per token.
+__global__ void __launch_bounds__(32 * kLossWarps)
+head_losses_kernel(const HeadLossJob j) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const int lane = threadIdx.x & 31;
+    const int rows = *j.count;
+    for (int r = blockIdx.x * kLossWarps + (threadIdx.x >> 5); r < rows; r += gridDim.x * kLossWarps) {
+        const size_t p0 = static_cast<size_t>(r) * j.parts;
+        float m = -INFINITY;
+        for (int i = lane; i < j.parts; i += 32) m = fmaxf(m, j.part[p0 + i].x);
+        m = warp_max(m);
+        double s0 = 0.0, s1 = 0.0;
+        for (int i = lane; i < j.parts; i += 32) {            // parts without columns of the vocabulary hold (-inf, 0)
+            const float2 v = j.part[p0 + i];
+            s0 += static_cast<double>(v.y) * static_cast<double>(expf((v.x - m) * static_cast<float>(j.inv_tau)));
+            if (j.part1 != nullptr) s1 += static_cast<double>(j.part1[p0 + i]) * static_cast<double>(expf(v.x - m));
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            s0 += __shfl_xor_sync(0xFFFFFFFFu, s0, o);
+            s1 += __shfl_xor_sync(0xFFFFFFFFu, s1, o);
+        }
+        const int t = j.row_src[r];
+        const double lse0 = static_cast<double>(m) * j.inv_tau + log(s0);
+        if (j.tg.flags == nullptr) {                          // cross entropy
+            if (lane == 0) {
+                j.lse0[t] = static_cast<float>(lse0);
+                j.loss1[t] = static_cast<float>(lse0 - static_cast<double>(j.z_ev[r]));
+            }
+            continue;
+        }
+        const double lse1 = static_cast<double>(m) + (j.part1 != nullptr ? log(s1) : 0.0);
+        const int flags = j.tg.flags[t];
+        double kd = 0.0, ce = 0.0;
+        for (int i = lane; i < j.tg.events; i += 32) {
+            if (j.tg.ev_col[static_cast<size_t>(t) * j.tg.events + i] == kNoColumn) continue;
+            const float q = j.tg.ev_w[static_cast<size_t>(t) * j.tg.events + i];
+            const double z = static_cast<double>(j.z_ev[static_cast<size_t>(r) * j.tg.events + i]);
+            if (q < 0.0f) ce = lse1 - z;
+            else if (!(q == 0.0f)) kd += static_cast<double>(q) * (static_cast<double>(logf(q)) - z * j.inv_tau + lse0);
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            kd += __shfl_xor_sync(0xFFFFFFFFu, kd, o);
+            ce += __shfl_xor_sync(0xFFFFFFFFu, ce, o);
+        }
+        if (lane == 0) {
+            const float bad = __uint_as_float(0x7FC00000u);
+            j.loss0[t] = (flags & kRowBadTeacher) ? bad : static_cast<float>(kd);
+            j.lse0[t] = (flags & kRowDistill) ? static_cast<float>(lse0) : 0.0f;
+            if (j.loss1 != nullptr) {
+                j.loss1[t] = (flags & kRowBadLabel) ? bad : static_cast<float>(ce);
+                j.lse1[t] = (flags & kRowLabel) ? static_cast<float>(lse1) : 0.0f;
+            }
+        }
+    }
+}
+
+struct HeadDxJob {
+    const int* row_of;
+    const float* acc;                             // [slots][T][K]
+    int slots, T, K;
+    uint16_t* dx;                                 // [T][K]
+};
+
+constexpr int kDxThreads = 256;
+
+__global__ void __launch_bounds__(kDxThreads)
+head_dx_kernel(const HeadDxJob j) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const int vecs = j.K >> 3;                    // 8 values per thread and step
+    const long long all = static_cast<long long>(j.T) * vecs;
+    const size_t slot = static_cast<size_t>(j.T) * j.K;
+    for (long long i = static_cast<long long>(blockIdx.x) * kDxThreads + threadIdx.x; i < all; i += static_cast<long long>(gridDim.x) * kDxThreads) {
+        const int t = static_cast<int>(i / vecs), c = static_cast<int>(i - static_cast<long long>(t) * vecs);
+        const int r = j.row_of[t];
+        float v[8] = {};
+        if (r >= 0) {
+            const float* a = j.acc + static_cast<size_t>(r) * j.K + 8 * c;
+            for (int s = 0; s < j.slots; ++s, a += slot) {
+                const float4 lo = *reinterpret_cast<const float4*>(a), hi = *reinterpret_cast<const float4*>(a + 4);
+                v[0] += lo.x; v[1] += lo.y; v[2] += lo.z; v[3] += lo.w;
+                v[4] += hi.x; v[5] += hi.y; v[6] += hi.z; v[7] += hi.w;
+            }
+        }
+        uint32_t o[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[q]) : "f"(v[2 * q + 1]), "f"(v[2 * q]));
+        *reinterpret_cast<uint4*>(j.dx + static_cast<size_t>(t) * j.K + 8 * c) = make_uint4(o[0], o[1], o[2], o[3]);
+    }
+}
+
+}  // namespace sbn

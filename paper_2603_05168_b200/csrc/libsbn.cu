@@ -604,6 +604,12 @@ static sbn_status run_backward(const void* dY, int T, const int8_t* xq, const fl
     return SBN_OK;
 }
 
+}  // namespace sbn
+
+#include "head_loss.cuh"
+
+namespace sbn {
+
 // ------------------------------------------------------------------------------------------------
 // Built-in scratch for sbn_quantize_mask_pack_static_ws: part of the library image, so callers
 // that cannot allocate still have somewhere to put the pass-1 partial sums.  In host code the
@@ -1037,6 +1043,88 @@ sbn_status sbn_bitlinear_backward(const void* dY_bf16, int T, const int8_t* xq, 
     return run_backward(dY_bf16, T, xq, a_scale, vals, meta, w_scale, N, K, dX_bf16, dW, ws, s);
 }
 
+static bool head_shape_ok(int T, int N, int K) {
+    return T > 0 && N > 0 && K > 0 && K % kBK == 0 && K <= (1 << 20) && T <= (1 << 30) && N <= (1 << 30);
+}
+
+size_t sbn_head_workspace_bytes(int backward, int T, int N, int K, int top) {
+    if (!head_shape_ok(T, N, K) || top < 0 || top > kHeadMaxTop) return 0;
+    return head_ws_layout(head_plan(T, N, K), backward != 0, T, K, top).total;
+}
+
+// What the four calls check alike; `c` is filled in for them.
+static sbn_status head_call(HeadCall* c, bool backward, const void* x, int T, int K, const void* head, int N, const int64_t* labels,
+                            const int64_t* top_index, const void* top_logits, int top_dtype, int top, float tau, void* ws, size_t ws_bytes) {
+    if (!x || !head) return SBN_ERR_NULL;
+    if (!head_shape_ok(T, N, K)) return SBN_ERR_SHAPE;
+    if (!ws || ws_bytes < sbn_head_workspace_bytes(backward, T, N, K, top)) return SBN_ERR_WORKSPACE;
+    if (misaligned(x, 16) || misaligned(head, 16) || misaligned(ws, 256) || (labels && misaligned(labels, 8)) || (top_index && misaligned(top_index, 8)) ||
+        (top_logits && misaligned(top_logits, top_dtype == SBN_OUT_BF16 ? 2 : 4)))
+        return SBN_ERR_ALIGN;
+    *c = HeadCall{x, T, K, head, N, reinterpret_cast<const long long*>(labels), reinterpret_cast<const long long*>(top_index), top_logits,
+                  top_dtype == SBN_OUT_BF16, top, tau, static_cast<char*>(ws)};
+    return SBN_OK;
+}
+static sbn_status head_distill_args(const int64_t* top_index, const void* top_logits, int top_dtype, int top, float tau) {
+    if (!top_index || !top_logits) return SBN_ERR_NULL;
+    if (top < 1 || top > kHeadMaxTop || (top_dtype != SBN_OUT_F32 && top_dtype != SBN_OUT_BF16)) return SBN_ERR_UNSUPPORTED;
+    if (!(tau > 0.0f) || !std::isfinite(tau) || !std::isfinite(static_cast<float>(1.4426950408889634 / static_cast<double>(tau)))) return SBN_ERR_UNSUPPORTED;
+    return SBN_OK;
+}
+static sbn_status head_gradient_args(const void* x, const void* head, const void* dx, const void* dhead) {
+    if (!dx && !dhead) return SBN_ERR_NULL;
+    if (dx == x || dhead == head) return SBN_ERR_UNSUPPORTED;
+    if ((dx && misaligned(dx, 16)) || (dhead && misaligned(dhead, 16))) return SBN_ERR_ALIGN;
+    return SBN_OK;
+}
+
+sbn_status sbn_head_cross_entropy(const void* x_bf16, int T, int K, const void* head_bf16, int N, const int64_t* labels, float* loss, float* lse,
+                                  void* ws, size_t ws_bytes, void* stream) {
+    if (!labels || !loss || !lse) return SBN_ERR_NULL;
+    HeadCall c;
+    const sbn_status st = head_call(&c, false, x_bf16, T, K, head_bf16, N, labels, nullptr, nullptr, SBN_OUT_F32, 0, 1.0f, ws, ws_bytes);
+    if (st != SBN_OK) return st;
+    if (misaligned(loss, 4) || misaligned(lse, 4)) return SBN_ERR_ALIGN;
+    return head_forward(c, nullptr, loss, lse, nullptr, static_cast<cudaStream_t>(stream));
+}
+
+sbn_status sbn_head_cross_entropy_backward(const void* x_bf16, int T, int K, const void* head_bf16, int N, const int64_t* labels, const float* lse,
+                                           const float* dloss, void* dx_bf16, void* dhead_bf16, void* ws, size_t ws_bytes, void* stream) {
+    if (!labels || !lse || !dloss) return SBN_ERR_NULL;
+    HeadCall c;
+    sbn_status st = head_call(&c, true, x_bf16, T, K, head_bf16, N, labels, nullptr, nullptr, SBN_OUT_F32, 0, 1.0f, ws, ws_bytes);
+    if (st == SBN_OK) st = head_gradient_args(x_bf16, head_bf16, dx_bf16, dhead_bf16);
+    if (st != SBN_OK) return st;
+    if (misaligned(lse, 4) || misaligned(dloss, 4)) return SBN_ERR_ALIGN;
+    return head_backward(c, lse, nullptr, dloss, nullptr, dx_bf16, dhead_bf16, static_cast<cudaStream_t>(stream));
+}
+
+sbn_status sbn_head_distill(const void* x_bf16, int T, int K, const void* head_bf16, int N, const int64_t* top_index, const void* top_logits,
+                            sbn_out_dtype top_dtype, int top, float temperature, const int64_t* labels, float* distill_loss, float* ce_loss, float* lse,
+                            void* ws, size_t ws_bytes, void* stream) {
+    if (!distill_loss || !lse || (labels != nullptr) != (ce_loss != nullptr)) return SBN_ERR_NULL;
+    HeadCall c;
+    sbn_status st = head_distill_args(top_index, top_logits, top_dtype, top, temperature);
+    if (st == SBN_OK) st = head_call(&c, false, x_bf16, T, K, head_bf16, N, labels, top_index, top_logits, top_dtype, top, temperature, ws, ws_bytes);
+    if (st != SBN_OK) return st;
+    if (misaligned(distill_loss, 4) || misaligned(lse, 4) || (ce_loss && misaligned(ce_loss, 4))) return SBN_ERR_ALIGN;
+    return head_forward(c, distill_loss, ce_loss, lse, labels ? lse + T : nullptr, static_cast<cudaStream_t>(stream));
+}
+
+sbn_status sbn_head_distill_backward(const void* x_bf16, int T, int K, const void* head_bf16, int N, const int64_t* top_index, const void* top_logits,
+                                     sbn_out_dtype top_dtype, int top, float temperature, const int64_t* labels, const float* lse,
+                                     const float* d_distill, const float* d_ce, void* dx_bf16, void* dhead_bf16, void* ws, size_t ws_bytes,
+                                     void* stream) {
+    if (!lse || !d_distill || (labels != nullptr) != (d_ce != nullptr)) return SBN_ERR_NULL;
+    HeadCall c;
+    sbn_status st = head_distill_args(top_index, top_logits, top_dtype, top, temperature);
+    if (st == SBN_OK) st = head_call(&c, true, x_bf16, T, K, head_bf16, N, labels, top_index, top_logits, top_dtype, top, temperature, ws, ws_bytes);
+    if (st == SBN_OK) st = head_gradient_args(x_bf16, head_bf16, dx_bf16, dhead_bf16);
+    if (st != SBN_OK) return st;
+    if (misaligned(lse, 4) || misaligned(d_distill, 4) || (d_ce && misaligned(d_ce, 4))) return SBN_ERR_ALIGN;
+    return head_backward(c, lse, labels ? lse + T : nullptr, d_distill, d_ce, dx_bf16, dhead_bf16, static_cast<cudaStream_t>(stream));
+}
+
 sbn_status sbn_check_status(void* stream) {
     if (cudaStreamSynchronize(static_cast<cudaStream_t>(stream)) != cudaSuccess) return SBN_ERR_CUDA;
     int h = 0;
@@ -1059,6 +1147,7 @@ const char* sbn_status_string(sbn_status s) {
         case SBN_ERR_WORKSPACE: return "workspace missing or too small";
         case SBN_ERR_CUDA: return "CUDA call failed";
         case SBN_ERR_TIMEOUT: return "a bounded device-side wait ran out";
+        case SBN_ERR_INDEX: return "a label or a teacher's index is not in the vocabulary";
         case SBN_ERR_TOO_LARGE: return "problem larger than the library's built-in scratch can serve";
         default: return "unknown status";
     }

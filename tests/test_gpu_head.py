@@ -1,0 +1,489 @@
+"""The losses at the output head (cross entropy, distillation) and their gradients on the GPU, through the C ABI, against the
+float64 definitions of ``oracle/head.py`` within the bounds derived there."""
+import pytest
+import torch
+
+from oracle import head as oh
+from paper_2603_05168_b200 import binding as b
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16, I64 = torch.float32, torch.bfloat16, torch.int64
+NAN, INF = float("nan"), float("inf")
+
+
+@pytest.fixture(autouse=True)
+def _clean_status():
+    yield
+    b.sbn_check_status()
+
+
+def make(T, N, K, seed, ignored=0.3, lean=1.0, scale=0.02, top=0, dtype=F32, labels=True, absent=0.2):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    rand = lambda *s: torch.rand(*s, generator=g, device="cuda")
+    randn = lambda *s: torch.randn(*s, generator=g, device="cuda")
+    head = (randn(N, K) * scale).to(BF16)
+    y = torch.randint(0, N, (T,), generator=g, device="cuda")
+    x = (randn(T, K) + lean * rand(T, 1) * 5.0 / (scale * K) * head[y].float() / scale).to(BF16)
+    c = dict(T=T, N=N, K=K, x=x, head=head, tau=1.0)
+    if labels:
+        c["labels"] = torch.where(rand(T) < ignored, torch.full_like(y, -100), y)
+        c["d_ce"] = (rand(T) + 0.5) / T
+    if top:
+        idx = torch.randint(0, N, (T, top), generator=g, device="cuda")          # an index may come twice
+        idx[:, 0] = y
+        idx = torch.where(rand(T, top) < absent, -1 - idx % 7, idx)
+        idx[rand(T) < ignored] = -1
+        c["top_index"], c["top_logits"] = idx, (randn(T, top) * 3.0).to(dtype)
+        c["d_distill"] = (rand(T) + 0.5) / T
+    return c
+
+
+def forward(c, ws=None, dirty=True):
+    T, N, K = c["T"], c["N"], c["K"]
+    out = {}
+    top = c["top_index"].shape[1] if "top_index" in c else 0
+    ws = b.alloc_head_ws(T, N, K, top=top) if ws is None else ws
+    if dirty:
+        ws.fill_(0xFF)                                     # NaN everywhere: contents need no initialisation
+    if not top:
+        loss, lse = torch.full((T,), NAN, device="cuda"), torch.full((T,), NAN, device="cuda")
+        b.sbn_head_cross_entropy(c["x"], c["head"], c["labels"], loss, lse, ws=ws)
+        return dict(ce=loss, lse_ce=lse, lse=lse)
+    labels = c.get("labels")
+    lse = torch.full((1 if labels is None else 2, T), NAN, device="cuda")
+    out["distill"] = torch.full((T,), NAN, device="cuda")
+    if labels is not None:
+        out["ce"] = torch.full((T,), NAN, device="cuda")
+    b.sbn_head_distill(c["x"], c["head"], c["top_index"], c["top_logits"], c["tau"], out["distill"], lse, labels=labels,
+                       ce_loss=out.get("ce"), ws=ws)
+    out["lse"], out["lse_distill"] = lse, lse[0]
+    if labels is not None:
+        out["lse_ce"] = lse[1]
+    return out
+
+
+def backward(c, lse, dx=True, dhead=True, ws=None, dirty=True):
+    T, N, K = c["T"], c["N"], c["K"]
+    top = c["top_index"].shape[1] if "top_index" in c else 0
+    ws = b.alloc_head_ws(T, N, K, top=top, backward=True) if ws is None else ws
+    if dirty:
+        ws.fill_(0xFF)
+    dx = torch.full((T, K), NAN, dtype=BF16, device="cuda") if dx else None
+    dhead = torch.full((N, K), NAN, dtype=BF16, device="cuda") if dhead else None
+    if not top:
+        b.sbn_head_cross_entropy_backward(c["x"], c["head"], c["labels"], lse, c["d_ce"], dx=dx, dhead=dhead, ws=ws)
+    else:
+        b.sbn_head_distill_backward(c["x"], c["head"], c["top_index"], c["top_logits"], c["tau"], lse, c["d_distill"],
+                                    labels=c.get("labels"), d_ce=c.get("d_ce") if "labels" in c else None, dx=dx, dhead=dhead, ws=ws)
+    return dx, dhead
+
+
+def reference(c):
+    kw = dict(tau=c["tau"], d_ce=c.get("d_ce"), d_distill=c.get("d_distill"))
+    o = oh.head_loss(c["x"], c["head"], c.get("labels"), c.get("top_index"), c.get("top_logits"), **kw)
+    return o, oh.bounds(o, **kw)
+
+
+def assert_near(name, got, want, bound):
+    err = (got.double() - want).abs()
+    bad = torch.nonzero(~(err <= bound))
+    assert bad.numel() == 0, (f"{name}: {bad.shape[0]} of {err.numel()} beyond the bound, first at {bad[0].tolist()}: got "
+                              f"{got[tuple(bad[0])].item()}, want {want[tuple(bad[0])].item()}, bound {bound[tuple(bad[0])].item()}")
+
+
+def check(c, o=None, bd=None):
+    if o is None:
+        o, bd = reference(c)
+    f = forward(c)
+    for name in ("ce", "distill", "lse_ce", "lse_distill"):
+        if name in f and name in o:
+            assert_near(name, f[name], o[name], bd[name])
+    dx, dhead = backward(c, f["lse"])
+    b.sbn_check_status()
+    assert_near("dx", dx, o["dx"], bd["dx"])
+    assert_near("dhead", dhead, o["dhead"], bd["dhead"])
+    assert not dx[~o["counts"]].any()
+    return f, dx, dhead
+
+
+# one token, one word, widths that leave part of a tile, of a chunk, of a stage; rows around the tile's 32, 64, 128, 256
+CE_SHAPES = [(1, 1, 128), (1, 2, 128), (1, 1009, 256), (2, 33, 128), (5, 31, 384), (31, 64, 128), (33, 65, 256), (64, 129, 128), (65, 255, 256), (127, 257, 128),
+             (129, 300, 640), (255, 511, 128), (257, 1000, 384), (300, 4099, 640), (513, 1537, 256), (700, 333, 1152), (1030, 2050, 512)]
+
+
+@pytest.mark.parametrize("T,N,K", CE_SHAPES)
+def test_cross_entropy(T, N, K):
+    check(make(T, N, K, seed=T + N + K))
+
+
+@pytest.mark.parametrize("T,N,K", [(1, 130, 128), (77, 500, 256), (300, 700, 256)])
+def test_cross_entropy_no_row_left_out(T, N, K):
+    check(make(T, N, K, seed=7 + T, ignored=0.0))
+
+
+# the vocabulary in several pieces, the last one short; dx from several slices of each piece, from one, and from half tiles
+@pytest.mark.parametrize("T,N,K", [(3, 12007, 4096), (200, 11009, 4096), (400, 24001, 2048), (5000, 30011, 256)])
+def test_cross_entropy_in_pieces(T, N, K):
+    c = make(T, N, K, seed=T + K)
+    assert b.sbn_head_workspace_bytes(T, N, K, backward=True) < 2 * T * N + 10 * T * K * 4 + (160 << 20)
+    check(c)
+
+
+def test_cross_entropy_wide_token_groups():
+    # more than 16 row tiles: the second group of row tiles goes over the vocabulary again
+    check(make(4500, 1100, 128, seed=3))
+
+
+@pytest.mark.parametrize("T", [1, 64, 300])
+def test_every_row_left_out(T):
+    c = make(T, 200, 256, seed=5)
+    c["labels"].fill_(-1)
+    c["x"].fill_(NAN)
+    f = forward(c)
+    dx, dhead = backward(c, f["lse"])
+    b.sbn_check_status()
+    assert not f["ce"].any() and not f["lse"].any() and not dx.any() and not dhead.any()
+
+
+@pytest.mark.parametrize("hold", [NAN, INF, -INF, 3.3895e38])
+def test_rows_left_out_reach_nothing(hold):
+    c = make(200, 400, 256, seed=11)
+    out = c["labels"] < 0
+    assert 0 < int(out.sum()) < 200
+    o, bd = reference(c)
+    clean = check(c, o, bd)
+    c["x"][out] = hold
+    c["d_ce"][out] = NAN
+    dirty = check(c, o, bd)
+    for p, q in zip(clean[1:], dirty[1:]):
+        assert torch.equal(p, q)
+    assert torch.equal(clean[0]["ce"], dirty[0]["ce"])
+
+
+@pytest.mark.parametrize("where", ["first", "last", "one", "alternate"])
+def test_which_rows_count(where):
+    T = 330
+    c = make(T, 500, 128, seed=13, ignored=0.0)
+    drop = torch.zeros(T, dtype=torch.bool, device="cuda")
+    if where == "first":
+        drop[:200] = True
+    elif where == "last":
+        drop[100:] = True
+    elif where == "one":
+        drop[:] = True
+        drop[257] = False
+    else:
+        drop[::2] = True
+    c["labels"][drop] = -(2 ** 40)
+    check(c)
+
+
+def test_labels_outside_the_vocabulary_are_reported():
+    c = make(100, 300, 128, seed=17, ignored=0.1)
+    o, bd = reference(c)
+    bad = torch.tensor([3, 64, 99], device="cuda")
+    c["labels"][bad] = torch.tensor([300, 2 ** 31, 2 ** 40], device="cuda")
+    f = forward(c)
+    with pytest.raises(b.SbnError) as err:
+        b.sbn_check_status()
+    assert err.value.code == 9
+    b.sbn_check_status()                                            # reported once
+    assert torch.isnan(f["ce"][bad]).all() and not f["lse"][bad].any()
+    rest = torch.ones(100, dtype=torch.bool, device="cuda")
+    rest[bad] = False
+    assert_near("ce", f["ce"][rest], o["ce"][rest], bd["ce"][rest])
+    dx, dhead = backward(c, f["lse"])
+    with pytest.raises(b.SbnError):
+        b.sbn_check_status()
+    ref = dict(c, labels=torch.where(rest, c["labels"], torch.full_like(c["labels"], -1)))
+    o, bd = reference(ref)
+    assert_near("dx", dx, o["dx"], bd["dx"])
+    assert_near("dhead", dhead, o["dhead"], bd["dhead"])
+
+
+def test_extreme_logits():
+    # logits of several hundred: the maximum has to come off before exp
+    c = make(70, 300, 128, seed=19, scale=4.0, lean=0.0)
+    o, bd = reference(c)
+    assert float(o["Z"].abs().max()) > 100
+    check(c, o, bd)
+
+
+def test_sure_rows():
+    # one word far ahead of all others: loss next to zero, gradient next to zero
+    c = make(40, 500, 256, seed=23, ignored=0.0, lean=30.0)
+    check(c)
+
+
+DISTILL = [  # T, N, K, top, teacher type, tau, with labels
+    (1, 1, 128, 1, F32, 1.0, False), (1, 7, 128, 9, F32, 1.0, True), (2, 1000, 128, 3, BF16, 2.0, False), (33, 65, 256, 1, F32, 0.5, True),
+    (64, 300, 128, 256, F32, 1.0, True), (100, 4099, 256, 255, BF16, 4.0, True), (129, 513, 384, 17, BF16, 1.5, False), (257, 2000, 256, 32, F32, 2.0, True),
+    (300, 1111, 640, 64, F32, 2.0, False), (1030, 700, 128, 5, F32, 1.0, True)]
+
+
+@pytest.mark.parametrize("T,N,K,top,dtype,tau,labels", DISTILL)
+def test_distill(T, N, K, top, dtype, tau, labels):
+    c = make(T, N, K, seed=T + N + K + top, top=top, dtype=dtype, labels=labels)
+    c["tau"] = tau
+    check(c)
+
+
+def test_distill_in_pieces():
+    c = make(260, 24001, 2048, seed=29, top=40)
+    c["tau"] = 2.0
+    check(c)
+
+
+def test_distill_masked_entries():
+    # -inf and the type's lowest value as teacher logits; rows with nothing but those; a single entry; one index in every place
+    T, N, K, top = 40, 300, 128, 12
+    for dtype in (F32, BF16):
+        for tau in (0.25, 1.0):
+            c = make(T, N, K, seed=31, top=top, dtype=dtype, ignored=0.0, absent=0.0)
+            c["tau"] = tau
+            low = torch.finfo(dtype).min
+            c["top_logits"][0:4, 3:] = -INF
+            c["top_logits"][4:8, 3:] = low
+            c["top_logits"][8, :] = -INF                            # left out (its label stays)
+            c["top_logits"][9, :] = low                             # uniform
+            c["top_index"][10, 1:] = -1
+            c["top_index"][11, :] = -5                              # left out
+            c["top_index"][12, :] = 299
+            c["top_logits"][13, :6] = low
+            c["top_index"][14, ::2] = -1
+            c["top_logits"][14, ::2] = NAN                          # not there: not looked at
+            c["labels"][[8, 11, 20]] = -1                           # 8 and 11: nothing asked of the row
+            c["x"][8] = NAN
+            f, dx, dhead = check(c)
+            assert float(f["distill"][8]) == 0.0 and float(f["distill"][11]) == 0.0 and float(f["ce"][20]) == 0.0
+            assert not dx[8].any() and not dx[11].any()
+
+
+def test_distill_index_outside_the_vocabulary():
+    c = make(50, 300, 128, seed=37, top=6, ignored=0.0, absent=0.0)
+    ref = dict(c, top_index=c["top_index"].clone())
+    c["top_index"][7, 2] = 300
+    c["top_index"][8, 0] = 2 ** 40
+    c["labels"][9] = 300
+    ref["top_index"][[7, 8]] = -1
+    ref["labels"] = c["labels"].clone()
+    ref["labels"][9] = -1
+    f = forward(c)
+    with pytest.raises(b.SbnError) as err:
+        b.sbn_check_status()
+    assert err.value.code == 9
+    assert torch.isnan(f["distill"][[7, 8]]).all() and torch.isnan(f["ce"][9]) and torch.isfinite(f["ce"][[7, 8]]).all()
+    o, bd = reference(ref)
+    dx, dhead = backward(c, f["lse"])
+    with pytest.raises(b.SbnError):
+        b.sbn_check_status()
+    assert_near("dx", dx, o["dx"], bd["dx"])
+    assert_near("dhead", dhead, o["dhead"], bd["dhead"])
+
+
+def test_distill_with_one_entry_is_cross_entropy():
+    # top = 1, tau = 1: q = 1 at the label, so both losses are the same numbers
+    c = make(130, 900, 256, seed=41, ignored=0.2)
+    d = dict(c, top_index=c["labels"][:, None].contiguous(), top_logits=torch.zeros(130, 1, device="cuda"), d_distill=c["d_ce"])
+    del d["labels"], d["d_ce"]
+    f, dx, dhead = check(c)
+    g, ex, ehead = check(d)
+    assert torch.equal(f["ce"], g["distill"]) and torch.equal(dx, ex) and torch.equal(dhead, ehead)
+
+
+@pytest.mark.parametrize("top", [0, 5])
+def test_either_gradient_alone(top):
+    c = make(140, 700, 256, seed=43, top=top)
+    f = forward(c)
+    dx, dhead = backward(c, f["lse"])
+    only_dx, none = backward(c, f["lse"], dhead=False)
+    assert none is None and torch.equal(dx, only_dx)
+    none, only_dhead = backward(c, f["lse"], dx=False)
+    assert none is None and torch.equal(dhead, only_dhead)
+
+
+def test_gradient_is_the_slope_of_the_loss():
+    # central differences of the library's own losses along a direction: bf16 steps that are exact
+    c = make(64, 300, 128, seed=47, ignored=0.2)
+    c["x"] = torch.round(c["x"].float() * 16).clamp(-64, 64).div(16).to(BF16)
+    f = forward(c)
+    dx, _ = backward(c, f["lse"], dhead=False)
+    step = torch.randint(-1, 2, c["x"].shape, generator=torch.Generator().manual_seed(1)).to("cuda").float() / 16
+    up, down = (dict(c, x=(c["x"].float() + s * step).to(BF16)) for s in (1, -1))
+    assert torch.equal(up["x"].float() - c["x"].float(), step)
+    fu, fd = forward(up), forward(down)
+    slope = (fu["ce"].double() - fd["ce"].double()) / 2 * c["d_ce"].double()
+    o, bd = reference(c)
+    u = step.double() @ c["head"].double().T                        # change of the logits
+    third = (u.max(1).values - u.min(1).values) ** 3                # |f'''| of log-sum-exp along a line, over 6 below
+    want = (dx.double() * step.double()).sum(1)
+    tol = (bd["dx"] * step.abs().double()).sum(1) + c["d_ce"].double() * (third / 6 + bd["ce"] * 2)
+    has = c["labels"] >= 0
+    assert bool(((slope - want).abs() <= tol)[has].all()), ((slope - want).abs() / tol)[has].max()
+    assert float(slope[has].abs().max()) > 5 * float(tol[has].median())
+
+
+def test_same_bits_from_call_to_call_and_on_another_stream():
+    c = make(500, 3001, 512, seed=53, top=9)
+    f = forward(c)
+    dx, dhead = backward(c, f["lse"])
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        g = forward(c)
+        ex, ehead = backward(c, g["lse"])
+    torch.cuda.current_stream().wait_stream(s)
+    for k in f:
+        assert torch.equal(f[k], g[k]), k
+    assert torch.equal(dx, ex) and torch.equal(dhead, ehead)
+
+
+def test_calls_back_to_back_on_one_workspace():
+    # no synchronisation in between: each call overwrites the workspace the one before it used
+    cs = [make(T, N, K, seed=59 + T, top=top) for T, N, K, top in ((300, 2000, 256, 0), (70, 900, 512, 4), (300, 2000, 256, 7), (1, 500, 128, 0))]
+    n = max(b.sbn_head_workspace_bytes(c["T"], c["N"], c["K"], c["top_index"].shape[1] if "top_index" in c else 0, w) for c in cs for w in (False, True))
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    got = []
+    for c in cs:
+        f = forward(c, ws=ws, dirty=False)
+        got.append((f, *backward(c, f["lse"], ws=ws, dirty=False)))
+    for c, (f, dx, dhead) in zip(cs, got):
+        o, bd = reference(c)
+        for name in ("ce", "distill"):
+            if name in f and name in o:
+                assert_near(name, f[name], o[name], bd[name])
+        assert_near("dx", dx, o["dx"], bd["dx"])
+        assert_near("dhead", dhead, o["dhead"], bd["dhead"])
+
+
+@pytest.mark.parametrize("top", [0, 6])
+def test_captured_into_a_graph(top):
+    # a whole step in a graph, replayed on other inputs (other rows left out) in the same buffers
+    c = make(200, 1500, 256, seed=61, top=top)
+    ws = [b.alloc_head_ws(200, 1500, 256, top=top, backward=w) for w in (False, True)]
+    f = forward(c, ws=ws[0])
+    backward(c, f["lse"], ws=ws[1])
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        f = forward(c, ws=ws[0])
+        dx, dhead = backward(c, f["lse"], ws=ws[1])
+    for seed in (67, 71):
+        new = make(200, 1500, 256, seed=seed, top=top, ignored=0.6 if seed == 67 else 0.0)
+        for k, v in new.items():
+            if torch.is_tensor(v):
+                c[k].copy_(v)
+        g.replay()
+        o, bd = reference(c)
+        for name in ("ce", "distill"):
+            if name in f and name in o:
+                assert_near(name, f[name], o[name], bd[name])
+        assert_near("dx", dx, o["dx"], bd["dx"])
+        assert_near("dhead", dhead, o["dhead"], bd["dhead"])
+
+
+@pytest.mark.parametrize("T,N,K", [(3, 33, 128), (130, 700, 256), (300, 1000, 384)])
+def test_nothing_is_written_outside_the_outputs(T, N, K):
+    c = make(T, N, K, seed=73)
+    pad = 4096
+
+    def guarded(shape, dtype):
+        n = shape[0] * (shape[1] if len(shape) > 1 else 1)
+        buf = torch.full((n + 2 * pad,), 7.0, dtype=dtype, device="cuda")
+        return buf, buf[pad:pad + n].view(shape)
+
+    bufs = {k: guarded(s, d) for k, s, d in (("loss", (T,), F32), ("lse", (T,), F32), ("dx", (T, K), BF16), ("dhead", (N, K), BF16))}
+    wss = []
+    for back in (False, True):
+        n = b.sbn_head_workspace_bytes(T, N, K, backward=back)
+        wss.append((n, torch.full((n + 2 * pad,), 0x5A, dtype=torch.uint8, device="cuda")))
+    b.sbn_head_cross_entropy(c["x"], c["head"], c["labels"], bufs["loss"][1], bufs["lse"][1], ws=wss[0][1][pad:pad + wss[0][0]])
+    b.sbn_head_cross_entropy_backward(c["x"], c["head"], c["labels"], bufs["lse"][1], c["d_ce"], dx=bufs["dx"][1], dhead=bufs["dhead"][1],
+                                      ws=wss[1][1][pad:pad + wss[1][0]])
+    b.sbn_check_status()
+    for k, (buf, view) in bufs.items():
+        assert bool((buf[:pad] == 7).all()) and bool((buf[pad + view.numel():] == 7).all()), k
+        assert bool(torch.isfinite(view).all())
+    for n, ws in wss:
+        assert bool((ws[:pad] == 0x5A).all()) and bool((ws[pad + n:] == 0x5A).all())
+
+
+def test_waits_are_bounded():
+    c = make(300, 700, 256, seed=79)
+    f = forward(c)
+    try:
+        b.sbn_set_wait_test(True, 1000)
+        forward(c)
+        with pytest.raises(b.SbnError) as err:
+            b.sbn_check_status()
+        assert err.value.code == 7
+        backward(c, f["lse"])
+        with pytest.raises(b.SbnError) as err:
+            b.sbn_check_status()
+        assert err.value.code == 7
+    finally:
+        b.sbn_set_wait_test(False, 0)
+    check(c)
+
+
+def test_a_training_step_together():
+    """Quantiser, sparse layer, head, loss, the head's gradients, the layer's gradients: one chain on one stream, its losses and
+    gradients against the same chain in float64 from the layer's own output on."""
+    T, K, H, V = 192, 256, 384, 1237
+    g = torch.Generator(device="cuda").manual_seed(83)
+    W = torch.randn(H, K, generator=g, device="cuda") * 0.05
+    x = torch.randn(T, K, generator=g, device="cuda").to(BF16)
+    head = (torch.randn(V, H, generator=g, device="cuda") * 0.05).to(BF16)
+    labels = torch.randint(-300, V, (T,), generator=g, device="cuda")
+    p = b.alloc_packed(H, K)
+    xq, sc = b.alloc_xq(T, K), torch.empty(T, device="cuda")
+    y = torch.empty(T, H, dtype=BF16, device="cuda")
+    loss, lse = torch.empty(T, device="cuda"), torch.empty(T, device="cuda")
+    dy, dhead = torch.empty_like(y), torch.empty_like(head)
+    dX, dW = torch.empty_like(x), torch.empty_like(W)
+    d = torch.full((T,), 1.0, device="cuda") / (labels >= 0).sum()
+    b.sbn_quantize_mask_pack(W, p["vals"], p["meta"], p["w_scale"], p["ws"])
+    b.sbn_quant_act(x, xq, sc)
+    b.sbn_sparse_bitlinear(xq, sc, p["vals"], p["meta"], p["w_scale"], y, ws=b.alloc_gemm_ws(b.OP_SPARSE_BITLINEAR, T, H, K))
+    b.sbn_head_cross_entropy(y, head, labels, loss, lse, ws=b.alloc_head_ws(T, V, H))
+    b.sbn_head_cross_entropy_backward(y, head, labels, lse, d, dx=dy, dhead=dhead, ws=b.alloc_head_ws(T, V, H, backward=True))
+    ws = torch.empty(b.sbn_workspace_bytes(b.OP_BACKWARD, T, H, K), dtype=torch.uint8, device="cuda")
+    b.sbn_bitlinear_backward(dy, xq, sc, p["vals"], p["meta"], p["w_scale"], H, K, dX=dX, dW=dW, ws=ws)
+    b.sbn_check_status()
+    o = oh.head_loss(y, head, labels, d_ce=d)
+    bd = oh.bounds(o, d_ce=d)
+    assert_near("loss", loss, o["ce"], bd["ce"])
+    assert_near("dy", dy, o["dx"], bd["dx"])
+    assert_near("dhead", dhead, o["dhead"], bd["dhead"])
+    # dW = dy^T x_q: the fake-quantised activations are the input within half a quantisation step
+    want = dy.double().T @ x.double()
+    step = sc.double()
+    assert bool(((dW.double() - want).abs() <= dy.double().abs().T @ ((0.51 * step + 2.0 ** -8 * 127 * step)[:, None].expand(T, K)) + 1e-30).all())
+    assert float(want.abs().max()) > 0 and bool(torch.isfinite(dX).all())
+
+
+@pytest.mark.parametrize("change", ["x_dtype", "x_strided", "labels_int32", "labels_short", "loss_dtype", "head_cols", "cpu_head", "ws_cpu"])
+def test_binding_refuses_wrong_tensors(change):
+    c = make(20, 100, 128, seed=89)
+    loss, lse, ws = torch.empty(20, device="cuda"), torch.empty(20, device="cuda"), b.alloc_head_ws(20, 100, 128)
+    x, head, labels = c["x"], c["head"], c["labels"]
+    if change == "x_dtype":
+        x = x.float()
+    elif change == "x_strided":
+        x = torch.cat([x, x], 1)[:, :128]
+    elif change == "labels_int32":
+        labels = labels.int()
+    elif change == "labels_short":
+        labels = labels[:-1]
+    elif change == "loss_dtype":
+        loss = loss.double()
+    elif change == "head_cols":
+        head = head[:, :64].contiguous()
+    elif change == "cpu_head":
+        head = head.cpu()
+    else:
+        ws = ws.cpu()
+    n = b.sbn_launch_count()
+    with pytest.raises(ValueError):
+        b.sbn_head_cross_entropy(x, head, labels, loss, lse, ws=ws)
+    assert b.sbn_launch_count() == n
