@@ -141,7 +141,8 @@ def _stream():
 
 
 _NATIVE_CALLS = ["sbn_quant_act", "sbn_quant_act_expand68", "sbn_norm_quant_act", "sbn_norm_quant_act_expand68", "sbn_sparse_bitlinear",
-                 "sbn_bitlinear", "sbn_sparse_bitlinear_packed", "sbn_quant_act_sparse_bitlinear", "sbn_quant_act_bitlinear"]
+                 "sbn_bitlinear", "sbn_sparse_bitlinear_packed", "sbn_quant_act_sparse_bitlinear", "sbn_quant_act_bitlinear",
+                 "sbn_head_cross_entropy", "sbn_head_cross_entropy_backward", "sbn_head_distill", "sbn_head_distill_backward"]
 
 
 def _load_native():
@@ -155,7 +156,7 @@ def _load_native():
     mod = importlib.util.module_from_spec(importlib.util.spec_from_loader("_sbn_native", loader))
     loader.exec_module(mod)
     addresses = {name: ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in _NATIVE_CALLS}
-    mod.bind(addresses, torch.bfloat16, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
+    mod.bind(addresses, torch.bfloat16, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, torch.float32, torch.int64)
     _native = mod
     return mod
 
@@ -327,78 +328,33 @@ def sbn_head_workspace_bytes(T: int, N: int, K: int, top: int = 0, backward: boo
     return int(lib().sbn_head_workspace_bytes(1 if backward else 0, T, N, K, top))
 
 
-def _head_tensor(name, t, dtype, shape, device):
-    """The C ABI takes pointers: what a tensor is has to be right here.  Raises ValueError."""
-    if t is None:
-        return None
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{name}: expected a contiguous {dtype} tensor {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} "
-                         f"on {t.device}{'' if t.is_contiguous() else ', not contiguous'}")
-    return t.data_ptr()
-
-
-def _head_inputs(x, head, labels):
-    if x.dim() != 2 or head.dim() != 2:
-        raise ValueError("x and head are two-dimensional")
-    (T, K), N, dev = x.shape, head.shape[0], x.device
-    if dev.type != "cuda" or dev.index != torch._C._cuda_getDevice():
-        raise ValueError(f"x is on {dev}, which is not the current CUDA device")
-    return (T, N, K, dev, _head_tensor("x", x, torch.bfloat16, (T, K), dev), _head_tensor("head", head, torch.bfloat16, (N, K), dev),
-            _head_tensor("labels", labels, torch.int64, (T,), dev))
-
-
-def _head_teacher(T, dev, top_index, top_logits):
-    if top_index.dim() != 2 or top_logits.dtype not in (torch.float32, torch.bfloat16):
-        raise ValueError("top_index is two-dimensional, top_logits are float32 or bfloat16")
-    top = top_index.shape[1]
-    return (_head_tensor("top_index", top_index, torch.int64, (T, top), dev), _head_tensor("top_logits", top_logits, top_logits.dtype, (T, top), dev),
-            OUT_BF16 if top_logits.dtype == torch.bfloat16 else OUT_F32, top)
-
-
-def _head_ws(ws, dev):
-    if ws is None:
-        return None, 0
-    if ws.device != dev or not ws.is_contiguous():
-        raise ValueError(f"ws: expected a contiguous tensor on {dev}")
-    return ws.data_ptr(), ws.numel() * ws.element_size()
+def _head(x):
+    """The extension, for the calls at the output head.  It checks type, shape, device (the current one) and contiguity of every tensor
+    (ValueError): the C ABI sees only addresses."""
+    if not x.is_cuda:
+        raise ValueError(f"x: expected a CUDA tensor, got one on {x.device}")
+    return _native or _load_native()
 
 
 def sbn_head_cross_entropy(x, head, labels, loss, lse, ws=None):
     """x bf16 [T][K], head bf16 [N][K], labels int64 [T] (negative: left out); writes loss and lse, fp32 [T]."""
-    T, N, K, dev, px, ph, pl = _head_inputs(x, head, labels)
-    _check(lib().sbn_head_cross_entropy(px, T, K, ph, N, pl, _head_tensor("loss", loss, torch.float32, (T,), dev),
-                                        _head_tensor("lse", lse, torch.float32, (T,), dev), *_head_ws(ws, dev), _stream()),
-           "sbn_head_cross_entropy")
+    _check(_head(x).head_cross_entropy(x, head, labels, loss, lse, ws), "sbn_head_cross_entropy")
 
 
 def sbn_head_cross_entropy_backward(x, head, labels, lse, dloss, dx=None, dhead=None, ws=None):
     """lse from the forward call, dloss fp32 [T]; writes dx (bf16, as x) and / or dhead (bf16, as head)."""
-    T, N, K, dev, px, ph, pl = _head_inputs(x, head, labels)
-    _check(lib().sbn_head_cross_entropy_backward(px, T, K, ph, N, pl, _head_tensor("lse", lse, torch.float32, (T,), dev),
-                                                 _head_tensor("dloss", dloss, torch.float32, (T,), dev),
-                                                 _head_tensor("dx", dx, torch.bfloat16, (T, K), dev),
-                                                 _head_tensor("dhead", dhead, torch.bfloat16, (N, K), dev), *_head_ws(ws, dev), _stream()),
-           "sbn_head_cross_entropy_backward")
+    _check(_head(x).head_cross_entropy_backward(x, head, labels, lse, dloss, dx, dhead, ws), "sbn_head_cross_entropy_backward")
 
 
 def sbn_head_distill(x, head, top_index, top_logits, temperature, loss, lse, labels=None, ce_loss=None, ws=None):
     """top_index int64, top_logits fp32 or bf16 [T][top] (negative index: not there); writes loss fp32 [T] and lse fp32 [1][T], or
     with labels and ce_loss [2][T]."""
-    T, N, K, dev, px, ph, pl = _head_inputs(x, head, labels)
-    _check(lib().sbn_head_distill(px, T, K, ph, N, *_head_teacher(T, dev, top_index, top_logits), float(temperature), pl,
-                                  _head_tensor("loss", loss, torch.float32, (T,), dev), _head_tensor("ce_loss", ce_loss, torch.float32, (T,), dev),
-                                  _head_tensor("lse", lse, torch.float32, (1 if labels is None else 2, T), dev), *_head_ws(ws, dev), _stream()),
-           "sbn_head_distill")
+    _check(_head(x).head_distill(x, head, top_index, top_logits, temperature, loss, lse, labels, ce_loss, ws), "sbn_head_distill")
 
 
 def sbn_head_distill_backward(x, head, top_index, top_logits, temperature, lse, d_loss, labels=None, d_ce=None, dx=None, dhead=None, ws=None):
     """lse from the forward call; d_loss and (with labels) d_ce fp32 [T]; writes dx and / or dhead."""
-    T, N, K, dev, px, ph, pl = _head_inputs(x, head, labels)
-    _check(lib().sbn_head_distill_backward(px, T, K, ph, N, *_head_teacher(T, dev, top_index, top_logits), float(temperature), pl,
-                                           _head_tensor("lse", lse, torch.float32, (1 if labels is None else 2, T), dev),
-                                           _head_tensor("d_loss", d_loss, torch.float32, (T,), dev), _head_tensor("d_ce", d_ce, torch.float32, (T,), dev),
-                                           _head_tensor("dx", dx, torch.bfloat16, (T, K), dev),
-                                           _head_tensor("dhead", dhead, torch.bfloat16, (N, K), dev), *_head_ws(ws, dev), _stream()),
+    _check(_head(x).head_distill_backward(x, head, top_index, top_logits, temperature, lse, d_loss, labels, d_ce, dx, dhead, ws),
            "sbn_head_distill_backward")
 
 

@@ -21,8 +21,13 @@ decltype(&sbn_bitlinear) f_bitlinear;
 decltype(&sbn_sparse_bitlinear_packed) f_sparse_bitlinear_packed;
 decltype(&sbn_quant_act_sparse_bitlinear) f_quant_act_sparse_bitlinear;
 decltype(&sbn_quant_act_bitlinear) f_quant_act_bitlinear;
+decltype(&sbn_head_cross_entropy) f_head_cross_entropy;
+decltype(&sbn_head_cross_entropy_backward) f_head_cross_entropy_backward;
+decltype(&sbn_head_distill) f_head_distill;
+decltype(&sbn_head_distill_backward) f_head_distill_backward;
 
-PyObject *s_data_ptr, *s_shape, *s_dtype, *s_numel, *s_element_size;      // interned names
+PyObject *s_data_ptr, *s_shape, *s_dtype, *s_numel, *s_element_size, *s_is_contiguous, *s_device_of;      // interned names
+PyObject *g_float32, *g_int64;                                             // torch's
 PyObject *g_bfloat16, *g_get_device, *g_get_raw_stream;                   // torch.bfloat16, torch's current device / stream
 
 // All conversions leave a Python error behind on failure and do nothing once there is one; run() looks before it calls
@@ -237,7 +242,118 @@ PyObject* py_quant_act_bitlinear(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return run([=] { return f_quant_act_bitlinear(x, T, q, w, N, K, bias, y, dt, acc, sc, s); });
 }
 
-// bind(addresses: dict name -> int, torch.bfloat16, get_device, get_raw_stream)
+// ---- the losses at the output head: what a tensor is gets checked, the C ABI sees only its address ----
+// Address of a contiguous tensor of this type and shape (cols < 0: one-dimensional) on device `dev`; None gives NULL.
+void* checked(PyObject* t, const char* name, PyObject* dtype, long long rows, long long cols, long long dev) {
+    if (t == Py_None || PyErr_Occurred()) return nullptr;
+    PyObject *d = PyObject_GetAttr(t, s_dtype), *shape = d ? PyObject_GetAttr(t, s_shape) : nullptr;
+    bool ok = shape && d == dtype && PyTuple_Check(shape) && PyTuple_GET_SIZE(shape) == (cols < 0 ? 1 : 2) &&
+              PyLong_AsLongLong(PyTuple_GET_ITEM(shape, 0)) == rows && (cols < 0 || PyLong_AsLongLong(PyTuple_GET_ITEM(shape, 1)) == cols);
+    Py_XDECREF(d);
+    Py_XDECREF(shape);
+    ok = ok && call_ll(t, s_device_of) == dev && call_ll(t, s_is_contiguous) == 1;
+    if (PyErr_Occurred()) return nullptr;
+    if (!ok) {
+        if (cols < 0) PyErr_Format(PyExc_ValueError, "%s: expected a contiguous %R tensor (%lld,) on cuda:%lld", name, dtype, rows, dev);
+        else PyErr_Format(PyExc_ValueError, "%s: expected a contiguous %R tensor (%lld, %lld) on cuda:%lld", name, dtype, rows, cols, dev);
+        return nullptr;
+    }
+    return ptr(t);
+}
+// What every call has: x [T][K], head [N][K], labels [T], a workspace, the current device and stream.
+struct HeadArgs {
+    int T, N, K;
+    long long dev;
+    const void *x, *head;
+    const int64_t* labels;
+    void* ws;
+    size_t ws_bytes;
+    void* stream;
+    HeadArgs(PyObject* x_, PyObject* head_, PyObject* labels_, PyObject* ws_) {
+        int head_k;
+        shape2(x_, T, K);
+        shape2(head_, N, head_k);
+        PyObject* d = PyErr_Occurred() ? nullptr : PyObject_CallNoArgs(g_get_device);
+        dev = d ? PyLong_AsLongLong(d) : -1;
+        Py_XDECREF(d);
+        x = checked(x_, "x", g_bfloat16, T, K, dev);
+        head = checked(head_, "head", g_bfloat16, N, K, dev);
+        labels = static_cast<const int64_t*>(checked(labels_, "labels", g_int64, T, -1, dev));
+        ws = nullptr;
+        ws_bytes = 0;
+        if (ws_ != Py_None && !PyErr_Occurred()) {
+            if (call_ll(ws_, s_device_of) != dev || call_ll(ws_, s_is_contiguous) != 1) {
+                if (!PyErr_Occurred()) PyErr_Format(PyExc_ValueError, "ws: expected a contiguous tensor on cuda:%lld", dev);
+            }
+            ws = ptr(ws_);
+            ws_bytes = PyErr_Occurred() ? 0 : bytes_of(ws_);
+        }
+        stream = current_stream();
+    }
+    float* per_token(PyObject* t, const char* name) const { return static_cast<float*>(checked(t, name, g_float32, T, -1, dev)); }
+    void* dx(PyObject* t) const { return checked(t, "dx", g_bfloat16, T, K, dev); }
+    void* dhead(PyObject* t) const { return checked(t, "dhead", g_bfloat16, N, K, dev); }
+};
+struct TeacherArgs {
+    int top;
+    const int64_t* index;
+    const void* logits;
+    sbn_out_dtype dt;
+    float tau;
+    TeacherArgs(const HeadArgs& h, PyObject* index_, PyObject* logits_, PyObject* tau_) {
+        int rows;
+        shape2(index_, rows, top);
+        index = static_cast<const int64_t*>(checked(index_, "top_index", g_int64, h.T, top, h.dev));
+        dt = out_dtype(logits_);
+        logits = checked(logits_, "top_logits", dt == SBN_OUT_BF16 ? g_bfloat16 : g_float32, h.T, top, h.dev);
+        tau = PyErr_Occurred() ? 0.0f : static_cast<float>(PyFloat_AsDouble(tau_));
+    }
+};
+
+// (x, head, labels, loss, lse, ws)
+PyObject* py_head_cross_entropy(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!expect(n, 6)) return nullptr;
+    const HeadArgs h(a[0], a[1], a[2], a[5]);
+    float *loss = h.per_token(a[3], "loss"), *lse = h.per_token(a[4], "lse");
+    return run([=] { return f_head_cross_entropy(h.x, h.T, h.K, h.head, h.N, h.labels, loss, lse, h.ws, h.ws_bytes, h.stream); });
+}
+
+// (x, head, labels, lse, dloss, dx, dhead, ws)
+PyObject* py_head_cross_entropy_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!expect(n, 8)) return nullptr;
+    const HeadArgs h(a[0], a[1], a[2], a[7]);
+    const float *lse = h.per_token(a[3], "lse"), *dloss = h.per_token(a[4], "dloss");
+    void *dx = h.dx(a[5]), *dhead = h.dhead(a[6]);
+    return run([=] { return f_head_cross_entropy_backward(h.x, h.T, h.K, h.head, h.N, h.labels, lse, dloss, dx, dhead, h.ws, h.ws_bytes, h.stream); });
+}
+
+// (x, head, top_index, top_logits, temperature, loss, lse, labels, ce_loss, ws)
+PyObject* py_head_distill(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!expect(n, 10)) return nullptr;
+    const HeadArgs h(a[0], a[1], a[7], a[9]);
+    const TeacherArgs q(h, a[2], a[3], a[4]);
+    float *loss = h.per_token(a[5], "loss"), *ce = h.per_token(a[8], "ce_loss");
+    float* lse = static_cast<float*>(checked(a[6], "lse", g_float32, a[7] == Py_None ? 1 : 2, h.T, h.dev));
+    return run([=] {
+        return f_head_distill(h.x, h.T, h.K, h.head, h.N, q.index, q.logits, q.dt, q.top, q.tau, h.labels, loss, ce, lse, h.ws, h.ws_bytes, h.stream);
+    });
+}
+
+// (x, head, top_index, top_logits, temperature, lse, d_loss, labels, d_ce, dx, dhead, ws)
+PyObject* py_head_distill_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!expect(n, 12)) return nullptr;
+    const HeadArgs h(a[0], a[1], a[7], a[11]);
+    const TeacherArgs q(h, a[2], a[3], a[4]);
+    const float *lse = static_cast<const float*>(checked(a[5], "lse", g_float32, a[7] == Py_None ? 1 : 2, h.T, h.dev));
+    const float *d_loss = h.per_token(a[6], "d_loss"), *d_ce = h.per_token(a[8], "d_ce");
+    void *dx = h.dx(a[9]), *dhead = h.dhead(a[10]);
+    return run([=] {
+        return f_head_distill_backward(h.x, h.T, h.K, h.head, h.N, q.index, q.logits, q.dt, q.top, q.tau, h.labels, lse, d_loss, d_ce, dx, dhead, h.ws,
+                                       h.ws_bytes, h.stream);
+    });
+}
+
+// bind(addresses: dict name -> int, torch.bfloat16, get_device, get_raw_stream, torch.float32, torch.int64)
 template <typename F>
 bool take(PyObject* addresses, const char* name, F& f) {
     PyObject* v = PyDict_GetItemString(addresses, name);                  // borrowed
@@ -253,8 +369,8 @@ void keep(PyObject*& slot, PyObject* v) {
     Py_XSETREF(slot, v);
 }
 PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    if (n != 4 || !PyDict_Check(a[0])) {
-        PyErr_SetString(PyExc_TypeError, "bind(addresses, bfloat16, get_device, get_raw_stream)");
+    if (n != 6 || !PyDict_Check(a[0])) {
+        PyErr_SetString(PyExc_TypeError, "bind(addresses, bfloat16, get_device, get_raw_stream, float32, int64)");
         return nullptr;
     }
     PyObject* d = a[0];
@@ -262,11 +378,15 @@ PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
         !take(d, "sbn_norm_quant_act_expand68", f_norm_quant_act_expand68) || !take(d, "sbn_sparse_bitlinear", f_sparse_bitlinear) ||
         !take(d, "sbn_bitlinear", f_bitlinear) || !take(d, "sbn_sparse_bitlinear_packed", f_sparse_bitlinear_packed) ||
         !take(d, "sbn_quant_act_sparse_bitlinear", f_quant_act_sparse_bitlinear) ||
-        !take(d, "sbn_quant_act_bitlinear", f_quant_act_bitlinear))
+        !take(d, "sbn_quant_act_bitlinear", f_quant_act_bitlinear) || !take(d, "sbn_head_cross_entropy", f_head_cross_entropy) ||
+        !take(d, "sbn_head_cross_entropy_backward", f_head_cross_entropy_backward) || !take(d, "sbn_head_distill", f_head_distill) ||
+        !take(d, "sbn_head_distill_backward", f_head_distill_backward))
         return nullptr;
     keep(g_bfloat16, a[1]);
     keep(g_get_device, a[2]);
     keep(g_get_raw_stream, a[3]);
+    keep(g_float32, a[4]);
+    keep(g_int64, a[5]);
     if (!take(d, "sbn_quant_act", f_quant_act)) return nullptr;           // last: its presence means bound
     Py_RETURN_NONE;
 }
@@ -275,6 +395,7 @@ PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyMethodDef methods[] = {
     SBN_METHOD(bind), SBN_METHOD(quant_act), SBN_METHOD(norm_quant_act), SBN_METHOD(sparse_bitlinear), SBN_METHOD(bitlinear),
     SBN_METHOD(sparse_bitlinear_packed), SBN_METHOD(quant_act_sparse_bitlinear), SBN_METHOD(quant_act_bitlinear),
+    SBN_METHOD(head_cross_entropy), SBN_METHOD(head_cross_entropy_backward), SBN_METHOD(head_distill), SBN_METHOD(head_distill_backward),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_sbn_native", "Tensor arguments to the C ABI of libsbn.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
@@ -286,6 +407,8 @@ PyMODINIT_FUNC PyInit__sbn_native(void) {
     s_dtype = PyUnicode_InternFromString("dtype");
     s_numel = PyUnicode_InternFromString("numel");
     s_element_size = PyUnicode_InternFromString("element_size");
-    if (!s_data_ptr || !s_shape || !s_dtype || !s_numel || !s_element_size) return nullptr;
+    s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
+    s_device_of = PyUnicode_InternFromString("get_device");
+    if (!s_is_contiguous || !s_device_of || !s_data_ptr || !s_shape || !s_dtype || !s_numel || !s_element_size) return nullptr;
     return PyModule_Create(&module_def);
 }

@@ -1,12 +1,14 @@
 // Host side of the losses at the output head: workspaces, pieces of the vocabulary, launches.  Included by libsbn.cu.
 #pragma once
 
-#include "head_gemm_tcgen05.cuh"
+#include "head_few_mma.cuh"
 
 namespace sbn {
 
 // How a call is cut up, from its sizes alone.
 struct HeadPlan {
+    bool few;                     // head_few_mma.cuh
+    int slabs, ranges, per;       // its gradient kernel: 256-column slabs x ranges of `per` blocks of 16 words
     int bn, parts;                // forward: columns per tile, partial sums per row
     int piece;                    // backward: columns of dz at a time (a multiple of 256)
     int bn_piece;                 // columns per tile of the pieces' logits
@@ -31,7 +33,18 @@ static int head_tile_columns(int T, int cols, int K) {
 }
 
 static HeadPlan head_plan(int T, int N, int K) {
-    HeadPlan h;
+    HeadPlan h{};
+    h.few = head_few_takes(T, K);
+    if (h.few) {
+        const int blocks = (N + 15) / 16;
+        h.parts = std::min(blocks, kNumSMs);
+        h.slabs = (K + 255) / 256;
+        h.per = (blocks + kNumSMs / h.slabs - 1) / (kNumSMs / h.slabs);
+        h.ranges = (blocks + h.per - 1) / h.per;
+        h.slots = h.ranges;
+        h.piece = static_cast<int>(head_up(N, 16));
+        return h;
+    }
     h.rows64 = head_up(T, 64);
     h.rows256 = head_up(T, 256);
     h.bn = head_tile_columns(T, N, K);
@@ -58,21 +71,23 @@ static HeadWs head_ws_layout(const HeadPlan& h, bool backward, int T, int K, int
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) & ~static_cast<size_t>(255); return here; };
     const size_t t = static_cast<size_t>(T), events = top ? static_cast<size_t>(top) + 1 : 1;
-    w.count = take(4);
-    w.row_src = take(4 * t);
-    w.row_of = take(4 * t);
+    if (!h.few) {
+        w.count = take(4);
+        w.row_src = take(4 * t);
+        w.row_of = take(4 * t);
+    }
     if (top) {
         w.flags = take(t);
         w.ev_col = take(4 * t * events);
         w.ev_w = take(4 * t * events);
     }
-    w.xc = take(2 * static_cast<size_t>(h.rows64) * K);
+    if (!h.few) w.xc = take(2 * static_cast<size_t>(h.rows64) * K);
     if (!backward) {
         w.z_ev = take(4 * t * events);
         w.part = take(8 * t * h.parts);
         if (top) w.part1 = take(4 * t * h.parts);
     } else {
-        w.dz = take(2 * static_cast<size_t>(h.rows256) * h.piece);
+        w.dz = take(2 * static_cast<size_t>(h.few ? T : h.rows256) * h.piece);
         w.acc = take(4 * static_cast<size_t>(h.slots) * t * K);
     }
     w.total = at;
@@ -115,27 +130,22 @@ static sbn_status launch_head_logits(const HeadMaps& maps, const HeadLogitsParam
     return dual ? launch_head_logits_as<MODE, true, true>(maps, p, stream) : launch_head_logits_as<MODE, true, false>(maps, p, stream);
 }
 
-// What both directions begin with: targets (distillation) and the rows that count.
-static sbn_status launch_head_rows(const HeadCall& c, const HeadWs& w, HeadRowsJob rows, HeadTargets* tg, cudaStream_t stream) {
-    tg->labels = c.labels;
-    tg->flags = nullptr;
-    tg->ev_col = nullptr;
-    tg->ev_w = nullptr;
-    tg->events = 1;
-    if (c.top) {
-        HeadTargetsJob t{c.top_index, c.top_logits, c.top_bf16, c.top, c.T, c.N, static_cast<float>(1.0 / static_cast<double>(c.tau)), c.labels,
-                         reinterpret_cast<unsigned char*>(c.ws + w.flags), reinterpret_cast<int*>(c.ws + w.ev_col),
-                         reinterpret_cast<float*>(c.ws + w.ev_w)};
-        const int blocks = std::min((c.T + kTargetWarps - 1) / kTargetWarps, 16 * device_sm_count());
-        if (launch_kernel(head_targets_kernel, dim3(blocks), dim3(32 * kTargetWarps), 0, stream, t) != cudaSuccess) return SBN_ERR_CUDA;
-        ++g_launch_count;
-        tg->flags = t.flags;
-        tg->ev_col = t.ev_col;
-        tg->ev_w = t.ev_w;
-        tg->events = c.top + (c.labels ? 1 : 0);
-    }
-    rows.labels = c.labels;
-    rows.flags = tg->flags;
+// What is asked of the tokens: the labels themselves, or for a distillation the sorted targets of every token.
+static sbn_status launch_head_targets(const HeadCall& c, const HeadWs& w, HeadTargets* tg, cudaStream_t stream) {
+    *tg = HeadTargets{c.labels, nullptr, nullptr, nullptr, 1};
+    if (!c.top) return SBN_OK;
+    HeadTargetsJob t{c.top_index, c.top_logits, c.top_bf16, c.top, c.T, c.N, static_cast<float>(1.0 / static_cast<double>(c.tau)), c.labels,
+                     reinterpret_cast<unsigned char*>(c.ws + w.flags), reinterpret_cast<int*>(c.ws + w.ev_col),
+                     reinterpret_cast<float*>(c.ws + w.ev_w)};
+    const int blocks = std::min((c.T + kTargetWarps - 1) / kTargetWarps, 16 * device_sm_count());
+    if (launch_kernel(head_targets_kernel, dim3(blocks), dim3(32 * kTargetWarps), 0, stream, t) != cudaSuccess) return SBN_ERR_CUDA;
+    ++g_launch_count;
+    *tg = HeadTargets{c.labels, t.flags, t.ev_col, t.ev_w, c.top + (c.labels ? 1 : 0)};
+    return SBN_OK;
+}
+
+// The rows that count.
+static sbn_status launch_head_rows(const HeadCall& c, const HeadWs& w, HeadRowsJob rows, cudaStream_t stream) {
     rows.x = static_cast<const uint16_t*>(c.x);
     rows.T = c.T;
     rows.K = c.K;
@@ -149,15 +159,101 @@ static sbn_status launch_head_rows(const HeadCall& c, const HeadWs& w, HeadRowsJ
     return SBN_OK;
 }
 
+static sbn_status launch_head_losses(const HeadLossJob& j, cudaStream_t stream) {
+    const int blocks = std::min((j.T + kLossWarps - 1) / kLossWarps, 8 * device_sm_count());
+    if (launch_kernel(head_losses_kernel, dim3(blocks), dim3(32 * kLossWarps), 0, stream, j) != cudaSuccess) return SBN_ERR_CUDA;
+    ++g_launch_count;
+    return SBN_OK;
+}
+static sbn_status launch_head_dx(const HeadDxJob& j, cudaStream_t stream) {
+    const long long steps = (static_cast<long long>(j.T) * (j.K / 8) + kDxThreads - 1) / kDxThreads;
+    const int blocks = static_cast<int>(std::min<long long>(steps, 16ll * device_sm_count()));
+    if (launch_kernel(head_dx_kernel, dim3(blocks), dim3(kDxThreads), 0, stream, j) != cudaSuccess) return SBN_ERR_CUDA;
+    ++g_launch_count;
+    return SBN_OK;
+}
+
+// ---- few tokens ------------------------------------------------------------------------------------
+template <int KBW, int NT, int MODE>
+static sbn_status launch_head_few_as(const HeadFewParams& p, int ctas, bool list, bool dual, cudaStream_t stream) {
+    auto* kernel = !list ? head_few_kernel<KBW, NT, MODE, false, false> : (dual ? head_few_kernel<KBW, NT, MODE, true, true> : head_few_kernel<KBW, NT, MODE, true, false>);
+    if (launch_kernel(kernel, dim3(ctas), dim3(kFewHeadThreads), 0, stream, p) != cudaSuccess) return SBN_ERR_CUDA;
+    ++g_launch_count;
+    return SBN_OK;
+}
+template <int MODE>
+static sbn_status launch_head_few(const HeadFewParams& p, int ctas, bool list, bool dual, cudaStream_t stream) {
+    if (p.T <= 8) {
+        if (p.K <= 1024) return launch_head_few_as<2, 1, MODE>(p, ctas, list, dual, stream);
+        if (p.K <= 2560) return launch_head_few_as<5, 1, MODE>(p, ctas, list, dual, stream);
+        return launch_head_few_as<8, 1, MODE>(p, ctas, list, dual, stream);
+    }
+    if (p.K <= 1024) return launch_head_few_as<2, 2, MODE>(p, ctas, list, dual, stream);
+    return launch_head_few_as<5, 2, MODE>(p, ctas, list, dual, stream);
+}
+static HeadFewParams head_few_params(const HeadCall& c, const HeadTargets& tg) {
+    HeadFewParams p{};
+    p.tg = tg;
+    p.x = static_cast<const uint16_t*>(c.x);
+    p.w = static_cast<const uint16_t*>(c.head);
+    p.T = c.T; p.N = c.N; p.K = c.K;
+    p.c0 = static_cast<float>(1.4426950408889634 / static_cast<double>(c.tau));
+    p.inv_tau = static_cast<float>(1.0 / static_cast<double>(c.tau));
+    return p;
+}
+
+static sbn_status head_few_forward(const HeadCall& c, const HeadPlan& h, float* loss0, float* loss1, float* lse0, float* lse1, cudaStream_t stream) {
+    const HeadWs w = head_ws_layout(h, false, c.T, c.K, c.top);
+    HeadTargets tg;
+    sbn_status st = launch_head_targets(c, w, &tg, stream);
+    if (st != SBN_OK) return st;
+    const bool list = c.top != 0, dual = list && c.labels;
+    HeadFewParams p = head_few_params(c, tg);
+    p.part = reinterpret_cast<float2*>(c.ws + w.part);
+    p.part1 = dual ? reinterpret_cast<float*>(c.ws + w.part1) : nullptr;
+    p.z_ev = reinterpret_cast<float*>(c.ws + w.z_ev);
+    st = launch_head_few<0>(p, h.parts, list, dual, stream);
+    if (st != SBN_OK) return st;
+    return launch_head_losses(HeadLossJob{tg, nullptr, nullptr, c.T, c.N, p.part, p.part1, p.z_ev, h.parts, 1.0 / static_cast<double>(c.tau), loss0, loss1, lse0, lse1},
+                              stream);
+}
+
+static sbn_status head_few_backward(const HeadCall& c, const HeadPlan& h, const float* lse0, const float* lse1, const float* g0, const float* g1, void* dx,
+                                    void* dhead, cudaStream_t stream) {
+    const HeadWs w = head_ws_layout(h, true, c.T, c.K, c.top);
+    HeadTargets tg;
+    sbn_status st = launch_head_targets(c, w, &tg, stream);
+    if (st != SBN_OK) return st;
+    const bool list = c.top != 0, dual = list && c.labels;
+    HeadFewParams p = head_few_params(c, tg);
+    p.lse0 = lse0; p.lse1 = lse1; p.g0 = g0; p.g1 = g1;
+    p.dz = reinterpret_cast<uint16_t*>(c.ws + w.dz);
+    p.ldz = h.piece;
+    st = launch_head_few<1>(p, h.parts, list, dual, stream);
+    if (st != SBN_OK) return st;
+    p.dw = static_cast<uint16_t*>(dhead);
+    p.acc = dx ? reinterpret_cast<float*>(c.ws + w.acc) : nullptr;
+    p.slabs = h.slabs;
+    p.per = h.per;
+    auto* kernel = c.T <= 8 ? head_few_grads_kernel<1> : head_few_grads_kernel<2>;
+    if (launch_kernel(kernel, dim3(h.slabs * h.ranges), dim3(kFewHeadThreads), 0, stream, p) != cudaSuccess) return SBN_ERR_CUDA;
+    ++g_launch_count;
+    return dx ? launch_head_dx(HeadDxJob{nullptr, p.acc, h.slots, c.T, c.K, static_cast<uint16_t*>(dx)}, stream) : SBN_OK;
+}
+
+// ---- any number of tokens --------------------------------------------------------------------------
 static sbn_status head_forward(const HeadCall& c, float* loss0, float* loss1, float* lse0, float* lse1, cudaStream_t stream) {
     const HeadPlan h = head_plan(c.T, c.N, c.K);
+    if (h.few) return head_few_forward(c, h, loss0, loss1, lse0, lse1, stream);
     const HeadWs w = head_ws_layout(h, false, c.T, c.K, c.top);
     HeadMaps maps;
     if (!head_encode(c, h, w, h.bn, &maps)) return SBN_ERR_CUDA;
     HeadRowsJob rows{};
     rows.loss0 = loss0; rows.loss1 = loss1; rows.lse0 = lse0; rows.lse1 = lse1;
     HeadLogitsParams p{};
-    sbn_status st = launch_head_rows(c, w, rows, &p.tg, stream);
+    sbn_status st = launch_head_targets(c, w, &p.tg, stream);
+    rows.tg = p.tg;
+    if (st == SBN_OK) st = launch_head_rows(c, w, rows, stream);
     if (st != SBN_OK) return st;
     const bool list = c.top != 0, dual = list && c.labels;
     p.count = reinterpret_cast<int*>(c.ws + w.count);
@@ -172,16 +268,14 @@ static sbn_status head_forward(const HeadCall& c, float* loss0, float* loss1, fl
     p.skip_loads = g_test_break_waits;
     st = launch_head_logits<0>(maps, p, list, dual, stream);
     if (st != SBN_OK) return st;
-    const HeadLossJob j{p.tg, p.count, p.row_src, p.part, p.part1, p.z_ev, h.parts, 1.0 / static_cast<double>(c.tau), loss0, loss1, lse0, lse1};
-    const int blocks = std::min((c.T + kLossWarps - 1) / kLossWarps, 8 * device_sm_count());
-    if (launch_kernel(head_losses_kernel, dim3(blocks), dim3(32 * kLossWarps), 0, stream, j) != cudaSuccess) return SBN_ERR_CUDA;
-    ++g_launch_count;
-    return SBN_OK;
+    return launch_head_losses(HeadLossJob{p.tg, p.count, p.row_src, c.T, c.N, p.part, p.part1, p.z_ev, h.parts, 1.0 / static_cast<double>(c.tau), loss0, loss1, lse0,
+                                          lse1}, stream);
 }
 
 static sbn_status head_backward(const HeadCall& c, const float* lse0, const float* lse1, const float* g0, const float* g1, void* dx, void* dhead,
                                 cudaStream_t stream) {
     const HeadPlan h = head_plan(c.T, c.N, c.K);
+    if (h.few) return head_few_backward(c, h, lse0, lse1, g0, g1, dx, dhead, stream);
     const HeadWs w = head_ws_layout(h, true, c.T, c.K, c.top);
     const uint64_t k = static_cast<uint64_t>(c.K), t = static_cast<uint64_t>(c.T);
     HeadMaps maps;
@@ -194,7 +288,9 @@ static sbn_status head_backward(const HeadCall& c, const float* lse0, const floa
     HeadRowsJob rows{};
     rows.row_of = reinterpret_cast<int*>(c.ws + w.row_of);
     HeadLogitsParams p{};
-    sbn_status st = launch_head_rows(c, w, rows, &p.tg, stream);
+    sbn_status st = launch_head_targets(c, w, &p.tg, stream);
+    rows.tg = p.tg;
+    if (st == SBN_OK) st = launch_head_rows(c, w, rows, stream);
     if (st != SBN_OK) return st;
     const bool list = c.top != 0, dual = list && c.labels;
     p.count = reinterpret_cast<int*>(c.ws + w.count);
@@ -234,14 +330,7 @@ static sbn_status head_backward(const HeadCall& c, const float* lse0, const floa
             return SBN_ERR_CUDA;
         ++g_launch_count;
     }
-    if (dx) {
-        const HeadDxJob j{rows.row_of, q.acc, h.slots, c.T, c.K, static_cast<uint16_t*>(dx)};
-        const long long steps = (static_cast<long long>(c.T) * (c.K / 8) + kDxThreads - 1) / kDxThreads;
-        const int blocks = static_cast<int>(std::min<long long>(steps, 16ll * device_sm_count()));
-        if (launch_kernel(head_dx_kernel, dim3(blocks), dim3(kDxThreads), 0, stream, j) != cudaSuccess) return SBN_ERR_CUDA;
-        ++g_launch_count;
-    }
-    return SBN_OK;
+    return dx ? launch_head_dx(HeadDxJob{rows.row_of, q.acc, h.slots, c.T, c.K, static_cast<uint16_t*>(dx)}, stream) : SBN_OK;
 }
 
 }  // namespace sbn

@@ -33,6 +33,25 @@ struct HeadTargets {
     int events;
 };
 
+// What is asked of token t.
+__device__ __forceinline__ int head_token_flags(const HeadTargets& tg, int t, int N) {
+    if (tg.flags != nullptr) return tg.flags[t];
+    const long long y = tg.labels[t];
+    return y < 0 ? 0 : (y < N ? kRowLabel : kRowBadLabel);
+}
+__device__ __forceinline__ void report_bad(int flags) {
+    if (flags & (kRowBadTeacher | kRowBadLabel)) atomicExch(&g_device_status, static_cast<int>(SBN_ERR_INDEX));
+}
+// A token left out: the outputs of a forward call (any pointer may be null; distillation 0, label 1), and what is wrong with it.
+__device__ __forceinline__ void write_left_out(float* loss0, float* loss1, float* lse0, float* lse1, int t, int flags) {
+    const float nan = __uint_as_float(0x7FC00000u);
+    if (loss0 != nullptr) loss0[t] = (flags & kRowBadTeacher) ? nan : 0.0f;
+    if (loss1 != nullptr) loss1[t] = (flags & kRowBadLabel) ? nan : 0.0f;
+    if (lse0 != nullptr) lse0[t] = 0.0f;
+    if (lse1 != nullptr) lse1[t] = 0.0f;
+    report_bad(flags);
+}
+
 struct HeadTargetsJob {
     const long long* index;                       // [T][top]
     const void* logits;                           // [T][top] fp32 or bf16
@@ -105,31 +124,24 @@ head_targets_kernel(const HeadTargetsJob j) {
         }
         if (lane == 0) {
             j.flags[t] = flags;
-            if (flags & (kRowBadTeacher | kRowBadLabel)) atomicExch(&g_device_status, static_cast<int>(SBN_ERR_INDEX));
+            report_bad(flags);
         }
         __syncwarp();
     }
 }
 
 struct HeadRowsJob {
-    const long long* labels;                      // cross entropy (flags null)
-    const unsigned char* flags;                   // distillation
+    HeadTargets tg;
     const uint16_t* x;                            // [T][K]
     int T, K, N;
     int* count;                                   // out: number of rows that count
     int* row_src;                                 // out [T]: token of row r
     int* row_of;                                  // out [T] or null: row of token t, -1 if left out
     uint16_t* xc;                                 // out [T up to a multiple of 64][K], written only if rows are left out
-    float *loss0, *loss1, *lse0, *lse1;           // forward: outputs of rows left out (any may be null): distillation / label
+    float *loss0, *loss1, *lse0, *lse1;           // forward: outputs of rows left out (all null: backward)
 };
 
 constexpr int kRowsThreads = 256;
-
-__device__ __forceinline__ int head_row_flags(const HeadRowsJob& j, int t) {
-    if (j.flags != nullptr) return j.flags[t];
-    const long long y = j.labels[t];
-    return y < 0 ? 0 : (y < j.N ? kRowLabel : kRowBadLabel);
-}
 
 // Sum of v over the block; every thread gets it.
 __device__ __forceinline__ int block_sum(int v, int* scratch) {
@@ -154,7 +166,7 @@ head_rows_kernel(const HeadRowsJob j, const int per) {
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     int before = 0, total = 0;
     for (int t = tid; t < j.T; t += kRowsThreads) {
-        const int c = (head_row_flags(j, t) & (kRowDistill | kRowLabel)) ? 1 : 0;
+        const int c = (head_token_flags(j.tg, t, j.N) & (kRowDistill | kRowLabel)) ? 1 : 0;
         total += c;
         before += t < first ? c : 0;
     }
@@ -163,7 +175,7 @@ head_rows_kernel(const HeadRowsJob j, const int per) {
     if (blockIdx.x == 0 && tid == 0) *j.count = total;
     for (int t0 = first; t0 < last; t0 += kRowsThreads) {
         const int t = t0 + tid;
-        const int flags = t < last ? head_row_flags(j, t) : 0;
+        const int flags = t < last ? head_token_flags(j.tg, t, j.N) : 0;
         const bool counts = (flags & (kRowDistill | kRowLabel)) != 0;
         const unsigned ballot = __ballot_sync(0xFFFFFFFFu, counts);
         __syncthreads();
@@ -179,13 +191,8 @@ head_rows_kernel(const HeadRowsJob j, const int per) {
         if (counts) j.row_src[r] = t;
         if (t < last) {
             if (j.row_of != nullptr) j.row_of[t] = counts ? r : -1;
-            if (j.flags == nullptr && (flags & kRowBadLabel)) atomicExch(&g_device_status, static_cast<int>(SBN_ERR_INDEX));
             if (!counts) {
-                const float nan = __uint_as_float(0x7FC00000u);
-                if (j.loss0 != nullptr) j.loss0[t] = (flags & kRowBadTeacher) ? nan : 0.0f;
-                if (j.loss1 != nullptr) j.loss1[t] = (flags & kRowBadLabel) ? nan : 0.0f;
-                if (j.lse0 != nullptr) j.lse0[t] = 0.0f;
-                if (j.lse1 != nullptr) j.lse1[t] = 0.0f;
+                write_left_out(j.loss0, j.loss1, j.lse0, j.lse1, t, flags);
             }
         }
         if (total < j.T) {
@@ -211,8 +218,9 @@ head_rows_kernel(const HeadRowsJob j, const int per) {
 
 struct HeadLossJob {
     HeadTargets tg;
-    const int* count;
+    const int* count;                             // null (few tokens): every token has its row
     const int* row_src;
+    int T, N;
     const float2* part;                           // [rows][parts]: maximum m of the raw logits, sum of exp((z - m) / tau)
     const float* part1;                           // [rows][parts] or null: sum of exp(z - m)
     const float* z_ev;                            // [rows][events]: logits at the events
@@ -230,8 +238,14 @@ head_losses_kernel(const HeadLossJob j) {
     pdl_launch_dependents();
     pdl_wait();
     const int lane = threadIdx.x & 31;
-    const int rows = *j.count;
+    const int rows = j.count != nullptr ? *j.count : j.T;
     for (int r = blockIdx.x * kLossWarps + (threadIdx.x >> 5); r < rows; r += gridDim.x * kLossWarps) {
+        const int t = j.count != nullptr ? j.row_src[r] : r;
+        const int flags = head_token_flags(j.tg, t, j.N);
+        if (!(flags & (kRowDistill | kRowLabel))) {           // few tokens only: rows left out are no rows otherwise
+            if (lane == 0) write_left_out(j.loss0, j.loss1, j.lse0, j.lse1, t, flags);
+            continue;
+        }
         const size_t p0 = static_cast<size_t>(r) * j.parts;
         float m = -INFINITY;
         for (int i = lane; i < j.parts; i += 32) m = fmaxf(m, j.part[p0 + i].x);
@@ -247,7 +261,6 @@ head_losses_kernel(const HeadLossJob j) {
             s0 += __shfl_xor_sync(0xFFFFFFFFu, s0, o);
             s1 += __shfl_xor_sync(0xFFFFFFFFu, s1, o);
         }
-        const int t = j.row_src[r];
         const double lse0 = static_cast<double>(m) * j.inv_tau + log(s0);
         if (j.tg.flags == nullptr) {                          // cross entropy
             if (lane == 0) {
@@ -257,7 +270,6 @@ head_losses_kernel(const HeadLossJob j) {
             continue;
         }
         const double lse1 = static_cast<double>(m) + (j.part1 != nullptr ? log(s1) : 0.0);
-        const int flags = j.tg.flags[t];
         double kd = 0.0, ce = 0.0;
         for (int i = lane; i < j.tg.events; i += 32) {
             if (j.tg.ev_col[static_cast<size_t>(t) * j.tg.events + i] == kNoColumn) continue;
@@ -284,7 +296,7 @@ head_losses_kernel(const HeadLossJob j) {
 }
 
 struct HeadDxJob {
-    const int* row_of;
+    const int* row_of;                            // null (few tokens): every token has its row
     const float* acc;                             // [slots][T][K]
     int slots, T, K;
     uint16_t* dx;                                 // [T][K]
@@ -301,7 +313,7 @@ head_dx_kernel(const HeadDxJob j) {
     const size_t slot = static_cast<size_t>(j.T) * j.K;
     for (long long i = static_cast<long long>(blockIdx.x) * kDxThreads + threadIdx.x; i < all; i += static_cast<long long>(gridDim.x) * kDxThreads) {
         const int t = static_cast<int>(i / vecs), c = static_cast<int>(i - static_cast<long long>(t) * vecs);
-        const int r = j.row_of[t];
+        const int r = j.row_of != nullptr ? j.row_of[t] : t;
         float v[8] = {};
         if (r >= 0) {
             const float* a = j.acc + static_cast<size_t>(r) * j.K + 8 * c;
