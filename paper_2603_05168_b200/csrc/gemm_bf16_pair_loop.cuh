@@ -2,7 +2,7 @@
 // accumulators (the output head's logits and gradients, head_gemm_tcgen05.cuh).  The scheme is that of
 // gemm_bf16_pair_tcgen05.cuh: two CTAs of a cluster issue one `tcgen05.mma.cta_group::2.kind::f16` (M = 256: each CTA
 // supplies 128 rows of A and half of the B tile and keeps its 128 x BN slice of the accumulator in its own tensor memory),
-// TMA fills seven stages of 64 contraction steps, the two 256-column halves of tensor memory alternate as accumulators, so
+// TMA fills the stages of 64 contraction steps, the two 256-column halves of tensor memory alternate as accumulators, so
 // the epilogue of a tile runs under the next tile's MMAs.  No TMA multicast.  All waits are bounded.
 //
 //   warps        0 TMA producer (both CTAs), 1 MMA issuer (leader CTA only; both allocate TMEM),
@@ -14,8 +14,11 @@
 //   Work::Tile                     a tile: at least { int k_stages; int bn; }
 //   Work::Tiles(work, pair)        the tiles of a CTA pair in order: bool next(Tile&)
 //   load(tile, ks, rank, st, bar)  issues stage ks of the tile for this CTA: A at st, B at st + kPairLoopStageA
+//   kStages, kStagingBytes         stages of 32 KB, and shared memory behind them for the epilogue
 //   idesc(tile), a_desc(tile, st), a_step(tile), b_desc(tile, st), b_step(tile)   operand descriptors and their advance per MMA
-//   Epilogue(work, rank, quarter, parity, lane): begin(tile) before the accumulator is there, then run(tile, taddr, release)
+//   Epilogue(work, rank, quarter, parity, lane, staging): begin(tile) before the accumulator is there, then
+//                                  run(tile, taddr, release); finish() after the last tile
+// All epilogue warps of a CTA take a tile or none does (a barrier with a vote), so an epilogue may synchronise its warps.
 #pragma once
 
 #include "gemm_bf16_pair_tcgen05.cuh"
@@ -24,9 +27,22 @@ namespace sbn {
 
 constexpr int kPairLoopStageA = kBf16StageA;
 constexpr int kPairLoopStageBytes = kBf16StageBytes;
-constexpr int kPairLoopStages = kBf16Stages;
-constexpr int kPairLoopSmemBytes = kBf16SmemBytes;
 constexpr int kPairLoopThreads = kBf16Threads;
+template <class Work>
+constexpr int pair_loop_smem_bytes() {
+    constexpr int bytes = Work::kStages * kPairLoopStageBytes + Work::kStagingBytes + kBarrierBytes;
+    static_assert(bytes <= 232448 && Work::kStagingBytes % 1024 == 0, "shared memory overflow");
+    return bytes;
+}
+
+// Barrier of the epilogue warps of a CTA.
+__device__ __forceinline__ void epilogue_sync() { asm volatile("bar.sync 1, %0;" ::"n"(32 * kBf16EpiWarps) : "memory"); }
+__device__ __forceinline__ bool epilogue_all(bool ok) {
+    uint32_t all;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.and.pred q, 1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(all) : "r"(static_cast<uint32_t>(ok)), "n"(32 * kBf16EpiWarps) : "memory");
+    return all != 0;
+}
 
 // Instruction descriptor for kind::f16: D = fp32, A = B = bf16; either operand K-major or MN-major.
 __host__ __device__ constexpr uint32_t make_idesc_bf16_any(int mma_m, int mma_n, bool a_mn_major, bool b_mn_major) {
@@ -36,14 +52,15 @@ __host__ __device__ constexpr uint32_t make_idesc_bf16_any(int mma_m, int mma_n,
 
 template <class Work>
 __device__ __forceinline__ void bf16_pair_loop(Work& work, const bool skip_loads) {
-    constexpr int STAGES = kPairLoopStages;
+    constexpr int STAGES = Work::kStages;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = smem_u32(smem_raw);
     if (smem_base & 1023u) {          // swizzled tiles need 1 KB alignment; identical in every CTA
         if (threadIdx.x == 0) atomicExch(&g_device_status, static_cast<int>(SBN_ERR_CUDA));
         return;
     }
-    const uint32_t bar_full = smem_base + STAGES * kPairLoopStageBytes;
+    const uint32_t staging = smem_base + STAGES * kPairLoopStageBytes;
+    const uint32_t bar_full = staging + Work::kStagingBytes;
     const uint32_t bar_empty = bar_full + 8 * STAGES;
     const uint32_t bar_acc_full = bar_empty + 8 * STAGES;     // [2]
     const uint32_t bar_acc_empty = bar_acc_full + 16;         // [2]
@@ -141,14 +158,13 @@ __device__ __forceinline__ void bf16_pair_loop(Work& work, const bool skip_loads
         uint32_t acc_iter = 0;
         typename Work::Tiles tiles(work, pair_id);
         typename Work::Tile t;
-        typename Work::Epilogue epi(work, static_cast<int>(rank), quarter, parity, lane);
+        typename Work::Epilogue epi(work, static_cast<int>(rank), quarter, parity, lane, staging);
         while (tiles.next(t)) {
             const uint32_t buf = acc_iter & 1u;
             const uint32_t acc_phase = (acc_iter >> 1) & 1u;
             const uint32_t acc_empty_leader = map_to_cta(bar_acc_empty + 8 * buf, 0);
             epi.begin(t);
-            // the lanes leave together or not at all: what follows reads tensor memory warp by warp
-            if (!__all_sync(0xFFFFFFFFu, mbar_wait(bar_acc_full + 8 * buf, acc_phase, abort_flag))) break;
+            if (!epilogue_all(mbar_wait(bar_acc_full + 8 * buf, acc_phase, abort_flag))) break;
             tcgen05_fence_after();
             // gives the accumulator back; once per tile and warp, after the warp's last read of it
             auto release = [&] {
@@ -159,6 +175,7 @@ __device__ __forceinline__ void bf16_pair_loop(Work& work, const bool skip_loads
             epi.run(t, tmem_base + lane_base + buf * 256u, release);
             ++acc_iter;
         }
+        epi.finish();
     }
 
     // teardown: nobody leaves while the peer may still touch this CTA's smem, barriers or TMEM

@@ -13,7 +13,7 @@
 // are not contracted over (dx, dW) `movmatrix` transposes registers as 8 x 8 tiles, whose columns then come out as 8 t + 2 j.
 #pragma once
 
-#include "head_gemm_tcgen05.cuh"
+#include "head_words_tcgen05.cuh"
 
 namespace sbn {
 

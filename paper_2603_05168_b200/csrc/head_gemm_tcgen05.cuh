@@ -24,6 +24,18 @@ __device__ __forceinline__ float ex2_approx(float v) {        // relative error 
     return r;
 }
 
+__device__ __forceinline__ void st_shared_16(uint32_t to, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, int c0, int c1, int c2, uint32_t src) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];"
+                 ::"l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(src) : "memory");
+}
+__device__ __forceinline__ void tma_add_3d(const CUtensorMap* map, int c0, int c1, int c2, uint32_t src) {
+    asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.bulk_group [%0, {%1, %2, %3}], [%4];"
+                 ::"l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(src) : "memory");
+}
+
 struct HeadMaps {
     CUtensorMap x, xc;            // K-major: the tokens' rows, or the rows that count moved together
     CUtensorMap w;                // K-major, BN / 2 rows per box
@@ -52,8 +64,137 @@ struct HeadLogitsParams {
 
 // MODE 0 stats, 1 grad.  LIST: targets are sorted events (distillation), else the label alone.  DUAL: the label's loss at
 // temperature 1 beside the teacher's.
+//
+// What a thread does with the logits of its row, 32 neighbouring columns at a time in ascending order.
+template <int MODE, bool LIST, bool DUAL>
+struct HeadRow {
+    int r, t;                     // row of the products, its token
+    bool here;                    // something is asked of it
+    int next_col, e;              // the next target at or behind the current column
+    float l0, l1, g0, g1;         // grad: -lse log2(e) and gradient per loss
+    float m, s0, s1;              // stats
+
+    static constexpr float kLog2e = 1.4426950408889634f;
+
+    // Row r with token t; `asked` says whether anything is asked of it.
+    __device__ void begin(const HeadLogitsParams& p, int row, int token, bool asked) {
+        r = row;
+        t = token;
+        here = asked;
+        next_col = kNoColumn;
+        e = 0;
+        m = l0 = l1 = -INFINITY;
+        s0 = s1 = g0 = g1 = 0.0f;
+        if constexpr (MODE == 1) {
+            if (!here) return;
+            const int flags = LIST ? p.tg.flags[t] : kRowDistill;
+            if (flags & kRowDistill) {
+                l0 = -p.lse0[t] * kLog2e;
+                g0 = p.g0[t] * p.inv_tau;
+            }
+            if (DUAL && (flags & kRowLabel)) {
+                l1 = -p.lse1[t] * kLog2e;
+                g1 = p.g1[t];
+            }
+        }
+    }
+    __device__ const int* list(const HeadLogitsParams& p) const { return p.tg.ev_col + static_cast<size_t>(t) * p.tg.events; }
+    // To the first target at or behind column n.
+    __device__ void seek(const HeadLogitsParams& p, int n) {
+        next_col = kNoColumn;
+        if (!here) return;
+        if constexpr (LIST) {
+            const int* col = list(p);
+            int lo = 0, hi = p.tg.events;
+            while (lo < hi) {
+                const int mid = (lo + hi) >> 1;
+                if (col[mid] < n) lo = mid + 1; else hi = mid;
+            }
+            e = lo;
+            if (e < p.tg.events) next_col = col[e];
+        } else {
+            const int label = static_cast<int>(p.tg.labels[t]);
+            if (label >= n) next_col = label;
+        }
+    }
+    __device__ void step(const HeadLogitsParams& p) {
+        if constexpr (LIST) {
+            ++e;
+            next_col = e < p.tg.events ? list(p)[e] : kNoColumn;
+        } else {
+            next_col = kNoColumn;
+        }
+    }
+
+    // Columns n .. n + 31.
+    __device__ void stats(const HeadLogitsParams& p, uint32_t (&z)[32], int n) {
+        while (next_col < n) step(p);
+        while (next_col < n + 32) {                    // rare: a row has a handful of targets in the whole vocabulary
+            float v = 0.0f;
+#pragma unroll
+            for (int q = 0; q < 32; ++q) v = next_col - n == q ? __uint_as_float(z[q]) : v;
+            p.z_ev[static_cast<size_t>(r) * p.tg.events + (LIST ? e : 0)] = v;
+            step(p);
+        }
+        if (n >= p.N) return;
+        if (n + 32 > p.N) {                            // behind the vocabulary: nothing
+#pragma unroll
+            for (int q = 0; q < 32; ++q) z[q] = n + q < p.N ? z[q] : 0xFF800000u;
+        }
+        float mc = __uint_as_float(z[0]);
+#pragma unroll
+        for (int q = 1; q < 32; ++q) mc = fmaxf(mc, __uint_as_float(z[q]));
+        const float m_new = fmaxf(m, mc);
+        s0 *= ex2_approx((m - m_new) * p.c0);
+        if (DUAL) s1 *= ex2_approx((m - m_new) * kLog2e);
+        m = m_new;
+#pragma unroll
+        for (int q = 0; q < 32; ++q) {
+            const float d = __uint_as_float(z[q]) - m;      // the difference first: exact where it matters
+            s0 += ex2_approx(d * p.c0);
+            if (DUAL) s1 += ex2_approx(d * kLog2e);
+        }
+    }
+    __device__ void store_part(const HeadLogitsParams& p, int part) const {
+        const size_t at = static_cast<size_t>(r) * p.parts + part;
+        p.part[at] = make_float2(m, s0);
+        if (DUAL) p.part1[at] = s1;
+    }
+
+    // Columns n .. n + 31 of dz, zeros in rows that nothing is asked of and behind the vocabulary.
+    __device__ void grad(const HeadLogitsParams& p, const uint32_t (&z)[32], int n) {
+        while (next_col < n) step(p);
+        float v[32];
+#pragma unroll
+        for (int q = 0; q < 32; ++q) {
+            v[q] = ex2_approx(fmaf(__uint_as_float(z[q]), p.c0, l0)) * g0;
+            if (DUAL) v[q] = fmaf(ex2_approx(fmaf(__uint_as_float(z[q]), kLog2e, l1)), g1, v[q]);
+        }
+        while (next_col < n + 32) {
+            float off = g0;
+            if constexpr (LIST) {
+                const float q = p.tg.ev_w[static_cast<size_t>(t) * p.tg.events + e];
+                off = q < 0.0f ? g1 : q * g0;
+            }
+#pragma unroll
+            for (int q = 0; q < 32; ++q) v[q] -= next_col - n == q ? off : 0.0f;
+            step(p);
+        }
+        uint32_t o[16];
+#pragma unroll
+        for (int q = 0; q < 16; ++q) {
+            const bool in0 = here && n + 2 * q < p.N, in1 = here && n + 2 * q + 1 < p.N;
+            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[q]) : "f"(in1 ? v[2 * q + 1] : 0.0f), "f"(in0 ? v[2 * q] : 0.0f));
+        }
+        uint4* to = reinterpret_cast<uint4*>(p.dz + static_cast<size_t>(r) * p.ldz + (n - p.v0));
+#pragma unroll
+        for (int q = 0; q < 4; ++q) to[q] = make_uint4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
+    }
+};
+
 template <int MODE, bool LIST, bool DUAL>
 struct HeadLogitsWork {
+    static constexpr int kStages = 7, kStagingBytes = 0;
     const HeadMaps& maps;
     const HeadLogitsParams& p;
     int rows, tiles_m, tiles_v;
@@ -101,74 +242,24 @@ struct HeadLogitsWork {
     struct Epilogue {
         const HeadLogitsWork& w;
         int rank, quarter, parity, lane;
-        int r, t;                 // row that counts, its token
-        int next_col, e;          // the next target at or behind the current column
-        const int* ev_col;
-        float l0, l1, g0, g1;     // grad: -lse log2(e) and gradient per loss
+        HeadRow<MODE, LIST, DUAL> row;
 
-        __device__ Epilogue(const HeadLogitsWork& work, int rk, int q, int par, int ln) : w(work), rank(rk), quarter(q), parity(par), lane(ln) {}
-
-        __device__ void advance(int col) {                 // to the first target at or behind `col`
-            if constexpr (LIST) {
-                while (next_col < col) {
-                    ++e;
-                    next_col = e < w.p.tg.events ? ev_col[e] : kNoColumn;
-                }
-            } else {
-                if (next_col < col) next_col = kNoColumn;
-            }
-        }
-
+        __device__ Epilogue(const HeadLogitsWork& work, int rk, int q, int par, int ln, uint32_t) : w(work), rank(rk), quarter(q), parity(par), lane(ln) {}
         __device__ void begin(const Tile& tile) {
-            const HeadLogitsParams& p = w.p;
-            r = tile.m0 + rank * 128 + quarter * 32 + lane;
-            t = 0;
-            next_col = kNoColumn;
-            e = 0;
-            l0 = l1 = -INFINITY;
-            g0 = g1 = 0.0f;
-            if (r >= w.rows) return;
-            t = p.row_src[r];
-            if constexpr (LIST) {
-                ev_col = p.tg.ev_col + static_cast<size_t>(t) * p.tg.events;
-                int lo = 0, hi = p.tg.events;              // first event at or behind the tile's columns
-                while (lo < hi) {
-                    const int mid = (lo + hi) >> 1;
-                    if (ev_col[mid] < tile.n0) lo = mid + 1; else hi = mid;
-                }
-                e = lo;
-                next_col = e < p.tg.events ? ev_col[e] : kNoColumn;
-            } else {
-                next_col = static_cast<int>(p.tg.labels[t]);
-                if (next_col < tile.n0) next_col = kNoColumn;
-            }
-            if constexpr (MODE == 1) {
-                constexpr float kLog2e = 1.4426950408889634f;
-                const int flags = LIST ? p.tg.flags[t] : kRowDistill;
-                if (flags & kRowDistill) {
-                    l0 = -p.lse0[t] * kLog2e;
-                    g0 = p.g0[t] * p.inv_tau;
-                }
-                if (DUAL && (flags & kRowLabel)) {
-                    l1 = -p.lse1[t] * kLog2e;
-                    g1 = p.g1[t];
-                }
-            }
+            const int r = tile.m0 + rank * 128 + quarter * 32 + lane;
+            const bool here = r < w.rows;
+            row.begin(w.p, r, here ? w.p.row_src[r] : 0, here);
+            row.seek(w.p, tile.n0);
         }
-
         template <class Release>
         __device__ void run(const Tile& tile, uint32_t taddr, Release&& release) {
-            const HeadLogitsParams& p = w.p;
             const int chunks = tile.bn >> 5;
-            const bool here = r < w.rows;
             const int first_row = tile.m0 + rank * 128 + quarter * 32;
             // rows that nobody reads: behind the last that counts (grad: behind the last stage that dW reads)
-            const bool idle = first_row >= (MODE == 0 ? w.rows : ((max(w.rows, 1) + 63) & ~63));
-            if (idle) {
+            if (first_row >= (MODE == 0 ? w.rows : ((max(w.rows, 1) + 63) & ~63))) {
                 release();
                 return;
             }
-            float m = -INFINITY, s0 = 0.0f, s1 = 0.0f;
 #pragma unroll 1
             for (int c = parity; c < chunks; c += 2) {
                 uint32_t z[32];
@@ -176,82 +267,12 @@ struct HeadLogitsWork {
                 tmem_ld_32x32b_x32(taddr + static_cast<uint32_t>(c * 32), z);
                 tmem_ld_wait();
                 if (c + 2 >= chunks) release();
-                const int n = tile.n0 + c * 32;
-                advance(n);
-                if constexpr (MODE == 0) {
-                    while (next_col < n + 32) {            // rare: a row has a handful of targets in the whole vocabulary
-                        float v = 0.0f;
-#pragma unroll
-                        for (int q = 0; q < 32; ++q) v = next_col - n == q ? __uint_as_float(z[q]) : v;
-                        if constexpr (LIST) {
-                            p.z_ev[static_cast<size_t>(r) * p.tg.events + e] = v;
-                            ++e;
-                            next_col = e < p.tg.events ? ev_col[e] : kNoColumn;
-                        } else {
-                            p.z_ev[r] = v;
-                            next_col = kNoColumn;
-                        }
-                    }
-                    if (n >= p.N) continue;
-                    if (n + 32 > p.N) {                    // behind the vocabulary: nothing
-#pragma unroll
-                        for (int q = 0; q < 32; ++q) z[q] = n + q < p.N ? z[q] : 0xFF800000u;
-                    }
-                    float mc = __uint_as_float(z[0]);
-#pragma unroll
-                    for (int q = 1; q < 32; ++q) mc = fmaxf(mc, __uint_as_float(z[q]));
-                    const float m_new = fmaxf(m, mc);
-                    s0 *= ex2_approx((m - m_new) * p.c0);
-                    if (DUAL) s1 *= ex2_approx((m - m_new) * 1.4426950408889634f);
-                    m = m_new;
-#pragma unroll
-                    for (int q = 0; q < 32; ++q) {
-                        const float d = __uint_as_float(z[q]) - m;      // the difference first: exact where it matters
-                        s0 += ex2_approx(d * p.c0);
-                        if (DUAL) s1 += ex2_approx(d * 1.4426950408889634f);
-                    }
-                } else {
-                    float v[32];
-#pragma unroll
-                    for (int q = 0; q < 32; ++q) {
-                        v[q] = ex2_approx(fmaf(__uint_as_float(z[q]), p.c0, l0)) * g0;
-                        if (DUAL) v[q] = fmaf(ex2_approx(fmaf(__uint_as_float(z[q]), 1.4426950408889634f, l1)), g1, v[q]);
-                    }
-                    while (next_col < n + 32) {
-                        float off = g0;
-                        if constexpr (LIST) {
-                            const float q = p.tg.ev_w[static_cast<size_t>(t) * p.tg.events + e];
-                            off = q < 0.0f ? g1 : q * g0;
-                        }
-#pragma unroll
-                        for (int q = 0; q < 32; ++q) v[q] -= next_col - n == q ? off : 0.0f;
-                        if constexpr (LIST) {
-                            ++e;
-                            next_col = e < p.tg.events ? ev_col[e] : kNoColumn;
-                        } else {
-                            next_col = kNoColumn;
-                        }
-                    }
-                    uint32_t o[16];
-#pragma unroll
-                    for (int q = 0; q < 16; ++q) {
-                        const bool in0 = here && n + 2 * q < p.N, in1 = here && n + 2 * q + 1 < p.N;
-                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[q]) : "f"(in1 ? v[2 * q + 1] : 0.0f), "f"(in0 ? v[2 * q] : 0.0f));
-                    }
-                    uint4* to = reinterpret_cast<uint4*>(p.dz + static_cast<size_t>(r) * p.ldz + (n - p.v0));
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) to[q] = make_uint4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
-                }
+                if constexpr (MODE == 0) row.stats(w.p, z, tile.n0 + c * 32);
+                else row.grad(w.p, z, tile.n0 + c * 32);
             }
-            if constexpr (MODE == 0) {
-                if (here) store_part(tile, m, s0, s1);
-            }
+            if (MODE == 0 && row.here) row.store_part(w.p, 2 * ((tile.n0 - w.p.v0) / tile.bn) + parity);
         }
-        __device__ void store_part(const Tile& tile, float m, float s0, float s1) const {
-            const size_t at = static_cast<size_t>(r) * w.p.parts + 2 * ((tile.n0 - w.p.v0) / tile.bn) + parity;
-            w.p.part[at] = make_float2(m, s0);
-            if (DUAL) w.p.part1[at] = s1;
-        }
+        __device__ void finish() {}
     };
 };
 
@@ -264,18 +285,19 @@ head_logits_kernel(const __grid_constant__ HeadMaps maps, const __grid_constant_
 }
 
 // ---- gradients of a piece --------------------------------------------------------------------------
+// dw, acc: how results leave, in boxes of 128 rows x 128 bytes.
 struct HeadGradMaps {
     CUtensorMap aw;               // dz piece for dW: MN-major, two blocks of 64 columns
     CUtensorMap ax;               // dz piece for dx: K-major
     CUtensorMap bx[2], bxc[2];    // x, or the rows that count moved together: MN-major, two blocks, one block (half tiles)
     CUtensorMap bw[2];            // the piece's rows of W
+    CUtensorMap dw;               // [cols][K] bf16
+    CUtensorMap acc;              // [slots][T][K] fp32
 };
 struct HeadGradParams {
-    const int* count;
+    const int* count;             // null: all rows, zeros in place of those left out (`moved` rows)
     int T, K;
     int cols;                     // vocabulary rows of the piece
-    uint16_t* dw;                 // [cols][K], or null with no tiles of part 0
-    float* acc;                   // dx sums: [slots][T][K]
     int slot_stages;              // dx's contraction is cut into slices of that many stages, each with a slot of its own
     int add;                      // not the first piece: add to acc
     BackwardPlan plan;            // part 0: dW, part 1: dx (tile index = slice * tiles of dx + tile)
@@ -283,6 +305,7 @@ struct HeadGradParams {
 };
 
 struct HeadGradsWork {
+    static constexpr int kStages = 6, kStagingBytes = 2 * 128 * 128;
     const HeadGradMaps& maps;
     const HeadGradParams& p;
     int rows;
@@ -290,8 +313,8 @@ struct HeadGradsWork {
 
     __device__ HeadGradsWork(const HeadGradMaps& m, const HeadGradParams& q) : maps(m), p(q) {}
     __device__ void start() {
-        rows = *p.count;
-        moved = rows < p.T;
+        rows = p.count != nullptr ? *p.count : p.T;
+        moved = p.count == nullptr || rows < p.T;
     }
 
     struct Tile { int part, m0, n0, bn, k_stages, k_first, slot; };
@@ -345,49 +368,72 @@ struct HeadGradsWork {
     __device__ uint64_t a_desc(const Tile& t, uint32_t s) const { return make_smem_desc(s, t.part == 0 ? 8192 : 16, 1024, kSwz128); }
     __device__ uint64_t b_desc(const Tile&, uint32_t s) const { return make_smem_desc(s, 8192, 1024, kSwz128); }
 
+    // 64 columns of the tile at a time: every warp puts its 32 rows x 32 columns into shared memory (the 128-byte swizzle keeps the
+    // rows' 16-byte pieces on different banks), and one thread stores 128 rows x 128 bytes by TMA, which also clips what lies
+    // outside.  Stored by the threads themselves, a row each, every 16 bytes were a transaction of their own: 4 us per fp32 tile.
     struct Epilogue {
         const HeadGradsWork& w;
         int rank, quarter, parity, lane;
-        __device__ Epilogue(const HeadGradsWork& work, int rk, int q, int par, int ln) : w(work), rank(rk), quarter(q), parity(par), lane(ln) {}
+        uint32_t staging;
+        __device__ Epilogue(const HeadGradsWork& work, int rk, int q, int par, int ln, uint32_t st) : w(work), rank(rk), quarter(q), parity(par), lane(ln), staging(st) {}
         __device__ void begin(const Tile&) {}
+        __device__ bool leader() const { return quarter == 0 && parity == 0 && lane == 0; }
 
         template <class Release>
         __device__ void run(const Tile& t, uint32_t taddr, Release&& release) {
             const HeadGradParams& p = w.p;
-            const int m = t.m0 + rank * 128 + quarter * 32 + lane;
-            const int chunks = t.bn >> 5;
-            const bool mine = m < (t.part == 0 ? p.cols : w.rows);
+            const int m0 = t.m0 + rank * 128;
+            const bool rows_in = m0 < (t.part == 0 ? p.cols : w.rows);
+            const int pairs = t.bn >> 6;
+            const int row = quarter * 32 + lane;
 #pragma unroll 1
-            for (int c = parity; c < chunks; c += 2) {
+            for (int c = 0; c < pairs; ++c) {
                 uint32_t v[32];
                 __syncwarp();
-                tmem_ld_32x32b_x32(taddr + static_cast<uint32_t>(c * 32), v);
+                tmem_ld_32x32b_x32(taddr + static_cast<uint32_t>(c * 64 + parity * 32), v);
                 tmem_ld_wait();
-                if (c + 2 >= chunks) release();
-                const int n = t.n0 + c * 32;
-                if (!mine || n >= p.K) continue;            // K % 32 == 0: a chunk is in or out as a whole
+                if (c + 1 == pairs) release();
+                const int n = t.n0 + c * 64;
+                if (!rows_in || n >= p.K) continue;         // the same for all warps; K % 64 == 0
+                if (leader()) {                             // the buffers' last stores have been read out (dW: the one before the last)
+                    if (t.part == 0 && c > 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+                    else asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                }
+                epilogue_sync();
                 if (t.part == 0) {
-                    uint32_t o[16];
+                    const uint32_t to = staging + static_cast<uint32_t>((c & 1) * 16384 + row * 128);
 #pragma unroll
-                    for (int q = 0; q < 16; ++q)
-                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[q]) : "f"(__uint_as_float(v[2 * q + 1])), "f"(__uint_as_float(v[2 * q])));
-                    uint4* to = reinterpret_cast<uint4*>(p.dw + static_cast<size_t>(m) * p.K + n);
+                    for (int q = 0; q < 4; ++q) {
+                        uint32_t o[4];
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) to[q] = make_uint4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
-                } else {
-                    float* to = p.acc + (static_cast<size_t>(t.slot) * p.T + m) * p.K + n;
-                    // One tile of a launch writes an element, and launches follow one another: the sum's order is fixed
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) {
-                        if (p.add)
-                            asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};"
-                                         ::"l"(to + 4 * q), "f"(__uint_as_float(v[4 * q])), "f"(__uint_as_float(v[4 * q + 1])),
-                                           "f"(__uint_as_float(v[4 * q + 2])), "f"(__uint_as_float(v[4 * q + 3])) : "memory");
-                        else
-                            *reinterpret_cast<uint4*>(to + 4 * q) = make_uint4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+                        for (int i = 0; i < 4; ++i)
+                            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[i]) : "f"(__uint_as_float(v[8 * q + 2 * i + 1])), "f"(__uint_as_float(v[8 * q + 2 * i])));
+                        st_shared_16(to + (((parity * 4 + q) ^ (row & 7)) << 4), o[0], o[1], o[2], o[3]);
                     }
+                } else {
+                    const uint32_t to = staging + static_cast<uint32_t>(parity * 16384 + row * 128);
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) st_shared_16(to + ((q ^ (row & 7)) << 4), v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                epilogue_sync();
+                if (leader()) {
+                    if (t.part == 0) {
+                        tma_store_2d(&w.maps.dw, n, m0, staging + static_cast<uint32_t>((c & 1) * 16384));
+                    } else {
+                        // One tile of a launch adds to an element, and launches follow one another: the sum's order is fixed
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            if (p.add) tma_add_3d(&w.maps.acc, n + 32 * h, m0, t.slot, staging + static_cast<uint32_t>(h * 16384));
+                            else tma_store_3d(&w.maps.acc, n + 32 * h, m0, t.slot, staging + static_cast<uint32_t>(h * 16384));
+                        }
+                    }
+                    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                 }
             }
+        }
+        __device__ void finish() {
+            if (leader()) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
         }
     };
 };

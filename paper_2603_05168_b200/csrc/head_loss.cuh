@@ -8,6 +8,7 @@ namespace sbn {
 // How a call is cut up, from its sizes alone.
 struct HeadPlan {
     bool few;                     // head_few_mma.cuh
+    bool words;                   // logits by head_words_tcgen05.cuh, gradients as for any number of tokens
     int slabs, ranges, per;       // its gradient kernel: 256-column slabs x ranges of `per` blocks of 16 words
     int bn, parts;                // forward: columns per tile, partial sums per row
     int piece;                    // backward: columns of dz at a time (a multiple of 256)
@@ -47,10 +48,10 @@ static HeadPlan head_plan(int T, int N, int K) {
     }
     h.rows64 = head_up(T, 64);
     h.rows256 = head_up(T, 256);
+    h.words = T <= kWordsTokens;
     h.bn = head_tile_columns(T, N, K);
-    h.parts = 2 * ((N + h.bn - 1) / h.bn);
+    h.parts = h.words ? 4 * std::min((N + 127) / 128, kNumSMs) : 2 * ((N + h.bn - 1) / h.bn);
     long long cols = (128ll << 20) / (2 * h.rows256);
-    if (T <= 512) cols = std::min(cols, (40ll << 20) / (2ll * K));      // few tokens: the piece's rows of W stay in the L2 for dx
     cols = std::max(1024ll, cols / 256 * 256);
     const long long pieces = (N + cols - 1) / cols;
     h.piece = static_cast<int>(head_up((N + pieces - 1) / pieces, 256));
@@ -71,7 +72,7 @@ static HeadWs head_ws_layout(const HeadPlan& h, bool backward, int T, int K, int
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) & ~static_cast<size_t>(255); return here; };
     const size_t t = static_cast<size_t>(T), events = top ? static_cast<size_t>(top) + 1 : 1;
-    if (!h.few) {
+    if (!h.few && !h.words) {
         w.count = take(4);
         w.row_src = take(4 * t);
         w.row_of = take(4 * t);
@@ -81,7 +82,7 @@ static HeadWs head_ws_layout(const HeadPlan& h, bool backward, int T, int K, int
         w.ev_col = take(4 * t * events);
         w.ev_w = take(4 * t * events);
     }
-    if (!h.few) w.xc = take(2 * static_cast<size_t>(h.rows64) * K);
+    if (!h.few && !(h.words && !backward)) w.xc = take(2 * static_cast<size_t>(h.rows64) * K);
     if (!backward) {
         w.z_ev = take(4 * t * events);
         w.part = take(8 * t * h.parts);
@@ -92,6 +93,18 @@ static HeadWs head_ws_layout(const HeadPlan& h, bool backward, int T, int K, int
     }
     w.total = at;
     return w;
+}
+
+// Sums of dx, fp32 [slots][rows][cols], written in boxes of 128 rows x 128 bytes with the 128-byte swizzle in shared memory.
+static bool encode_3d_f32_out(CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, uint64_t slots) {
+    EncodeTiledFn fn = get_encode_fn();
+    if (!fn) return false;
+    cuuint64_t dims[3] = {cols, rows, slots};
+    cuuint64_t strides[2] = {cols * 4, cols * 4 * rows};
+    cuuint32_t box[3] = {32, 128, 1};
+    cuuint32_t estr[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // One call of either operator: top == 0 is the cross entropy.
@@ -110,16 +123,19 @@ struct HeadCall {
 
 static bool head_encode(const HeadCall& c, const HeadPlan& h, const HeadWs& w, int bn, HeadMaps* maps) {
     const uint64_t k = static_cast<uint64_t>(c.K);
+    if (h.words)
+        return encode_2d_bf16_sw128(&maps->x, c.x, k, c.T, k, static_cast<uint32_t>(head_up(c.T, 16))) && encode_2d_bf16_sw128(&maps->w, c.head, k, c.N, k, 128);
     return encode_2d_bf16_sw128(&maps->x, c.x, k, c.T, k, 128) && encode_2d_bf16_sw128(&maps->xc, c.ws + w.xc, k, h.rows64, k, 128) &&
            encode_2d_bf16_sw128(&maps->w, c.head, k, c.N, k, bn / 2);
 }
 
 template <int MODE, bool LIST, bool DUAL>
 static sbn_status launch_head_logits_as(const HeadMaps& maps, const HeadLogitsParams& p, cudaStream_t stream) {
-    if (!ensure_dynamic_smem<head_logits_kernel<MODE, LIST, DUAL>>(kPairLoopSmemBytes)) return SBN_ERR_CUDA;
+    constexpr int smem = pair_loop_smem_bytes<HeadLogitsWork<MODE, LIST, DUAL>>();
+    if (!ensure_dynamic_smem<head_logits_kernel<MODE, LIST, DUAL>>(smem)) return SBN_ERR_CUDA;
     const long long tiles = head_up(p.T, 256) / 256 * ((p.v1 - p.v0 + p.bn - 1) / p.bn);
     const unsigned pairs = static_cast<unsigned>(std::min<long long>(tiles, kBackwardPairs));
-    if (launch_kernel(head_logits_kernel<MODE, LIST, DUAL>, dim3(2 * pairs), dim3(kPairLoopThreads), kPairLoopSmemBytes, stream, maps, p) != cudaSuccess)
+    if (launch_kernel(head_logits_kernel<MODE, LIST, DUAL>, dim3(2 * pairs), dim3(kPairLoopThreads), smem, stream, maps, p) != cudaSuccess)
         return SBN_ERR_CUDA;
     ++g_launch_count;
     return SBN_OK;
@@ -128,6 +144,21 @@ template <int MODE>
 static sbn_status launch_head_logits(const HeadMaps& maps, const HeadLogitsParams& p, bool list, bool dual, cudaStream_t stream) {
     if (!list) return launch_head_logits_as<MODE, false, false>(maps, p, stream);
     return dual ? launch_head_logits_as<MODE, true, true>(maps, p, stream) : launch_head_logits_as<MODE, true, false>(maps, p, stream);
+}
+
+template <int MODE, bool LIST, bool DUAL>
+static sbn_status launch_head_words_as(const HeadMaps& maps, const HeadWordsParams& p, cudaStream_t stream) {
+    if (!ensure_dynamic_smem<head_words_kernel<MODE, LIST, DUAL>>(232448)) return SBN_ERR_CUDA;
+    const int ctas = std::min((p.p.v1 - p.p.v0 + 127) / 128, kNumSMs);
+    if (launch_kernel(head_words_kernel<MODE, LIST, DUAL>, dim3(ctas), dim3(kWordsThreads), words_smem_bytes(p.tok_pad), stream, maps, p) != cudaSuccess)
+        return SBN_ERR_CUDA;
+    ++g_launch_count;
+    return SBN_OK;
+}
+template <int MODE>
+static sbn_status launch_head_words(const HeadMaps& maps, const HeadWordsParams& p, bool list, bool dual, cudaStream_t stream) {
+    if (!list) return launch_head_words_as<MODE, false, false>(maps, p, stream);
+    return dual ? launch_head_words_as<MODE, true, true>(maps, p, stream) : launch_head_words_as<MODE, true, false>(maps, p, stream);
 }
 
 // What is asked of the tokens: the labels themselves, or for a distillation the sorted targets of every token.
@@ -166,7 +197,7 @@ static sbn_status launch_head_losses(const HeadLossJob& j, cudaStream_t stream) 
     return SBN_OK;
 }
 static sbn_status launch_head_dx(const HeadDxJob& j, cudaStream_t stream) {
-    const long long steps = (static_cast<long long>(j.T) * (j.K / 8) + kDxThreads - 1) / kDxThreads;
+    const long long steps = (static_cast<long long>(j.T) * (j.K / 4) + kDxThreads - 1) / kDxThreads;
     const int blocks = static_cast<int>(std::min<long long>(steps, 16ll * device_sm_count()));
     if (launch_kernel(head_dx_kernel, dim3(blocks), dim3(kDxThreads), 0, stream, j) != cudaSuccess) return SBN_ERR_CUDA;
     ++g_launch_count;
@@ -253,11 +284,13 @@ static sbn_status head_forward(const HeadCall& c, float* loss0, float* loss1, fl
     HeadLogitsParams p{};
     sbn_status st = launch_head_targets(c, w, &p.tg, stream);
     rows.tg = p.tg;
-    if (st == SBN_OK) st = launch_head_rows(c, w, rows, stream);
+    if (st == SBN_OK && !h.words) st = launch_head_rows(c, w, rows, stream);
     if (st != SBN_OK) return st;
     const bool list = c.top != 0, dual = list && c.labels;
-    p.count = reinterpret_cast<int*>(c.ws + w.count);
-    p.row_src = reinterpret_cast<int*>(c.ws + w.row_src);
+    if (!h.words) {
+        p.count = reinterpret_cast<int*>(c.ws + w.count);
+        p.row_src = reinterpret_cast<int*>(c.ws + w.row_src);
+    }
     p.T = c.T; p.N = c.N; p.K = c.K;
     p.v0 = 0; p.v1 = c.N; p.bn = h.bn;
     p.c0 = static_cast<float>(1.4426950408889634 / static_cast<double>(c.tau));
@@ -266,7 +299,9 @@ static sbn_status head_forward(const HeadCall& c, float* loss0, float* loss1, fl
     p.z_ev = reinterpret_cast<float*>(c.ws + w.z_ev);
     p.parts = h.parts;
     p.skip_loads = g_test_break_waits;
-    st = launch_head_logits<0>(maps, p, list, dual, stream);
+    const int tok_pad = static_cast<int>(head_up(c.T, 16));
+    st = h.words ? launch_head_words<0>(maps, HeadWordsParams{p, tok_pad, words_stages(tok_pad), nullptr, nullptr}, list, dual, stream)
+                 : launch_head_logits<0>(maps, p, list, dual, stream);
     if (st != SBN_OK) return st;
     return launch_head_losses(HeadLossJob{p.tg, p.count, p.row_src, c.T, c.N, p.part, p.part1, p.z_ev, h.parts, 1.0 / static_cast<double>(c.tau), loss0, loss1, lse0,
                                           lse1}, stream);
@@ -283,18 +318,22 @@ static sbn_status head_backward(const HeadCall& c, const float* lse0, const floa
     if (!head_encode(c, h, w, h.bn_piece, &maps)) return SBN_ERR_CUDA;
     bool ok = encode_3d_bf16_blocks(&gm.aw, c.ws + w.dz, h.piece, h.rows256, 2) && encode_2d_bf16_sw128(&gm.ax, c.ws + w.dz, h.piece, h.rows256, h.piece, 128);
     for (int half = 0; ok && half < 2; ++half)
-        ok = encode_3d_bf16_blocks(&gm.bx[half], c.x, k, t, half ? 1 : 2) && encode_3d_bf16_blocks(&gm.bxc[half], c.ws + w.xc, k, h.rows64, half ? 1 : 2);
-    if (!ok || !ensure_dynamic_smem<head_grads_kernel>(kPairLoopSmemBytes)) return SBN_ERR_CUDA;
+        ok = (h.words || encode_3d_bf16_blocks(&gm.bx[half], c.x, k, t, half ? 1 : 2)) && encode_3d_bf16_blocks(&gm.bxc[half], c.ws + w.xc, k, h.rows64, half ? 1 : 2);
+    ok = ok && (!dx || encode_3d_f32_out(&gm.acc, c.ws + w.acc, k, t, h.slots));
+    constexpr int grads_smem = pair_loop_smem_bytes<HeadGradsWork>();
+    if (!ok || !ensure_dynamic_smem<head_grads_kernel>(grads_smem)) return SBN_ERR_CUDA;
     HeadRowsJob rows{};
-    rows.row_of = reinterpret_cast<int*>(c.ws + w.row_of);
+    if (!h.words) rows.row_of = reinterpret_cast<int*>(c.ws + w.row_of);
     HeadLogitsParams p{};
     sbn_status st = launch_head_targets(c, w, &p.tg, stream);
     rows.tg = p.tg;
-    if (st == SBN_OK) st = launch_head_rows(c, w, rows, stream);
+    if (st == SBN_OK && !h.words) st = launch_head_rows(c, w, rows, stream);
     if (st != SBN_OK) return st;
     const bool list = c.top != 0, dual = list && c.labels;
-    p.count = reinterpret_cast<int*>(c.ws + w.count);
-    p.row_src = reinterpret_cast<int*>(c.ws + w.row_src);
+    if (!h.words) {
+        p.count = reinterpret_cast<int*>(c.ws + w.count);
+        p.row_src = reinterpret_cast<int*>(c.ws + w.row_src);
+    }
     p.T = c.T; p.N = c.N; p.K = c.K;
     p.bn = h.bn_piece;
     p.c0 = static_cast<float>(1.4426950408889634 / static_cast<double>(c.tau));
@@ -306,31 +345,32 @@ static sbn_status head_backward(const HeadCall& c, const float* lse0, const floa
     HeadGradParams q{};
     q.count = p.count;
     q.T = c.T; q.K = c.K;
-    q.acc = reinterpret_cast<float*>(c.ws + w.acc);
     q.slot_stages = h.slot_stages;
     q.skip_loads = g_test_break_waits;
-    const int tiles_k = (c.K + 255) / 256;
+    const int tiles_k = (c.K + 255) / 256, tok_pad = static_cast<int>(head_up(c.T, 16));
     for (int v0 = 0; v0 < c.N; v0 += h.piece) {
         const int cols = std::min(h.piece, c.N - v0);
         p.v0 = v0; p.v1 = v0 + cols;
-        st = launch_head_logits<1>(maps, p, list, dual, stream);
+        st = h.words ? launch_head_words<1>(maps, HeadWordsParams{p, tok_pad, words_stages(tok_pad), static_cast<const uint16_t*>(c.x), reinterpret_cast<uint16_t*>(c.ws + w.xc)},
+                                            list, dual, stream)
+                     : launch_head_logits<1>(maps, p, list, dual, stream);
         if (st != SBN_OK) return st;
         const char* w_rows = static_cast<const char*>(c.head) + static_cast<size_t>(v0) * c.K * 2;
         for (int half = 0; half < 2; ++half)
             if (!encode_3d_bf16_blocks(&gm.bw[half], w_rows, k, cols, half ? 1 : 2)) return SBN_ERR_CUDA;
         const int all_stages = (cols + 63) / 64;
         q.cols = cols;
-        q.dw = dhead ? static_cast<uint16_t*>(dhead) + static_cast<size_t>(v0) * c.K : nullptr;
+        if (dhead && !encode_2d_bf16_sw128(&gm.dw, static_cast<uint16_t*>(dhead) + static_cast<size_t>(v0) * c.K, k, cols, k, 128)) return SBN_ERR_CUDA;
         q.add = v0 > 0;
         const int slices = (all_stages + h.slot_stages - 1) / h.slot_stages;     // fewer in a short last piece
         const int tiles[2] = {dhead ? (cols + 255) / 256 * tiles_k : 0, dx ? static_cast<int>(h.rows256 / 256) * tiles_k * slices : 0};
         const int stages[2] = {(c.T + 63) / 64, h.slot_stages};
         q.plan = plan_backward(tiles, stages, -1);
-        if (launch_kernel(head_grads_kernel, dim3(2 * kBackwardPairs), dim3(kPairLoopThreads), kPairLoopSmemBytes, stream, gm, q) != cudaSuccess)
+        if (launch_kernel(head_grads_kernel, dim3(2 * kBackwardPairs), dim3(kPairLoopThreads), grads_smem, stream, gm, q) != cudaSuccess)
             return SBN_ERR_CUDA;
         ++g_launch_count;
     }
-    return dx ? launch_head_dx(HeadDxJob{rows.row_of, q.acc, h.slots, c.T, c.K, static_cast<uint16_t*>(dx)}, stream) : SBN_OK;
+    return dx ? launch_head_dx(HeadDxJob{rows.row_of, reinterpret_cast<const float*>(c.ws + w.acc), h.slots, c.T, c.K, static_cast<uint16_t*>(dx)}, stream) : SBN_OK;
 }
 
 }  // namespace sbn

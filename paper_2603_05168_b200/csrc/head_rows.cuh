@@ -308,25 +308,25 @@ __global__ void __launch_bounds__(kDxThreads)
 head_dx_kernel(const HeadDxJob j) {
     pdl_launch_dependents();
     pdl_wait();
-    const int vecs = j.K >> 3;                    // 8 values per thread and step
+    const int vecs = j.K >> 2;                    // 4 values per thread and step
     const long long all = static_cast<long long>(j.T) * vecs;
     const size_t slot = static_cast<size_t>(j.T) * j.K;
     for (long long i = static_cast<long long>(blockIdx.x) * kDxThreads + threadIdx.x; i < all; i += static_cast<long long>(gridDim.x) * kDxThreads) {
         const int t = static_cast<int>(i / vecs), c = static_cast<int>(i - static_cast<long long>(t) * vecs);
         const int r = j.row_of != nullptr ? j.row_of[t] : t;
-        float v[8] = {};
+        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         if (r >= 0) {
-            const float* a = j.acc + static_cast<size_t>(r) * j.K + 8 * c;
-            for (int s = 0; s < j.slots; ++s, a += slot) {
-                const float4 lo = *reinterpret_cast<const float4*>(a), hi = *reinterpret_cast<const float4*>(a + 4);
-                v[0] += lo.x; v[1] += lo.y; v[2] += lo.z; v[3] += lo.w;
-                v[4] += hi.x; v[5] += hi.y; v[6] += hi.z; v[7] += hi.w;
+            const float* a = j.acc + static_cast<size_t>(r) * j.K + 4 * c;
+#pragma unroll 8
+            for (int s = 0; s < j.slots; ++s) {
+                const float4 o = *reinterpret_cast<const float4*>(a + s * slot);
+                v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
             }
         }
-        uint32_t o[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[q]) : "f"(v[2 * q + 1]), "f"(v[2 * q]));
-        *reinterpret_cast<uint4*>(j.dx + static_cast<size_t>(t) * j.K + 8 * c) = make_uint4(o[0], o[1], o[2], o[3]);
+        uint2 o;
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o.x) : "f"(v.y), "f"(v.x));
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o.y) : "f"(v.w), "f"(v.z));
+        *reinterpret_cast<uint2*>(j.dx + static_cast<size_t>(t) * j.K + 4 * c) = o;
     }
 }
 

@@ -131,8 +131,16 @@ def test_few_tokens(T, N, K, top):
     check(make(T, N, K, seed=T + N + K, top=top))
 
 
+# up to 256 tokens words are on the lanes: token groups of 16 and 32, tiles of 128 words, more tiles than SMs
+@pytest.mark.parametrize("top", [0, 11])
+@pytest.mark.parametrize("T,N,K", [(17, 129, 128), (32, 20001, 256), (47, 1000, 2560), (49, 19007, 384), (96, 128, 1024), (161, 5000, 128), (192, 301, 4224),
+                                   (250, 38500, 128), (256, 2049, 640), (257, 2049, 640)])
+def test_words_on_the_lanes(T, N, K, top):
+    check(make(T, N, K, seed=T + N + K, top=top))
+
+
 # the vocabulary in several pieces, the last one short; dx from several slices of each piece, from one, and from half tiles
-@pytest.mark.parametrize("T,N,K", [(3, 12007, 4096), (200, 11009, 4096), (400, 24001, 2048), (5000, 30011, 256)])
+@pytest.mark.parametrize("T,N,K", [(3, 12007, 4096), (200, 11009, 4096), (400, 24001, 2048), (5000, 30011, 256), (2100, 70001, 128)])
 def test_cross_entropy_in_pieces(T, N, K):
     c = make(T, N, K, seed=T + K)
     assert b.sbn_head_workspace_bytes(T, N, K, backward=True) < 2 * T * N + 10 * T * K * 4 + (160 << 20)
@@ -238,8 +246,9 @@ def test_distill(T, N, K, top, dtype, tau, labels):
     check(c)
 
 
-def test_distill_in_pieces():
-    c = make(260, 24001, 2048, seed=29, top=40)
+@pytest.mark.parametrize("T,N,K,top", [(260, 24001, 2048, 40), (3000, 50021, 128, 12)])
+def test_distill_in_pieces(T, N, K, top):
+    c = make(T, N, K, seed=29, top=top)
     c["tau"] = 2.0
     check(c)
 
