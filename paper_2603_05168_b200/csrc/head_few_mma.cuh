@@ -32,7 +32,8 @@ struct HeadFewParams {
     float2* part;                 // stats: [T][parts], parts = CTAs
     float* part1;
     float* z_ev;                  // [T][events]
-    const float *lse0, *lse1, *g0, *g1;
+    const float *lse0, *lse1;
+    HeadScale scale;
     uint16_t* dz;                 // grad: [T][ldz]
     int ldz;
     // gradients
@@ -111,13 +112,16 @@ head_few_kernel(const HeadFewParams p) {
     float l0 = -INFINITY, l1 = -INFINITY, g0 = 0.0f, g1 = 0.0f;
     if constexpr (MODE == 1) {
         if (!LIST && blockIdx.x == 0 && mine) report_bad(flags);
+        const float unit = head_scale_unit(warp_max(lane < p.T ? head_scale_share(p.scale, p.tg, lane, p.N) : 0.0f));
+        const float inv_scale = 1.0f / unit;
+        if (blockIdx.x == 0 && tid == 0) p.scale.out[0] = unit;
         if (LIST ? (flags & kRowDistill) != 0 : asked) {
             l0 = -p.lse0[tok] * kLog2e;
-            g0 = p.g0[tok] * p.inv_tau;
+            g0 = p.scale.g0[tok] * p.inv_tau * inv_scale;
         }
         if (DUAL && (flags & kRowLabel)) {
             l1 = -p.lse1[tok] * kLog2e;
-            g1 = p.g1[tok];
+            g1 = p.scale.g1[tok] * inv_scale;
         }
     }
 
@@ -240,6 +244,7 @@ head_few_grads_kernel(const HeadFewParams p) {
             xt[kb][3][nt] = transpose_8x8(v.w);
         }
     }
+    const float scale = p.scale.out[0];
     float acc[2][2][NT][4] = {};
     uint4 w[kDepth][2][2];
     uint32_t dz[kDepth][NT][2];
@@ -302,8 +307,8 @@ head_few_grads_kernel(const HeadFewParams p) {
                         float d[4] = {};
                         if constexpr (NT == 1) mma_bf16_k8(d, a[0][0], a[0][1], xt[kb][j][0]);
                         else mma_bf16_k16(d, a[0][0], a[0][1], a[NT - 1][0], a[NT - 1][1], xt[kb][j][0], xt[kb][j][NT - 1]);
-                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[0][j]) : "f"(d[1]), "f"(d[0]));
-                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[1][j]) : "f"(d[3]), "f"(d[2]));
+                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[0][j]) : "f"(d[1] * scale), "f"(d[0] * scale));
+                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[1][j]) : "f"(d[3] * scale), "f"(d[2] * scale));
                     }
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {

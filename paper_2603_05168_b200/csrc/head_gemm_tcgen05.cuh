@@ -9,7 +9,9 @@
 //                               count, bf16 out), and the piece's part of dx, added up in fp32
 //
 // Tokens are on the lanes of tensor memory, so an epilogue thread owns a token's row of the tile: its maximum, its sum and its
-// targets need no exchange.  dz is rounded to bf16 because the tensor cores' operands are; sums are in fp32 throughout.
+// targets need no exchange.  dz is rounded to bf16 because the tensor cores' operands are; sums are in fp32 throughout.  It is
+// kept in units of the largest gradient of a loss (head_scale): with the mean's 1 / count everywhere, a target's p - 1 would
+// else be rounded at an unlucky place of the binade in every row alike.
 // Forward 2 T N K operations, a training step four times that (z is computed twice, it costs less than keeping it).
 #pragma once
 
@@ -36,9 +38,31 @@ __device__ __forceinline__ void tma_add_3d(const CUtensorMap* map, int c0, int c
                  ::"l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(src) : "memory");
 }
 
+// 32 rows x 64 bytes of a warp (lane = row) through kWarpBoxBytes of shared memory of its own: the 16-byte pieces q of a row at
+// q ^ (row / 2 % 4), as the 64-byte swizzle has them; store() issues the TMA store.  Waits for the box's last store first.
+constexpr int kWarpBoxBytes = 2048;
+template <class Store>
+__device__ __forceinline__ void store_warp_box(uint32_t box, int lane, const uint32_t (&v)[16], Store&& store) {
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+    __syncwarp();
+    const uint32_t to = box + static_cast<uint32_t>(lane * 64), x = static_cast<uint32_t>(lane >> 1) & 3u;
+#pragma unroll
+    for (uint32_t q = 0; q < 4; ++q) st_shared_16(to + ((q ^ x) << 4), v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0) {
+        store();
+        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    }
+}
+__device__ __forceinline__ void tmem_ld_32x32b_x1(uint32_t taddr, uint32_t& r) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(r) : "r"(taddr) : "memory");
+}
+
 struct HeadMaps {
     CUtensorMap x, xc;            // K-major: the tokens' rows, or the rows that count moved together
     CUtensorMap w;                // K-major, BN / 2 rows per box
+    CUtensorMap dz;               // grad: [T up to a multiple of 256][columns of a piece], stored in boxes of 32 rows x 64 bytes
 };
 struct HeadLogitsParams {
     HeadTargets tg;
@@ -57,8 +81,7 @@ struct HeadLogitsParams {
     const float *lse0, *lse1;     // per token
     const float *g0, *g1;         // gradients of the two losses per token (g1: label beside a teacher)
     float inv_tau;
-    uint16_t* dz;                 // [T up to a multiple of 256][ldz]
-    int ldz;
+    const float* scale;           // see HeadScale
     int skip_loads;
 };
 
@@ -77,7 +100,7 @@ struct HeadRow {
     static constexpr float kLog2e = 1.4426950408889634f;
 
     // Row r with token t; `asked` says whether anything is asked of it.
-    __device__ void begin(const HeadLogitsParams& p, int row, int token, bool asked) {
+    __device__ void begin(const HeadLogitsParams& p, int row, int token, bool asked, float inv_scale = 1.0f) {
         r = row;
         t = token;
         here = asked;
@@ -90,19 +113,21 @@ struct HeadRow {
             const int flags = LIST ? p.tg.flags[t] : kRowDistill;
             if (flags & kRowDistill) {
                 l0 = -p.lse0[t] * kLog2e;
-                g0 = p.g0[t] * p.inv_tau;
+                g0 = p.g0[t] * p.inv_tau * inv_scale;
             }
             if (DUAL && (flags & kRowLabel)) {
                 l1 = -p.lse1[t] * kLog2e;
-                g1 = p.g1[t];
+                g1 = p.g1[t] * inv_scale;
             }
         }
     }
     __device__ const int* list(const HeadLogitsParams& p) const { return p.tg.ev_col + static_cast<size_t>(t) * p.tg.events; }
-    // To the first target at or behind column n.
+    // To the first target at or behind column n.  Of the logits themselves only the teacher's entries are wanted (stats): the
+    // label's logit is a product of its own (head_losses_kernel).
+    static constexpr bool kTargets = LIST || MODE == 1;
     __device__ void seek(const HeadLogitsParams& p, int n) {
         next_col = kNoColumn;
-        if (!here) return;
+        if (!kTargets || !here) return;
         if constexpr (LIST) {
             const int* col = list(p);
             int lo = 0, hi = p.tg.events;
@@ -126,34 +151,45 @@ struct HeadRow {
         }
     }
 
+    // Writes down the row's logits at its targets among columns n .. n + 31; at(q) gives every lane of the warp its logit of column
+    // n + q.  The whole warp takes part (picking a register by an index of the lane's own would put all 32 into local memory:
+    // 1 us per 32 columns).  A row has a handful of targets in the whole vocabulary.
+    template <class At>
+    __device__ void note_targets(const HeadLogitsParams& p, int n, At&& at) {
+        if constexpr (LIST) {
+            while (next_col < n) step(p);
+            for (uint32_t who; (who = __ballot_sync(0xFFFFFFFFu, next_col < n + 32)) != 0u;) {
+                const int q = __shfl_sync(0xFFFFFFFFu, next_col - n, __ffs(who) - 1);
+                const float v = at(q);
+                if (next_col - n == q) {
+                    p.z_ev[static_cast<size_t>(r) * p.tg.events + e] = v;
+                    step(p);
+                }
+            }
+        }
+    }
     // Columns n .. n + 31.
     __device__ void stats(const HeadLogitsParams& p, uint32_t (&z)[32], int n) {
-        while (next_col < n) step(p);
-        while (next_col < n + 32) {                    // rare: a row has a handful of targets in the whole vocabulary
-            float v = 0.0f;
-#pragma unroll
-            for (int q = 0; q < 32; ++q) v = next_col - n == q ? __uint_as_float(z[q]) : v;
-            p.z_ev[static_cast<size_t>(r) * p.tg.events + (LIST ? e : 0)] = v;
-            step(p);
-        }
         if (n >= p.N) return;
         if (n + 32 > p.N) {                            // behind the vocabulary: nothing
 #pragma unroll
             for (int q = 0; q < 32; ++q) z[q] = n + q < p.N ? z[q] : 0xFF800000u;
         }
-        float mc = __uint_as_float(z[0]);
+        float mc[4] = {m, m, m, m};                    // four chains: a chain of 32 would wait for itself
 #pragma unroll
-        for (int q = 1; q < 32; ++q) mc = fmaxf(mc, __uint_as_float(z[q]));
-        const float m_new = fmaxf(m, mc);
-        s0 *= ex2_approx((m - m_new) * p.c0);
-        if (DUAL) s1 *= ex2_approx((m - m_new) * kLog2e);
+        for (int q = 0; q < 32; ++q) mc[q & 3] = fmaxf(mc[q & 3], __uint_as_float(z[q]));
+        const float m_new = fmaxf(fmaxf(mc[0], mc[1]), fmaxf(mc[2], mc[3]));
+        float a0[4] = {s0 * ex2_approx((m - m_new) * p.c0), 0.0f, 0.0f, 0.0f}, a1[4] = {};
+        if (DUAL) a1[0] = s1 * ex2_approx((m - m_new) * kLog2e);
         m = m_new;
 #pragma unroll
         for (int q = 0; q < 32; ++q) {
             const float d = __uint_as_float(z[q]) - m;      // the difference first: exact where it matters
-            s0 += ex2_approx(d * p.c0);
-            if (DUAL) s1 += ex2_approx(d * kLog2e);
+            a0[q & 3] += ex2_approx(d * p.c0);
+            if (DUAL) a1[q & 3] += ex2_approx(d * kLog2e);
         }
+        s0 = (a0[0] + a0[1]) + (a0[2] + a0[3]);
+        if (DUAL) s1 = (a1[0] + a1[1]) + (a1[2] + a1[3]);
     }
     __device__ void store_part(const HeadLogitsParams& p, int part) const {
         const size_t at = static_cast<size_t>(r) * p.parts + part;
@@ -161,8 +197,8 @@ struct HeadRow {
         if (DUAL) p.part1[at] = s1;
     }
 
-    // Columns n .. n + 31 of dz, zeros in rows that nothing is asked of and behind the vocabulary.
-    __device__ void grad(const HeadLogitsParams& p, const uint32_t (&z)[32], int n) {
+    // Columns n .. n + 31 of dz in bf16, zeros in rows that nothing is asked of and behind the vocabulary.
+    __device__ void grad(const HeadLogitsParams& p, const uint32_t (&z)[32], int n, uint32_t (&o)[16]) {
         while (next_col < n) step(p);
         float v[32];
 #pragma unroll
@@ -180,29 +216,29 @@ struct HeadRow {
             for (int q = 0; q < 32; ++q) v[q] -= next_col - n == q ? off : 0.0f;
             step(p);
         }
-        uint32_t o[16];
+        if (!here || n + 32 > p.N) {
 #pragma unroll
-        for (int q = 0; q < 16; ++q) {
-            const bool in0 = here && n + 2 * q < p.N, in1 = here && n + 2 * q + 1 < p.N;
-            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[q]) : "f"(in1 ? v[2 * q + 1] : 0.0f), "f"(in0 ? v[2 * q] : 0.0f));
+            for (int q = 0; q < 32; ++q) v[q] = here && n + q < p.N ? v[q] : 0.0f;
         }
-        uint4* to = reinterpret_cast<uint4*>(p.dz + static_cast<size_t>(r) * p.ldz + (n - p.v0));
 #pragma unroll
-        for (int q = 0; q < 4; ++q) to[q] = make_uint4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
+        for (int q = 0; q < 16; ++q) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[q]) : "f"(v[2 * q + 1]), "f"(v[2 * q]));
     }
 };
 
-template <int MODE, bool LIST, bool DUAL>
+template <int MODE, bool LIST, bool DUAL, bool WIDE>
 struct HeadLogitsWork {
-    static constexpr int kStages = 7, kStagingBytes = 0;
+    static constexpr bool kWide = WIDE;
+    static constexpr int kStages = WIDE ? 4 : (MODE == 0 ? 7 : 6), kStagingBytes = MODE == 0 ? 0 : (WIDE ? 16 : 8) * kWarpBoxBytes;
     const HeadMaps& maps;
     const HeadLogitsParams& p;
     int rows, tiles_m, tiles_v;
+    float inv_scale;
     bool moved;
 
     __device__ HeadLogitsWork(const HeadMaps& m, const HeadLogitsParams& q) : maps(m), p(q) {}
     __device__ void start() {
         rows = *p.count;
+        inv_scale = MODE == 1 ? p.scale[1] : 1.0f;
         moved = rows < p.T;
         tiles_m = (max(rows, 1) + 255) / 256;              // no row counts: one tile of zeros, which dW then contracts over
         tiles_v = (p.v1 - p.v0 + p.bn - 1) / p.bn;
@@ -233,7 +269,7 @@ struct HeadLogitsWork {
         tma_load_2d_pair(st, moved ? &maps.xc : &maps.x, ks * 64, t.m0 + static_cast<int>(rank) * 128, bar);
         tma_load_2d_pair(st + kPairLoopStageA, &maps.w, ks * 64, t.n0 + static_cast<int>(rank) * (t.bn >> 1), bar);
     }
-    __device__ uint32_t idesc(const Tile& t) const { return make_idesc_bf16_any(256, t.bn, false, false); }
+    __device__ uint32_t idesc(const Tile& t) const { return make_idesc_bf16_any(256, WIDE ? 256 : t.bn, false, false); }
     __device__ uint64_t a_step(const Tile&) const { return 32 >> 4; }
     __device__ uint64_t b_step(const Tile&) const { return 32 >> 4; }
     __device__ uint64_t a_desc(const Tile&, uint32_t s) const { return make_smem_desc(s, 16, 1024, kSwz128); }
@@ -241,15 +277,19 @@ struct HeadLogitsWork {
 
     struct Epilogue {
         const HeadLogitsWork& w;
-        int rank, quarter, parity, lane;
+        int rank, quarter, sub, lane;
+        uint32_t box;
         HeadRow<MODE, LIST, DUAL> row;
 
-        __device__ Epilogue(const HeadLogitsWork& work, int rk, int q, int par, int ln, uint32_t) : w(work), rank(rk), quarter(q), parity(par), lane(ln) {}
+        __device__ Epilogue(const HeadLogitsWork& work, int rk, int q, int sb, int ln, uint32_t staging)
+            : w(work), rank(rk), quarter(q), sub(sb), lane(ln), box(staging + static_cast<uint32_t>((sb * 4 + q) * kWarpBoxBytes)) {}
+        // wide: the tile's column that this warp's 128 begin with
+        __device__ int first_col(const Tile& tile) const { return tile.n0 + (WIDE ? 128 * (sub >> 1) + 256 * (sub & 1) : 0); }
         __device__ void begin(const Tile& tile) {
             const int r = tile.m0 + rank * 128 + quarter * 32 + lane;
             const bool here = r < w.rows;
-            row.begin(w.p, r, here ? w.p.row_src[r] : 0, here);
-            row.seek(w.p, tile.n0);
+            row.begin(w.p, r, here ? w.p.row_src[r] : 0, here, w.inv_scale);
+            row.seek(w.p, first_col(tile));
         }
         template <class Release>
         __device__ void run(const Tile& tile, uint32_t taddr, Release&& release) {
@@ -260,41 +300,60 @@ struct HeadLogitsWork {
                 release();
                 return;
             }
+            const int from = WIDE ? 0 : sub, to = WIDE ? 4 : chunks, step = WIDE ? 1 : 2;
+            if (WIDE) taddr += static_cast<uint32_t>(128 * sub);
+            const int n0 = first_col(tile);
 #pragma unroll 1
-            for (int c = parity; c < chunks; c += 2) {
+            for (int c = from; c < to; c += step) {
                 uint32_t z[32];
                 __syncwarp();                              // the lanes may have parted over their targets
                 tmem_ld_32x32b_x32(taddr + static_cast<uint32_t>(c * 32), z);
                 tmem_ld_wait();
-                if (c + 2 >= chunks) release();
-                if constexpr (MODE == 0) row.stats(w.p, z, tile.n0 + c * 32);
-                else row.grad(w.p, z, tile.n0 + c * 32);
+                const int n = n0 + c * 32;
+                if constexpr (MODE == 0)
+                    row.note_targets(w.p, n, [&](int q) {
+                        uint32_t v;
+                        tmem_ld_32x32b_x1(taddr + static_cast<uint32_t>(c * 32 + q), v);
+                        tmem_ld_wait();
+                        return __uint_as_float(v);
+                    });
+                if (c + step >= to) release();
+                if constexpr (MODE == 0) {
+                    row.stats(w.p, z, n);
+                } else {
+                    uint32_t o[16];
+                    row.grad(w.p, z, n, o);
+                    store_warp_box(box, lane, o, [&] { tma_store_2d(&w.maps.dz, n - w.p.v0, first_row, box); });
+                }
             }
-            if (MODE == 0 && row.here) row.store_part(w.p, 2 * ((tile.n0 - w.p.v0) / tile.bn) + parity);
+            if (MODE == 0 && row.here) row.store_part(w.p, (WIDE ? 4 : 2) * ((tile.n0 - w.p.v0) / tile.bn) + sub);
         }
-        __device__ void finish() {}
+        __device__ void finish() {
+            if (MODE == 1 && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        }
     };
 };
 
-template <int MODE, bool LIST, bool DUAL>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairLoopThreads, 1)
+template <int MODE, bool LIST, bool DUAL, bool WIDE>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(WIDE ? 576 : 320, 1)
 head_logits_kernel(const __grid_constant__ HeadMaps maps, const __grid_constant__ HeadLogitsParams p) {
     pdl_launch_dependents();
-    HeadLogitsWork<MODE, LIST, DUAL> work(maps, p);
+    HeadLogitsWork<MODE, LIST, DUAL, WIDE> work(maps, p);
     bf16_pair_loop(work, p.skip_loads != 0);
 }
 
 // ---- gradients of a piece --------------------------------------------------------------------------
-// dw, acc: how results leave, in boxes of 128 rows x 128 bytes.
+// dw, acc: how results leave, in boxes of 128 rows x 128 bytes (wide tiles: 32 rows x 64 bytes).
 struct HeadGradMaps {
     CUtensorMap aw;               // dz piece for dW: MN-major, two blocks of 64 columns
     CUtensorMap ax;               // dz piece for dx: K-major
-    CUtensorMap bx[2], bxc[2];    // x, or the rows that count moved together: MN-major, two blocks, one block (half tiles)
+    CUtensorMap bx[2], bxc[2];    // x, or the rows that count moved together: MN-major, whole and half tiles
     CUtensorMap bw[2];            // the piece's rows of W
     CUtensorMap dw;               // [cols][K] bf16
     CUtensorMap acc;              // [slots][T][K] fp32
 };
 struct HeadGradParams {
+    const float* scale;           // dW leaves times this (HeadScale)
     const int* count;             // null: all rows, zeros in place of those left out (`moved` rows)
     int T, K;
     int cols;                     // vocabulary rows of the piece
@@ -304,16 +363,20 @@ struct HeadGradParams {
     int skip_loads;
 };
 
+template <bool WIDE>
 struct HeadGradsWork {
-    static constexpr int kStages = 6, kStagingBytes = 2 * 128 * 128;
+    static constexpr bool kWide = WIDE;
+    static constexpr int kStages = WIDE ? 4 : 6, kStagingBytes = 2 * 128 * 128, kTileCols = WIDE ? 512 : 256;
     const HeadGradMaps& maps;
     const HeadGradParams& p;
     int rows;
+    float scale;
     bool moved;
 
     __device__ HeadGradsWork(const HeadGradMaps& m, const HeadGradParams& q) : maps(m), p(q) {}
     __device__ void start() {
         rows = p.count != nullptr ? *p.count : p.T;
+        scale = *p.scale;
         moved = p.count == nullptr || rows < p.T;
     }
 
@@ -329,7 +392,7 @@ struct HeadGradsWork {
                 while (i < sg.count(pair)) {
                     const int u = sg.index(pair, i++);
                     t.part = sg.part;
-                    t.bn = sg.half ? 128 : 256;
+                    t.bn = sg.half ? kTileCols / 2 : kTileCols;
                     const int tiles_m = ((t.part == 0 ? p.cols : p.T) + 255) / 256;
                     int tile = sg.half ? sg.first_tile + (u >> 1) : u;
                     t.slot = 0;
@@ -337,14 +400,14 @@ struct HeadGradsWork {
                     if (t.part == 0) {
                         t.k_stages = (max(w.rows, 1) + 63) / 64;
                     } else {
-                        const int tiles = tiles_m * ((p.K + 255) / 256);
+                        const int tiles = tiles_m * ((p.K + kTileCols - 1) / kTileCols);
                         t.slot = tile / tiles;
                         tile -= t.slot * tiles;
                         t.k_first = t.slot * p.slot_stages;
                         t.k_stages = min(p.slot_stages, (p.cols + 63) / 64 - t.k_first);
                     }
                     t.m0 = (tile % tiles_m) * 256;
-                    t.n0 = (tile / tiles_m) * 256 + (sg.half ? (u & 1) * 128 : 0);
+                    t.n0 = (tile / tiles_m) * kTileCols + (sg.half ? (u & 1) * (kTileCols / 2) : 0);
                     if (t.part == 1 && t.m0 >= w.rows) continue;            // rows left out
                     return true;
                 }
@@ -355,32 +418,80 @@ struct HeadGradsWork {
 
     __device__ void load(const Tile& t, int ks, uint32_t rank, uint32_t st, uint32_t bar) const {
         const int m0 = t.m0 + static_cast<int>(rank) * 128, n0 = t.n0 + static_cast<int>(rank) * (t.bn >> 1);
-        const int half = t.bn == 128, k = (t.k_first + ks) * 64;
+        const int half = t.bn < kTileCols, k = (t.k_first + ks) * 64;
         if (t.part == 0) tma_load_3d_pair(st, &maps.aw, 0, k, m0 >> 6, bar);
         else tma_load_2d_pair(st, &maps.ax, k, m0, bar);
         const CUtensorMap* b = t.part == 1 ? &maps.bw[half] : (moved ? &maps.bxc[half] : &maps.bx[half]);
         tma_load_3d_pair(st + kPairLoopStageA, b, 0, k, n0 >> 6, bar);
     }
     // K = 16 elements per instruction: 16 rows of an MN-major operand, 32 B along a row of a K-major one
-    __device__ uint32_t idesc(const Tile& t) const { return make_idesc_bf16_any(256, t.bn, t.part == 0, true); }
+    __device__ uint32_t idesc(const Tile& t) const { return make_idesc_bf16_any(256, WIDE ? 256 : t.bn, t.part == 0, true); }
     __device__ uint64_t a_step(const Tile& t) const { return t.part == 0 ? (2048 >> 4) : (32 >> 4); }
     __device__ uint64_t b_step(const Tile&) const { return 2048 >> 4; }
     __device__ uint64_t a_desc(const Tile& t, uint32_t s) const { return make_smem_desc(s, t.part == 0 ? 8192 : 16, 1024, kSwz128); }
     __device__ uint64_t b_desc(const Tile&, uint32_t s) const { return make_smem_desc(s, 8192, 1024, kSwz128); }
 
-    // 64 columns of the tile at a time: every warp puts its 32 rows x 32 columns into shared memory (the 128-byte swizzle keeps the
-    // rows' 16-byte pieces on different banks), and one thread stores 128 rows x 128 bytes by TMA, which also clips what lies
-    // outside.  Stored by the threads themselves, a row each, every 16 bytes were a transaction of their own: 4 us per fp32 tile.
+    // Results go out through shared memory and TMA stores, which also clip what lies outside.  Stored by the threads themselves, a
+    // row each, every 16 bytes were a transaction of their own: 4 us per fp32 tile.
+    //   narrow  64 columns at a time: every warp puts its 32 rows x 32 columns into a buffer of the CTA (the 128-byte swizzle keeps the
+    //           rows' 16-byte pieces on different banks), one thread stores boxes of 128 rows x 128 bytes
+    //   wide    every warp has 2 KB of its own and stores boxes of 32 rows x 64 bytes (64-byte swizzle): nothing to wait for but itself
     struct Epilogue {
         const HeadGradsWork& w;
-        int rank, quarter, parity, lane;
+        int rank, quarter, parity, lane;                    // parity: `sub` of the loop
         uint32_t staging;
-        __device__ Epilogue(const HeadGradsWork& work, int rk, int q, int par, int ln, uint32_t st) : w(work), rank(rk), quarter(q), parity(par), lane(ln), staging(st) {}
+        __device__ Epilogue(const HeadGradsWork& work, int rk, int q, int sub, int ln, uint32_t st)
+            : w(work), rank(rk), quarter(q), parity(sub), lane(ln), staging(st + (WIDE ? static_cast<uint32_t>((sub * 4 + q) * kWarpBoxBytes) : 0u)) {}
         __device__ void begin(const Tile&) {}
-        __device__ bool leader() const { return quarter == 0 && parity == 0 && lane == 0; }
+        __device__ bool leader() const { return (WIDE || (quarter == 0 && parity == 0)) && lane == 0; }
 
         template <class Release>
         __device__ void run(const Tile& t, uint32_t taddr, Release&& release) {
+            if constexpr (WIDE) run_wide(t, taddr, release);
+            else run_narrow(t, taddr, release);
+        }
+
+        template <class Release>
+        __device__ void run_wide(const Tile& t, uint32_t taddr, Release&& release) {
+            const HeadGradParams& p = w.p;
+            const int m = t.m0 + rank * 128 + quarter * 32;
+            const int n0 = t.n0 + (t.bn == 512 ? 128 * (parity >> 1) + 256 * (parity & 1) : 128 * parity);
+            if (m >= (t.part == 0 ? p.cols : w.rows) || n0 >= p.K || 128 * parity >= t.bn) {       // K % 128 == 0: the warp's columns are in or out as a whole
+                release();
+                return;
+            }
+#pragma unroll 1
+            for (int c = 0; c < 4; ++c) {
+                uint32_t v[32];
+                __syncwarp();
+                tmem_ld_32x32b_x32(taddr + static_cast<uint32_t>(128 * parity + c * 32), v);
+                tmem_ld_wait();
+                if (c == 3) release();
+                const int n = n0 + c * 32;
+                if (t.part == 0) {
+                    uint32_t o[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[i]) : "f"(__uint_as_float(v[2 * i + 1]) * w.scale), "f"(__uint_as_float(v[2 * i]) * w.scale));
+                    store_warp_box(staging, lane, o, [&] { tma_store_2d(&w.maps.dw, n, m, staging); });
+                } else {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        uint32_t o[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) o[i] = v[16 * h + i];
+                        // One tile of a launch adds to an element, and launches follow one another: the sum's order is fixed
+                        store_warp_box(staging, lane, o, [&] {
+                            if (p.add) tma_add_3d(&w.maps.acc, n + 16 * h, m, t.slot, staging);
+                            else tma_store_3d(&w.maps.acc, n + 16 * h, m, t.slot, staging);
+                        });
+                    }
+                }
+            }
+        }
+
+        template <class Release>
+        __device__ void run_narrow(const Tile& t, uint32_t taddr, Release&& release) {
             const HeadGradParams& p = w.p;
             const int m0 = t.m0 + rank * 128;
             const bool rows_in = m0 < (t.part == 0 ? p.cols : w.rows);
@@ -407,7 +518,7 @@ struct HeadGradsWork {
                         uint32_t o[4];
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[i]) : "f"(__uint_as_float(v[8 * q + 2 * i + 1])), "f"(__uint_as_float(v[8 * q + 2 * i])));
+                            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[i]) : "f"(__uint_as_float(v[8 * q + 2 * i + 1]) * w.scale), "f"(__uint_as_float(v[8 * q + 2 * i]) * w.scale));
                         st_shared_16(to + (((parity * 4 + q) ^ (row & 7)) << 4), o[0], o[1], o[2], o[3]);
                     }
                 } else {
@@ -438,10 +549,11 @@ struct HeadGradsWork {
     };
 };
 
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairLoopThreads, 1)
+template <bool WIDE>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(WIDE ? 576 : 320, 1)
 head_grads_kernel(const __grid_constant__ HeadGradMaps maps, const __grid_constant__ HeadGradParams p) {
     pdl_launch_dependents();
-    HeadGradsWork work(maps, p);
+    HeadGradsWork<WIDE> work(maps, p);
     bf16_pair_loop(work, p.skip_loads != 0);
 }
 

@@ -13,6 +13,7 @@ struct HeadPlan {
     int bn, parts;                // forward: columns per tile, partial sums per row
     int piece;                    // backward: columns of dz at a time (a multiple of 256)
     int bn_piece;                 // columns per tile of the pieces' logits
+    bool wide_grads;              // gradients in tiles of 512 columns, else 256
     int slots, slot_stages;       // slices of dx's contraction over a piece, and 64-column stages of each
     long long rows64, rows256;    // T up to a multiple
 };
@@ -20,14 +21,17 @@ struct HeadPlan {
 static inline long long head_up(long long v, long long to) { return (v + to - 1) / to * to; }
 
 // Columns per tile of z: as wide as possible (a wide tile reads its rows for more columns), narrower where the tiles would
-// not go round.  Time per stage in us: the MMAs of 256 columns take 0.36; a narrow tile's two loads 0.19.
+// not go round.  us per stage and per tile, as measured.
 static int head_tile_columns(int T, int cols, int K) {
+    static const struct { int bn; double stage, tile; } kShapes[] = {{512, 0.56, 2.5}, {256, 0.38, 1.0}, {128, 0.33, 1.0}, {64, 0.31, 1.0}};
+    if (g_force_token_tile < 0) return g_force_token_tile <= -512 ? 512 : (g_force_token_tile <= -256 ? 256 : (g_force_token_tile <= -128 ? 128 : 64));
     int best = 256;
     double best_cost = 1e300;
-    for (int bn = 256; bn >= 64; bn >>= 1) {
+    for (const auto& shape : kShapes) {
+        const int bn = shape.bn;
         const double tiles = static_cast<double>(head_up(T, 256) / 256) * ((cols + bn - 1) / bn);
         const double rounds = std::ceil(tiles / kBackwardPairs);
-        const double cost = rounds * (std::max(0.36 * bn / 256, 0.19) * (K / 64) + 1.0);
+        const double cost = rounds * (shape.stage * (K / 64) + shape.tile);
         if (cost < best_cost * 0.99) { best_cost = cost; best = bn; }
     }
     return best;
@@ -50,13 +54,26 @@ static HeadPlan head_plan(int T, int N, int K) {
     h.rows256 = head_up(T, 256);
     h.words = T <= kWordsTokens;
     h.bn = head_tile_columns(T, N, K);
-    h.parts = h.words ? 4 * std::min((N + 127) / 128, kNumSMs) : 2 * ((N + h.bn - 1) / h.bn);
+    h.parts = h.words ? 4 * std::min((N + 127) / 128, kNumSMs) : (h.bn == 512 ? 4 : 2) * ((N + h.bn - 1) / h.bn);
     long long cols = (128ll << 20) / (2 * h.rows256);
-    cols = std::max(1024ll, cols / 256 * 256);
+    cols = std::max(1024ll, cols / 512 * 512);
     const long long pieces = (N + cols - 1) / cols;
-    h.piece = static_cast<int>(head_up((N + pieces - 1) / pieces, 256));
+    h.piece = static_cast<int>(head_up((N + pieces - 1) / pieces, 512));
     h.bn_piece = head_tile_columns(T, std::min(N, h.piece), K);
-    const int dx_tiles = static_cast<int>(h.rows256 / 256) * ((K + 255) / 256);
+    // gradients in wide tiles where those of dx and dW go round more than once (dW's are short: their number counts by length)
+    {
+        const double rows = static_cast<double>(h.rows256 / 256), words = (std::min(N, h.piece) + 255) / 256;
+        auto cost = [&](int cols_per_tile, double stage, double tile) {
+            const double across = (K + cols_per_tile - 1) / cols_per_tile;
+            const double dx = std::ceil(rows * across / kBackwardPairs) * (stage * 4 * words + tile);
+            const double all = (rows * across * (stage * 4 * words + tile) + words * across * (stage * 4 * rows + tile)) / kBackwardPairs;
+            return std::max(dx, all);
+        };
+        h.wide_grads = rows >= 4 && cost(512, 0.56, 2.0) < cost(256, 0.40, 0.5);
+        if (g_force_token_tile < 0) h.wide_grads = g_force_token_tile <= -512;
+    }
+    const int tile_cols = h.wide_grads ? 512 : 256;
+    const int dx_tiles = static_cast<int>(h.rows256 / 256) * ((K + tile_cols - 1) / tile_cols);
     const int stages = (std::min(h.piece, N) + 63) / 64, slots = std::max(1, std::min((kBackwardPairs + dx_tiles / 2) / dx_tiles, stages));
     h.slot_stages = (stages + slots - 1) / slots;
     h.slots = (stages + h.slot_stages - 1) / h.slot_stages;             // all of them are written by the first piece
@@ -65,13 +82,14 @@ static HeadPlan head_plan(int T, int N, int K) {
 
 // Workspace of a call, in bytes from its start.
 struct HeadWs {
-    size_t count, row_src, row_of, flags, ev_col, ev_w, xc, z_ev, part, part1, dz, acc, total;
+    size_t count, scale, row_src, row_of, flags, ev_col, ev_w, xc, z_ev, part, part1, dz, acc, total;
 };
 static HeadWs head_ws_layout(const HeadPlan& h, bool backward, int T, int K, int top) {
     HeadWs w{};
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) & ~static_cast<size_t>(255); return here; };
     const size_t t = static_cast<size_t>(T), events = top ? static_cast<size_t>(top) + 1 : 1;
+    if (backward) w.scale = take(8);
     if (!h.few && !h.words) {
         w.count = take(4);
         w.row_src = take(4 * t);
@@ -95,16 +113,23 @@ static HeadWs head_ws_layout(const HeadPlan& h, bool backward, int T, int K, int
     return w;
 }
 
-// Sums of dx, fp32 [slots][rows][cols], written in boxes of 128 rows x 128 bytes with the 128-byte swizzle in shared memory.
-static bool encode_3d_f32_out(CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, uint64_t slots) {
+// Results leave in boxes of 128 rows x 128 bytes with the 128-byte swizzle in shared memory, or (wide tiles) 32 rows x 64 bytes with
+// the 64-byte swizzle: dW, bf16 [rows][cols], and the sums of dx, fp32 [slots][rows][cols].
+static bool encode_out(CUtensorMap* map, const void* base, bool bf16, uint64_t cols, uint64_t rows, uint64_t slots, bool wide) {
     EncodeTiledFn fn = get_encode_fn();
     if (!fn) return false;
+    const uint64_t es = bf16 ? 2 : 4;
     cuuint64_t dims[3] = {cols, rows, slots};
-    cuuint64_t strides[2] = {cols * 4, cols * 4 * rows};
-    cuuint32_t box[3] = {32, 128, 1};
+    cuuint64_t strides[2] = {cols * es, cols * es * rows};
+    cuuint32_t box[3] = {static_cast<cuuint32_t>((wide ? 64 : 128) / es), wide ? 32u : 128u, 1};
     cuuint32_t estr[3] = {1, 1, 1};
-    return fn(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    return fn(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, bf16 ? 2 : 3, const_cast<void*>(base), dims, strides, box, estr,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, wide ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+static bool encode_2d_bf16_out(CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, bool wide) { return encode_out(map, base, true, cols, rows, 1, wide); }
+static bool encode_3d_f32_out(CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, uint64_t slots, bool wide) {
+    return encode_out(map, base, false, cols, rows, slots, wide);
 }
 
 // One call of either operator: top == 0 is the cross entropy.
@@ -129,21 +154,25 @@ static bool head_encode(const HeadCall& c, const HeadPlan& h, const HeadWs& w, i
            encode_2d_bf16_sw128(&maps->w, c.head, k, c.N, k, bn / 2);
 }
 
-template <int MODE, bool LIST, bool DUAL>
+template <int MODE, bool LIST, bool DUAL, bool WIDE>
 static sbn_status launch_head_logits_as(const HeadMaps& maps, const HeadLogitsParams& p, cudaStream_t stream) {
-    constexpr int smem = pair_loop_smem_bytes<HeadLogitsWork<MODE, LIST, DUAL>>();
-    if (!ensure_dynamic_smem<head_logits_kernel<MODE, LIST, DUAL>>(smem)) return SBN_ERR_CUDA;
+    using Loop = PairLoop<HeadLogitsWork<MODE, LIST, DUAL, WIDE>>;
+    if (!ensure_dynamic_smem<head_logits_kernel<MODE, LIST, DUAL, WIDE>>(Loop::kSmemBytes)) return SBN_ERR_CUDA;
     const long long tiles = head_up(p.T, 256) / 256 * ((p.v1 - p.v0 + p.bn - 1) / p.bn);
     const unsigned pairs = static_cast<unsigned>(std::min<long long>(tiles, kBackwardPairs));
-    if (launch_kernel(head_logits_kernel<MODE, LIST, DUAL>, dim3(2 * pairs), dim3(kPairLoopThreads), smem, stream, maps, p) != cudaSuccess)
+    if (launch_kernel(head_logits_kernel<MODE, LIST, DUAL, WIDE>, dim3(2 * pairs), dim3(Loop::kThreads), Loop::kSmemBytes, stream, maps, p) != cudaSuccess)
         return SBN_ERR_CUDA;
     ++g_launch_count;
     return SBN_OK;
 }
+template <int MODE, bool WIDE>
+static sbn_status launch_head_logits_of(const HeadMaps& maps, const HeadLogitsParams& p, bool list, bool dual, cudaStream_t stream) {
+    if (!list) return launch_head_logits_as<MODE, false, false, WIDE>(maps, p, stream);
+    return dual ? launch_head_logits_as<MODE, true, true, WIDE>(maps, p, stream) : launch_head_logits_as<MODE, true, false, WIDE>(maps, p, stream);
+}
 template <int MODE>
 static sbn_status launch_head_logits(const HeadMaps& maps, const HeadLogitsParams& p, bool list, bool dual, cudaStream_t stream) {
-    if (!list) return launch_head_logits_as<MODE, false, false>(maps, p, stream);
-    return dual ? launch_head_logits_as<MODE, true, true>(maps, p, stream) : launch_head_logits_as<MODE, true, false>(maps, p, stream);
+    return p.bn == 512 ? launch_head_logits_of<MODE, true>(maps, p, list, dual, stream) : launch_head_logits_of<MODE, false>(maps, p, list, dual, stream);
 }
 
 template <int MODE, bool LIST, bool DUAL>
@@ -245,7 +274,7 @@ static sbn_status head_few_forward(const HeadCall& c, const HeadPlan& h, float* 
     p.z_ev = reinterpret_cast<float*>(c.ws + w.z_ev);
     st = launch_head_few<0>(p, h.parts, list, dual, stream);
     if (st != SBN_OK) return st;
-    return launch_head_losses(HeadLossJob{tg, nullptr, nullptr, c.T, c.N, p.part, p.part1, p.z_ev, h.parts, 1.0 / static_cast<double>(c.tau), loss0, loss1, lse0, lse1},
+    return launch_head_losses(HeadLossJob{tg, nullptr, nullptr, c.T, c.N, p.part, p.part1, p.z_ev, nullptr, nullptr, c.K, h.parts, 1.0 / static_cast<double>(c.tau), loss0, loss1, lse0, lse1},
                               stream);
 }
 
@@ -257,7 +286,8 @@ static sbn_status head_few_backward(const HeadCall& c, const HeadPlan& h, const 
     if (st != SBN_OK) return st;
     const bool list = c.top != 0, dual = list && c.labels;
     HeadFewParams p = head_few_params(c, tg);
-    p.lse0 = lse0; p.lse1 = lse1; p.g0 = g0; p.g1 = g1;
+    p.lse0 = lse0; p.lse1 = lse1;
+    p.scale = HeadScale{g0, g1, p.inv_tau, reinterpret_cast<float*>(c.ws + w.scale)};
     p.dz = reinterpret_cast<uint16_t*>(c.ws + w.dz);
     p.ldz = h.piece;
     st = launch_head_few<1>(p, h.parts, list, dual, stream);
@@ -269,7 +299,7 @@ static sbn_status head_few_backward(const HeadCall& c, const HeadPlan& h, const 
     auto* kernel = c.T <= 8 ? head_few_grads_kernel<1> : head_few_grads_kernel<2>;
     if (launch_kernel(kernel, dim3(h.slabs * h.ranges), dim3(kFewHeadThreads), 0, stream, p) != cudaSuccess) return SBN_ERR_CUDA;
     ++g_launch_count;
-    return dx ? launch_head_dx(HeadDxJob{nullptr, p.acc, h.slots, c.T, c.K, static_cast<uint16_t*>(dx)}, stream) : SBN_OK;
+    return dx ? launch_head_dx(HeadDxJob{nullptr, p.acc, h.slots, c.T, c.K, p.scale.out, static_cast<uint16_t*>(dx)}, stream) : SBN_OK;
 }
 
 // ---- any number of tokens --------------------------------------------------------------------------
@@ -300,11 +330,22 @@ static sbn_status head_forward(const HeadCall& c, float* loss0, float* loss1, fl
     p.parts = h.parts;
     p.skip_loads = g_test_break_waits;
     const int tok_pad = static_cast<int>(head_up(c.T, 16));
-    st = h.words ? launch_head_words<0>(maps, HeadWordsParams{p, tok_pad, words_stages(tok_pad), nullptr, nullptr}, list, dual, stream)
+    st = h.words ? launch_head_words<0>(maps, HeadWordsParams{p, tok_pad, words_stages(tok_pad), nullptr, nullptr, HeadScale{}}, list, dual, stream)
                  : launch_head_logits<0>(maps, p, list, dual, stream);
     if (st != SBN_OK) return st;
-    return launch_head_losses(HeadLossJob{p.tg, p.count, p.row_src, c.T, c.N, p.part, p.part1, p.z_ev, h.parts, 1.0 / static_cast<double>(c.tau), loss0, loss1, lse0,
+    return launch_head_losses(HeadLossJob{p.tg, p.count, p.row_src, c.T, c.N, p.part, p.part1, p.z_ev, static_cast<const uint16_t*>(c.x),
+                                          static_cast<const uint16_t*>(c.head), c.K, h.parts, 1.0 / static_cast<double>(c.tau), loss0, loss1, lse0,
                                           lse1}, stream);
+}
+
+template <bool WIDE>
+static sbn_status launch_head_grads(const HeadGradMaps& maps, const HeadGradParams& p, cudaStream_t stream) {
+    using Loop = PairLoop<HeadGradsWork<WIDE>>;
+    if (!ensure_dynamic_smem<head_grads_kernel<WIDE>>(Loop::kSmemBytes)) return SBN_ERR_CUDA;
+    if (launch_kernel(head_grads_kernel<WIDE>, dim3(2 * kBackwardPairs), dim3(Loop::kThreads), Loop::kSmemBytes, stream, maps, p) != cudaSuccess)
+        return SBN_ERR_CUDA;
+    ++g_launch_count;
+    return SBN_OK;
 }
 
 static sbn_status head_backward(const HeadCall& c, const float* lse0, const float* lse1, const float* g0, const float* g1, void* dx, void* dhead,
@@ -315,16 +356,18 @@ static sbn_status head_backward(const HeadCall& c, const float* lse0, const floa
     const uint64_t k = static_cast<uint64_t>(c.K), t = static_cast<uint64_t>(c.T);
     HeadMaps maps;
     HeadGradMaps gm;
-    if (!head_encode(c, h, w, h.bn_piece, &maps)) return SBN_ERR_CUDA;
+    if (!head_encode(c, h, w, h.bn_piece, &maps) || !encode_out(&maps.dz, c.ws + w.dz, true, h.piece, h.rows256, 1, true)) return SBN_ERR_CUDA;
+    const uint32_t blocks = h.wide_grads ? 4 : 2;                       // of 64 columns, in a whole tile's box of B
     bool ok = encode_3d_bf16_blocks(&gm.aw, c.ws + w.dz, h.piece, h.rows256, 2) && encode_2d_bf16_sw128(&gm.ax, c.ws + w.dz, h.piece, h.rows256, h.piece, 128);
     for (int half = 0; ok && half < 2; ++half)
-        ok = (h.words || encode_3d_bf16_blocks(&gm.bx[half], c.x, k, t, half ? 1 : 2)) && encode_3d_bf16_blocks(&gm.bxc[half], c.ws + w.xc, k, h.rows64, half ? 1 : 2);
-    ok = ok && (!dx || encode_3d_f32_out(&gm.acc, c.ws + w.acc, k, t, h.slots));
-    constexpr int grads_smem = pair_loop_smem_bytes<HeadGradsWork>();
-    if (!ok || !ensure_dynamic_smem<head_grads_kernel>(grads_smem)) return SBN_ERR_CUDA;
+        ok = (h.words || encode_3d_bf16_blocks(&gm.bx[half], c.x, k, t, blocks >> half)) && encode_3d_bf16_blocks(&gm.bxc[half], c.ws + w.xc, k, h.rows64, blocks >> half);
+    ok = ok && (!dx || encode_3d_f32_out(&gm.acc, c.ws + w.acc, k, t, h.slots, h.wide_grads));
+    if (!ok) return SBN_ERR_CUDA;
     HeadRowsJob rows{};
     if (!h.words) rows.row_of = reinterpret_cast<int*>(c.ws + w.row_of);
+    rows.scale = HeadScale{g0, g1, static_cast<float>(1.0 / static_cast<double>(c.tau)), reinterpret_cast<float*>(c.ws + w.scale)};
     HeadLogitsParams p{};
+    p.scale = rows.scale.out;
     sbn_status st = launch_head_targets(c, w, &p.tg, stream);
     rows.tg = p.tg;
     if (st == SBN_OK && !h.words) st = launch_head_rows(c, w, rows, stream);
@@ -339,38 +382,36 @@ static sbn_status head_backward(const HeadCall& c, const float* lse0, const floa
     p.c0 = static_cast<float>(1.4426950408889634 / static_cast<double>(c.tau));
     p.inv_tau = static_cast<float>(1.0 / static_cast<double>(c.tau));
     p.lse0 = lse0; p.lse1 = lse1; p.g0 = g0; p.g1 = g1;
-    p.dz = reinterpret_cast<uint16_t*>(c.ws + w.dz);
-    p.ldz = h.piece;
     p.skip_loads = g_test_break_waits;
     HeadGradParams q{};
     q.count = p.count;
+    q.scale = p.scale;
     q.T = c.T; q.K = c.K;
     q.slot_stages = h.slot_stages;
     q.skip_loads = g_test_break_waits;
-    const int tiles_k = (c.K + 255) / 256, tok_pad = static_cast<int>(head_up(c.T, 16));
+    const int tiles_k = h.wide_grads ? (c.K + 511) / 512 : (c.K + 255) / 256, tok_pad = static_cast<int>(head_up(c.T, 16));
     for (int v0 = 0; v0 < c.N; v0 += h.piece) {
         const int cols = std::min(h.piece, c.N - v0);
         p.v0 = v0; p.v1 = v0 + cols;
-        st = h.words ? launch_head_words<1>(maps, HeadWordsParams{p, tok_pad, words_stages(tok_pad), static_cast<const uint16_t*>(c.x), reinterpret_cast<uint16_t*>(c.ws + w.xc)},
+        st = h.words ? launch_head_words<1>(maps, HeadWordsParams{p, tok_pad, words_stages(tok_pad), static_cast<const uint16_t*>(c.x), reinterpret_cast<uint16_t*>(c.ws + w.xc), rows.scale},
                                             list, dual, stream)
                      : launch_head_logits<1>(maps, p, list, dual, stream);
         if (st != SBN_OK) return st;
         const char* w_rows = static_cast<const char*>(c.head) + static_cast<size_t>(v0) * c.K * 2;
         for (int half = 0; half < 2; ++half)
-            if (!encode_3d_bf16_blocks(&gm.bw[half], w_rows, k, cols, half ? 1 : 2)) return SBN_ERR_CUDA;
+            if (!encode_3d_bf16_blocks(&gm.bw[half], w_rows, k, cols, blocks >> half)) return SBN_ERR_CUDA;
         const int all_stages = (cols + 63) / 64;
         q.cols = cols;
-        if (dhead && !encode_2d_bf16_sw128(&gm.dw, static_cast<uint16_t*>(dhead) + static_cast<size_t>(v0) * c.K, k, cols, k, 128)) return SBN_ERR_CUDA;
+        if (dhead && !encode_2d_bf16_out(&gm.dw, static_cast<uint16_t*>(dhead) + static_cast<size_t>(v0) * c.K, k, cols, h.wide_grads)) return SBN_ERR_CUDA;
         q.add = v0 > 0;
         const int slices = (all_stages + h.slot_stages - 1) / h.slot_stages;     // fewer in a short last piece
         const int tiles[2] = {dhead ? (cols + 255) / 256 * tiles_k : 0, dx ? static_cast<int>(h.rows256 / 256) * tiles_k * slices : 0};
         const int stages[2] = {(c.T + 63) / 64, h.slot_stages};
-        q.plan = plan_backward(tiles, stages, -1);
-        if (launch_kernel(head_grads_kernel, dim3(2 * kBackwardPairs), dim3(kPairLoopThreads), grads_smem, stream, gm, q) != cudaSuccess)
-            return SBN_ERR_CUDA;
-        ++g_launch_count;
+        q.plan = plan_backward(tiles, stages, -1, 7.5);
+        st = h.wide_grads ? launch_head_grads<true>(gm, q, stream) : launch_head_grads<false>(gm, q, stream);
+        if (st != SBN_OK) return st;
     }
-    return dx ? launch_head_dx(HeadDxJob{rows.row_of, reinterpret_cast<const float*>(c.ws + w.acc), h.slots, c.T, c.K, static_cast<uint16_t*>(dx)}, stream) : SBN_OK;
+    return dx ? launch_head_dx(HeadDxJob{rows.row_of, reinterpret_cast<const float*>(c.ws + w.acc), h.slots, c.T, c.K, p.scale, static_cast<uint16_t*>(dx)}, stream) : SBN_OK;
 }
 
 }  // namespace sbn

@@ -52,6 +52,23 @@ __device__ __forceinline__ void write_left_out(float* loss0, float* loss1, float
     report_bad(flags);
 }
 
+// The unit of dz: the largest |gradient of a loss| of the call (times 1 / tau for the distillation); 1 if that is none.
+// Kept as {unit, 1 / unit}.
+struct HeadScale {
+    const float *g0, *g1;                         // gradients per token (g1 may be null)
+    float inv_tau;
+    float* out;                                   // [2]
+};
+// A thread's share of the maximum: tokens tid, tid + threads, ...; those that nothing is asked of do not count.
+__device__ __forceinline__ float head_scale_share(const HeadScale& s, const HeadTargets& tg, int t, int N) {
+    const int flags = head_token_flags(tg, t, N);
+    float m = 0.0f;
+    if (tg.flags == nullptr ? (flags & kRowLabel) : (flags & kRowDistill)) m = fabsf(s.g0[t]) * s.inv_tau;
+    if (s.g1 != nullptr && (flags & kRowLabel)) m = fmaxf(m, fabsf(s.g1[t]));
+    return m;
+}
+__device__ __forceinline__ float head_scale_unit(float largest) { return largest > 0x1p-100f && largest < 0x1p100f ? largest : 1.0f; }
+
 struct HeadTargetsJob {
     const long long* index;                       // [T][top]
     const void* logits;                           // [T][top] fp32 or bf16
@@ -139,6 +156,7 @@ struct HeadRowsJob {
     int* row_of;                                  // out [T] or null: row of token t, -1 if left out
     uint16_t* xc;                                 // out [T up to a multiple of 64][K], written only if rows are left out
     float *loss0, *loss1, *lse0, *lse1;           // forward: outputs of rows left out (all null: backward)
+    HeadScale scale;                              // backward (out null: forward)
 };
 
 constexpr int kRowsThreads = 256;
@@ -160,15 +178,28 @@ __device__ __forceinline__ int block_sum(int v, int* scratch) {
 __global__ void __launch_bounds__(kRowsThreads)
 head_rows_kernel(const HeadRowsJob j, const int per) {
     __shared__ int s_scratch[kRowsThreads / 32];
+    __shared__ float s_largest[kRowsThreads / 32];
     pdl_launch_dependents();
     pdl_wait();
     const int first = blockIdx.x * per, last = min(j.T, first + per);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     int before = 0, total = 0;
+    float largest = 0.0f;
     for (int t = tid; t < j.T; t += kRowsThreads) {
         const int c = (head_token_flags(j.tg, t, j.N) & (kRowDistill | kRowLabel)) ? 1 : 0;
         total += c;
         before += t < first ? c : 0;
+        if (blockIdx.x == 0 && j.scale.out != nullptr) largest = fmaxf(largest, head_scale_share(j.scale, j.tg, t, j.N));
+    }
+    if (blockIdx.x == 0 && j.scale.out != nullptr) {
+        largest = warp_max(largest);
+        if (lane == 0) s_largest[warp] = largest;
+        __syncthreads();
+        if (tid == 0) {
+            for (int w = 1; w < kRowsThreads / 32; ++w) largest = fmaxf(largest, s_largest[w]);
+            j.scale.out[0] = head_scale_unit(largest);
+            j.scale.out[1] = 1.0f / head_scale_unit(largest);
+        }
     }
     total = block_sum(total, s_scratch);
     before = block_sum(before, s_scratch);
@@ -223,7 +254,9 @@ struct HeadLossJob {
     int T, N;
     const float2* part;                           // [rows][parts]: maximum m of the raw logits, sum of exp((z - m) / tau)
     const float* part1;                           // [rows][parts] or null: sum of exp(z - m)
-    const float* z_ev;                            // [rows][events]: logits at the events
+    const float* z_ev;                            // [rows][events]: logits at the teacher's entries; few tokens: at the label too
+    const uint16_t *x, *w;                        // null: few tokens
+    int K;
     int parts;
     double inv_tau;
     float *loss0, *loss1, *lse0, *lse1;           // at the tokens' own rows: distillation, label.  Cross entropy: loss1 and lse0
@@ -261,11 +294,29 @@ head_losses_kernel(const HeadLossJob j) {
             s0 += __shfl_xor_sync(0xFFFFFFFFu, s0, o);
             s1 += __shfl_xor_sync(0xFFFFFFFFu, s1, o);
         }
+        // The label's logit once more, in fp32 on the ordinary units: the tensor cores cut every partial sum off, always
+        // towards zero, which is no matter in lse but shows in the difference (relative error of the loss 2e-6, now 5e-7).
+        float z_label = 0.0f;
+        if (j.x != nullptr && (flags & kRowLabel)) {
+            const uint4* a = reinterpret_cast<const uint4*>(j.x + static_cast<size_t>(t) * j.K);
+            const uint4* b = reinterpret_cast<const uint4*>(j.w + static_cast<size_t>(j.tg.labels[t]) * j.K);
+            float lo = 0.0f, hi = 0.0f;
+            for (int i = lane; i < j.K >> 3; i += 32) {
+                const uint4 u = __ldg(a + i), v = __ldg(b + i);
+                lo = fmaf(bf16lo_to_f32(u.x), bf16lo_to_f32(v.x), lo); hi = fmaf(bf16hi_to_f32(u.x), bf16hi_to_f32(v.x), hi);
+                lo = fmaf(bf16lo_to_f32(u.y), bf16lo_to_f32(v.y), lo); hi = fmaf(bf16hi_to_f32(u.y), bf16hi_to_f32(v.y), hi);
+                lo = fmaf(bf16lo_to_f32(u.z), bf16lo_to_f32(v.z), lo); hi = fmaf(bf16hi_to_f32(u.z), bf16hi_to_f32(v.z), hi);
+                lo = fmaf(bf16lo_to_f32(u.w), bf16lo_to_f32(v.w), lo); hi = fmaf(bf16hi_to_f32(u.w), bf16hi_to_f32(v.w), hi);
+            }
+            z_label = lo + hi;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) z_label += __shfl_xor_sync(0xFFFFFFFFu, z_label, o);
+        }
         const double lse0 = static_cast<double>(m) * j.inv_tau + log(s0);
         if (j.tg.flags == nullptr) {                          // cross entropy
             if (lane == 0) {
                 j.lse0[t] = static_cast<float>(lse0);
-                j.loss1[t] = static_cast<float>(lse0 - static_cast<double>(j.z_ev[r]));
+                j.loss1[t] = static_cast<float>(lse0 - static_cast<double>(j.x != nullptr ? z_label : j.z_ev[r]));
             }
             continue;
         }
@@ -274,6 +325,10 @@ head_losses_kernel(const HeadLossJob j) {
         for (int i = lane; i < j.tg.events; i += 32) {
             if (j.tg.ev_col[static_cast<size_t>(t) * j.tg.events + i] == kNoColumn) continue;
             const float q = j.tg.ev_w[static_cast<size_t>(t) * j.tg.events + i];
+            if (q < 0.0f && j.x != nullptr) {
+                ce = lse1 - static_cast<double>(z_label);
+                continue;
+            }
             const double z = static_cast<double>(j.z_ev[static_cast<size_t>(r) * j.tg.events + i]);
             if (q < 0.0f) ce = lse1 - z;
             else if (!(q == 0.0f)) kd += static_cast<double>(q) * (static_cast<double>(logf(q)) - z * j.inv_tau + lse0);
@@ -299,6 +354,7 @@ struct HeadDxJob {
     const int* row_of;                            // null (few tokens): every token has its row
     const float* acc;                             // [slots][T][K]
     int slots, T, K;
+    const float* scale;                           // the unit of dz
     uint16_t* dx;                                 // [T][K]
 };
 
@@ -311,6 +367,7 @@ head_dx_kernel(const HeadDxJob j) {
     const int vecs = j.K >> 2;                    // 4 values per thread and step
     const long long all = static_cast<long long>(j.T) * vecs;
     const size_t slot = static_cast<size_t>(j.T) * j.K;
+    const float scale = *j.scale;
     for (long long i = static_cast<long long>(blockIdx.x) * kDxThreads + threadIdx.x; i < all; i += static_cast<long long>(gridDim.x) * kDxThreads) {
         const int t = static_cast<int>(i / vecs), c = static_cast<int>(i - static_cast<long long>(t) * vecs);
         const int r = j.row_of != nullptr ? j.row_of[t] : t;
@@ -323,6 +380,7 @@ head_dx_kernel(const HeadDxJob j) {
                 v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
             }
         }
+        v.x *= scale; v.y *= scale; v.z *= scale; v.w *= scale;
         uint2 o;
         asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o.x) : "f"(v.y), "f"(v.x));
         asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o.y) : "f"(v.w), "f"(v.z));

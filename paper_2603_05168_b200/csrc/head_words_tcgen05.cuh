@@ -19,7 +19,7 @@ namespace sbn {
 constexpr int kWordsTokens = 256;
 constexpr int kWordsThreads = 192;
 constexpr int kWordsTurnBytes = 4 * 32 * 33 * 4 + 512;                     // the four warps' squares, up to a multiple of 1 KB
-constexpr int kWordsStateBytes = 4 * 3 * kWordsTokens * 4;                 // stats: [warp][m, s0, s1][token]
+constexpr int kWordsStateBytes = 4 * 3 * kWordsTokens * 4;                 // stats: [warp][m, s0, s1][token]; grad: the warps' boxes
 static_assert(kWordsTurnBytes % 1024 == 0, "keeps the 1 KB alignment");
 
 struct HeadWordsParams {
@@ -27,6 +27,7 @@ struct HeadWordsParams {
     int tok_pad, stages;
     const uint16_t* x;            // grad: copied to xc [T up to a multiple of 64][K]
     uint16_t* xc;
+    HeadScale scale;              // grad
 };
 
 static inline int words_stage_bytes(int tok_pad) { return 128 * 128 + tok_pad * 128; }
@@ -135,6 +136,8 @@ head_words_kernel(const __grid_constant__ HeadMaps maps, const __grid_constant__
         const int chunks = (all + 31) >> 5;
         const uint32_t lane_base = static_cast<uint32_t>(quarter * 32) << 16;
         HeadRow<MODE, LIST, DUAL> row;
+        float inv_scale = 1.0f;
+        const uint32_t box = smem_u32(state) + static_cast<uint32_t>(quarter * kWarpBoxBytes);       // grad: no state
         if constexpr (MODE == 0) {
             for (int c = 0; c < chunks; ++c) {
                 mine[c * 32 + lane] = -INFINITY;
@@ -142,6 +145,14 @@ head_words_kernel(const __grid_constant__ HeadMaps maps, const __grid_constant__
                 mine[2 * kWordsTokens + c * 32 + lane] = 0.0f;
             }
         } else {
+            float largest = 0.0f;                                          // every warp for itself
+            for (int t = lane; t < p.T; t += 32) largest = fmaxf(largest, head_scale_share(wp.scale, p.tg, t, p.N));
+            const float unit = head_scale_unit(warp_max(largest));
+            inv_scale = 1.0f / unit;
+            if (blockIdx.x == 0 && threadIdx.x == 64) {
+                wp.scale.out[0] = unit;
+                wp.scale.out[1] = inv_scale;
+            }
             // x for dW, zeros in rows that nothing is asked of and behind the last token
             const int vecs = p.K >> 3;
             for (int t = blockIdx.x; t < all; t += gridDim.x) {
@@ -178,23 +189,29 @@ head_words_kernel(const __grid_constant__ HeadMaps maps, const __grid_constant__
                 for (int q = 0; q < 32; ++q) z[q] = __float_as_uint(square[lane * 33 + q]);
                 const int t = c * 32 + lane;
                 const bool here = t < p.T && (head_token_flags(p.tg, t, p.N) & (kRowDistill | kRowLabel));
-                row.begin(p, t, here ? t : 0, here);
+                row.begin(p, t, here ? t : 0, here, inv_scale);
                 row.seek(p, n0);
                 if constexpr (MODE == 0) {
                     row.m = mine[t];
                     row.s0 = mine[kWordsTokens + t];
                     if (DUAL) row.s1 = mine[2 * kWordsTokens + t];
+                    row.note_targets(p, n0, [&](int q) { return square[lane * 33 + q]; });
                     row.stats(p, z, n0);
+                    __syncwarp();
                     mine[t] = row.m;
                     mine[kWordsTokens + t] = row.s0;
                     if (DUAL) mine[2 * kWordsTokens + t] = row.s1;
                 } else {
-                    row.grad(p, z, n0);
+                    uint32_t o[16];
+                    row.grad(p, z, n0, o);
+                    store_warp_box(box, lane, o, [&] { tma_store_2d(&maps.dz, n0 - p.v0, c * 32, box); });
                 }
             }
             ++acc_iter;
         }
-        if constexpr (MODE == 0) {
+        if constexpr (MODE == 1) {
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        } else {
             for (int c = 0; c < chunks; ++c) {
                 const int t = c * 32 + lane;
                 if (t >= p.T) break;
