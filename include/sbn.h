@@ -495,7 +495,7 @@ const char *sbn_status_string(sbn_status s);
  * 256 = force the single-CTA kernel with that token-tile width; a negative value -BN = force the
  * CTA-pair kernel with BN tokens per tile (rounded to a multiple of 16, capped at 240 sparse /
  * 256 dense; with split_k = 1 its variant with one M-tile per CTA) and the backward GEMMs with tiles of 128 (BN <= 128) or
- * 256 columns, and the calls at the output head for more than 256 tokens with tiles of 512 (BN >= 512), 256, 128 or 64 words
+ * 256 columns, and the calls at the output head for more than 256 tokens with tiles of 256 (BN >= 256), 128 or 64 words
  * and gradients in tiles of 512 (BN >= 512) or 256 columns (their workspaces are asked for under the same setting).  split_k: 0 = automatic; k > 0 = split K k ways through int32 atomics in the
  * workspace (single-CTA kernel); -2, -3, -4, -8 = split K inside thread-block clusters of that many
  * CTAs (token tile 64, or 32 if token_tile says so; a token_tile of 80 or more selects the wide-tile kernel with that width,

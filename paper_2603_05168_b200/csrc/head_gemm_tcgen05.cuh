@@ -225,10 +225,10 @@ struct HeadRow {
     }
 };
 
-template <int MODE, bool LIST, bool DUAL, bool WIDE>
+template <int MODE, bool LIST, bool DUAL>
 struct HeadLogitsWork {
-    static constexpr bool kWide = WIDE;
-    static constexpr int kStages = WIDE ? 4 : (MODE == 0 ? 7 : 6), kStagingBytes = MODE == 0 ? 0 : (WIDE ? 16 : 8) * kWarpBoxBytes;
+    static constexpr bool kWide = false;
+    static constexpr int kStages = MODE == 0 ? 7 : 6, kStagingBytes = MODE == 0 ? 0 : 8 * kWarpBoxBytes;
     const HeadMaps& maps;
     const HeadLogitsParams& p;
     int rows, tiles_m, tiles_v;
@@ -269,7 +269,7 @@ struct HeadLogitsWork {
         tma_load_2d_pair(st, moved ? &maps.xc : &maps.x, ks * 64, t.m0 + static_cast<int>(rank) * 128, bar);
         tma_load_2d_pair(st + kPairLoopStageA, &maps.w, ks * 64, t.n0 + static_cast<int>(rank) * (t.bn >> 1), bar);
     }
-    __device__ uint32_t idesc(const Tile& t) const { return make_idesc_bf16_any(256, WIDE ? 256 : t.bn, false, false); }
+    __device__ uint32_t idesc(const Tile& t) const { return make_idesc_bf16_any(256, t.bn, false, false); }
     __device__ uint64_t a_step(const Tile&) const { return 32 >> 4; }
     __device__ uint64_t b_step(const Tile&) const { return 32 >> 4; }
     __device__ uint64_t a_desc(const Tile&, uint32_t s) const { return make_smem_desc(s, 16, 1024, kSwz128); }
@@ -283,13 +283,11 @@ struct HeadLogitsWork {
 
         __device__ Epilogue(const HeadLogitsWork& work, int rk, int q, int sb, int ln, uint32_t staging)
             : w(work), rank(rk), quarter(q), sub(sb), lane(ln), box(staging + static_cast<uint32_t>((sb * 4 + q) * kWarpBoxBytes)) {}
-        // wide: the tile's column that this warp's 128 begin with
-        __device__ int first_col(const Tile& tile) const { return tile.n0 + (WIDE ? 128 * (sub >> 1) + 256 * (sub & 1) : 0); }
         __device__ void begin(const Tile& tile) {
             const int r = tile.m0 + rank * 128 + quarter * 32 + lane;
             const bool here = r < w.rows;
             row.begin(w.p, r, here ? w.p.row_src[r] : 0, here, w.inv_scale);
-            row.seek(w.p, first_col(tile));
+            row.seek(w.p, tile.n0);
         }
         template <class Release>
         __device__ void run(const Tile& tile, uint32_t taddr, Release&& release) {
@@ -300,16 +298,13 @@ struct HeadLogitsWork {
                 release();
                 return;
             }
-            const int from = WIDE ? 0 : sub, to = WIDE ? 4 : chunks, step = WIDE ? 1 : 2;
-            if (WIDE) taddr += static_cast<uint32_t>(128 * sub);
-            const int n0 = first_col(tile);
 #pragma unroll 1
-            for (int c = from; c < to; c += step) {
+            for (int c = sub; c < chunks; c += 2) {
                 uint32_t z[32];
                 __syncwarp();                              // the lanes may have parted over their targets
                 tmem_ld_32x32b_x32(taddr + static_cast<uint32_t>(c * 32), z);
                 tmem_ld_wait();
-                const int n = n0 + c * 32;
+                const int n = tile.n0 + c * 32;
                 if constexpr (MODE == 0)
                     row.note_targets(w.p, n, [&](int q) {
                         uint32_t v;
@@ -317,7 +312,7 @@ struct HeadLogitsWork {
                         tmem_ld_wait();
                         return __uint_as_float(v);
                     });
-                if (c + step >= to) release();
+                if (c + 2 >= chunks) release();
                 if constexpr (MODE == 0) {
                     row.stats(w.p, z, n);
                 } else {
@@ -326,7 +321,7 @@ struct HeadLogitsWork {
                     store_warp_box(box, lane, o, [&] { tma_store_2d(&w.maps.dz, n - w.p.v0, first_row, box); });
                 }
             }
-            if (MODE == 0 && row.here) row.store_part(w.p, (WIDE ? 4 : 2) * ((tile.n0 - w.p.v0) / tile.bn) + sub);
+            if (MODE == 0 && row.here) row.store_part(w.p, 2 * ((tile.n0 - w.p.v0) / tile.bn) + sub);
         }
         __device__ void finish() {
             if (MODE == 1 && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
@@ -334,11 +329,11 @@ struct HeadLogitsWork {
     };
 };
 
-template <int MODE, bool LIST, bool DUAL, bool WIDE>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(WIDE ? 576 : 320, 1)
+template <int MODE, bool LIST, bool DUAL>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(320, 1)
 head_logits_kernel(const __grid_constant__ HeadMaps maps, const __grid_constant__ HeadLogitsParams p) {
     pdl_launch_dependents();
-    HeadLogitsWork<MODE, LIST, DUAL, WIDE> work(maps, p);
+    HeadLogitsWork<MODE, LIST, DUAL> work(maps, p);
     bf16_pair_loop(work, p.skip_loads != 0);
 }
 
@@ -406,8 +401,11 @@ struct HeadGradsWork {
                         t.k_first = t.slot * p.slot_stages;
                         t.k_stages = min(p.slot_stages, (p.cols + 63) / 64 - t.k_first);
                     }
-                    t.m0 = (tile % tiles_m) * 256;
-                    t.n0 = (tile / tiles_m) * kTileCols + (sg.half ? (u & 1) * (kTileCols / 2) : 0);
+                    // dW: a group of words' tiles next to one another, so that its dz comes from memory once (x stays in the L2);
+                    // dx: all tiles run along the vocabulary side by side
+                    const int tiles_n = (p.K + kTileCols - 1) / kTileCols;
+                    t.m0 = (t.part == 0 ? tile / tiles_n : tile % tiles_m) * 256;
+                    t.n0 = (t.part == 0 ? tile % tiles_n : tile / tiles_m) * kTileCols + (sg.half ? (u & 1) * (kTileCols / 2) : 0);
                     if (t.part == 1 && t.m0 >= w.rows) continue;            // rows left out
                     return true;
                 }
@@ -460,33 +458,37 @@ struct HeadGradsWork {
                 release();
                 return;
             }
-#pragma unroll 1
-            for (int c = 0; c < 4; ++c) {
-                uint32_t v[32];
-                __syncwarp();
-                tmem_ld_32x32b_x32(taddr + static_cast<uint32_t>(128 * parity + c * 32), v);
-                tmem_ld_wait();
-                if (c == 3) release();
-                const int n = n0 + c * 32;
-                if (t.part == 0) {
-                    uint32_t o[16];
+            taddr += static_cast<uint32_t>(128 * parity);
+            if (t.part == 0) {
+                // all 128 columns into registers, halved in size, before anything is stored: the next tile's MMAs wait for this
+                uint32_t o[4][16];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[i]) : "f"(__uint_as_float(v[2 * i + 1]) * w.scale), "f"(__uint_as_float(v[2 * i]) * w.scale));
-                    store_warp_box(staging, lane, o, [&] { tma_store_2d(&w.maps.dw, n, m, staging); });
-                } else {
+                for (int c = 0; c < 8; ++c) {
+                    uint32_t v[16];
+                    tmem_ld_32x32b_x16(taddr + static_cast<uint32_t>(c * 16), v);
+                    tmem_ld_wait();
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        uint32_t o[16];
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) o[i] = v[16 * h + i];
-                        // One tile of a launch adds to an element, and launches follow one another: the sum's order is fixed
-                        store_warp_box(staging, lane, o, [&] {
-                            if (p.add) tma_add_3d(&w.maps.acc, n + 16 * h, m, t.slot, staging);
-                            else tma_store_3d(&w.maps.acc, n + 16 * h, m, t.slot, staging);
-                        });
-                    }
+                    for (int i = 0; i < 8; ++i)
+                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;"
+                            : "=r"(o[c >> 1][8 * (c & 1) + i]) : "f"(__uint_as_float(v[2 * i + 1]) * w.scale), "f"(__uint_as_float(v[2 * i]) * w.scale));
                 }
+                release();
+#pragma unroll
+                for (int c = 0; c < 4; ++c) store_warp_box(staging, lane, o[c], [&] { tma_store_2d(&w.maps.dw, n0 + c * 32, m, staging); });
+                return;
+            }
+#pragma unroll 1
+            for (int c = 0; c < 8; ++c) {
+                uint32_t v[16];
+                __syncwarp();
+                tmem_ld_32x32b_x16(taddr + static_cast<uint32_t>(c * 16), v);
+                tmem_ld_wait();
+                if (c == 7) release();
+                // One tile of a launch adds to an element, and launches follow one another: the sum's order is fixed
+                store_warp_box(staging, lane, v, [&] {
+                    if (p.add) tma_add_3d(&w.maps.acc, n0 + c * 16, m, t.slot, staging);
+                    else tma_store_3d(&w.maps.acc, n0 + c * 16, m, t.slot, staging);
+                });
             }
         }
 

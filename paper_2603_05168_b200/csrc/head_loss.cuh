@@ -23,8 +23,8 @@ static inline long long head_up(long long v, long long to) { return (v + to - 1)
 // Columns per tile of z: as wide as possible (a wide tile reads its rows for more columns), narrower where the tiles would
 // not go round.  us per stage and per tile, as measured.
 static int head_tile_columns(int T, int cols, int K) {
-    static const struct { int bn; double stage, tile; } kShapes[] = {{512, 0.56, 2.5}, {256, 0.38, 1.0}, {128, 0.33, 1.0}, {64, 0.31, 1.0}};
-    if (g_force_token_tile < 0) return g_force_token_tile <= -512 ? 512 : (g_force_token_tile <= -256 ? 256 : (g_force_token_tile <= -128 ? 128 : 64));
+    static const struct { int bn; double stage, tile; } kShapes[] = {{256, 0.38, 1.0}, {128, 0.33, 1.0}, {64, 0.31, 1.0}};
+    if (g_force_token_tile < 0) return g_force_token_tile <= -256 ? 256 : (g_force_token_tile <= -128 ? 128 : 64);
     int best = 256;
     double best_cost = 1e300;
     for (const auto& shape : kShapes) {
@@ -54,7 +54,7 @@ static HeadPlan head_plan(int T, int N, int K) {
     h.rows256 = head_up(T, 256);
     h.words = T <= kWordsTokens;
     h.bn = head_tile_columns(T, N, K);
-    h.parts = h.words ? 4 * std::min((N + 127) / 128, kNumSMs) : (h.bn == 512 ? 4 : 2) * ((N + h.bn - 1) / h.bn);
+    h.parts = h.words ? 4 * std::min((N + 127) / 128, kNumSMs) : 2 * ((N + h.bn - 1) / h.bn);
     long long cols = (128ll << 20) / (2 * h.rows256);
     cols = std::max(1024ll, cols / 512 * 512);
     const long long pieces = (N + cols - 1) / cols;
@@ -154,25 +154,21 @@ static bool head_encode(const HeadCall& c, const HeadPlan& h, const HeadWs& w, i
            encode_2d_bf16_sw128(&maps->w, c.head, k, c.N, k, bn / 2);
 }
 
-template <int MODE, bool LIST, bool DUAL, bool WIDE>
+template <int MODE, bool LIST, bool DUAL>
 static sbn_status launch_head_logits_as(const HeadMaps& maps, const HeadLogitsParams& p, cudaStream_t stream) {
-    using Loop = PairLoop<HeadLogitsWork<MODE, LIST, DUAL, WIDE>>;
-    if (!ensure_dynamic_smem<head_logits_kernel<MODE, LIST, DUAL, WIDE>>(Loop::kSmemBytes)) return SBN_ERR_CUDA;
+    using Loop = PairLoop<HeadLogitsWork<MODE, LIST, DUAL>>;
+    if (!ensure_dynamic_smem<head_logits_kernel<MODE, LIST, DUAL>>(Loop::kSmemBytes)) return SBN_ERR_CUDA;
     const long long tiles = head_up(p.T, 256) / 256 * ((p.v1 - p.v0 + p.bn - 1) / p.bn);
     const unsigned pairs = static_cast<unsigned>(std::min<long long>(tiles, kBackwardPairs));
-    if (launch_kernel(head_logits_kernel<MODE, LIST, DUAL, WIDE>, dim3(2 * pairs), dim3(Loop::kThreads), Loop::kSmemBytes, stream, maps, p) != cudaSuccess)
+    if (launch_kernel(head_logits_kernel<MODE, LIST, DUAL>, dim3(2 * pairs), dim3(Loop::kThreads), Loop::kSmemBytes, stream, maps, p) != cudaSuccess)
         return SBN_ERR_CUDA;
     ++g_launch_count;
     return SBN_OK;
 }
-template <int MODE, bool WIDE>
-static sbn_status launch_head_logits_of(const HeadMaps& maps, const HeadLogitsParams& p, bool list, bool dual, cudaStream_t stream) {
-    if (!list) return launch_head_logits_as<MODE, false, false, WIDE>(maps, p, stream);
-    return dual ? launch_head_logits_as<MODE, true, true, WIDE>(maps, p, stream) : launch_head_logits_as<MODE, true, false, WIDE>(maps, p, stream);
-}
 template <int MODE>
 static sbn_status launch_head_logits(const HeadMaps& maps, const HeadLogitsParams& p, bool list, bool dual, cudaStream_t stream) {
-    return p.bn == 512 ? launch_head_logits_of<MODE, true>(maps, p, list, dual, stream) : launch_head_logits_of<MODE, false>(maps, p, list, dual, stream);
+    if (!list) return launch_head_logits_as<MODE, false, false>(maps, p, stream);
+    return dual ? launch_head_logits_as<MODE, true, true>(maps, p, stream) : launch_head_logits_as<MODE, true, false>(maps, p, stream);
 }
 
 template <int MODE, bool LIST, bool DUAL>
