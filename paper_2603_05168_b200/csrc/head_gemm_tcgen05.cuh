@@ -39,11 +39,11 @@ __device__ __forceinline__ void tma_add_3d(const CUtensorMap* map, int c0, int c
 }
 
 // 32 rows x 64 bytes of a warp (lane = row) through kWarpBoxBytes of shared memory of its own: the 16-byte pieces q of a row at
-// q ^ (row / 2 % 4), as the 64-byte swizzle has them; store() issues the TMA store.  Waits for the box's last store first.
+// q ^ (row / 2 % 4), as the 64-byte swizzle has them; store() issues the TMA store.  Waits for the warp's stores before it to be read out.
 constexpr int kWarpBoxBytes = 2048;
 template <class Store>
-__device__ __forceinline__ void store_warp_box(uint32_t box, int lane, const uint32_t (&v)[16], Store&& store) {
-    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+__device__ __forceinline__ void store_warp_box(uint32_t box, int lane, const uint32_t (&v)[16], Store&& store, bool wait = true) {
+    if (wait && lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
     __syncwarp();
     const uint32_t to = box + static_cast<uint32_t>(lane * 64), x = static_cast<uint32_t>(lane >> 1) & 3u;
 #pragma unroll
@@ -338,7 +338,7 @@ head_logits_kernel(const __grid_constant__ HeadMaps maps, const __grid_constant_
 }
 
 // ---- gradients of a piece --------------------------------------------------------------------------
-// dw, acc: how results leave, in boxes of 128 rows x 128 bytes (wide tiles: 32 rows x 64 bytes).
+// dw, acc: how results leave, in boxes of 32 rows x 64 bytes.
 struct HeadGradMaps {
     CUtensorMap aw;               // dz piece for dW: MN-major, two blocks of 64 columns
     CUtensorMap ax;               // dz piece for dx: K-major
@@ -354,6 +354,7 @@ struct HeadGradParams {
     int cols;                     // vocabulary rows of the piece
     int slot_stages;              // dx's contraction is cut into slices of that many stages, each with a slot of its own
     int add;                      // not the first piece: add to acc
+    int want_dx, want_dw;
     BackwardPlan plan;            // part 0: dW, part 1: dx (tile index = slice * tiles of dx + tile)
     int skip_loads;
 };
@@ -361,7 +362,7 @@ struct HeadGradParams {
 template <bool WIDE>
 struct HeadGradsWork {
     static constexpr bool kWide = WIDE;
-    static constexpr int kStages = WIDE ? 4 : 6, kStagingBytes = 2 * 128 * 128, kTileCols = WIDE ? 512 : 256;
+    static constexpr int kStages = WIDE ? 4 : 6, kStagingBytes = 16 * kWarpBoxBytes, kTileCols = WIDE ? 512 : 256;
     const HeadGradMaps& maps;
     const HeadGradParams& p;
     int rows;
@@ -373,6 +374,35 @@ struct HeadGradsWork {
         rows = p.count != nullptr ? *p.count : p.T;
         scale = *p.scale;
         moved = p.count == nullptr || rows < p.T;
+        if (fewer_rows()) share();
+    }
+    __device__ bool fewer_rows() const { return p.count != nullptr && rows < p.T; }
+    __device__ int tiles_m() const { return (max(rows, 1) + 255) / 256; }
+
+    // With rows left out (the count is known here only): dx's tiles, which are long, go round; dW's go to the pairs with one tile of dx
+    // less first (`most` pairs have one more than the others), as many as are as long, then round.
+    int dx_all, most, dw_each, dw_extra, dw_left;
+    __device__ void share() {
+        const int tiles_n = (p.K + kTileCols - 1) / kTileCols;
+        const int slices = p.want_dx ? ((p.cols + 63) / 64 + p.slot_stages - 1) / p.slot_stages : 0;
+        const int dw_all = p.want_dw ? (p.cols + 255) / 256 * tiles_n : 0;
+        dx_all = tiles_m() * tiles_n * slices;
+        most = dx_all % kBackwardPairs;
+        const int others = kBackwardPairs - most;
+        const float longer = (static_cast<float>(p.slot_stages) + 3.0f) / (fmaxf(static_cast<float>((rows + 63) / 64), 7.5f) + 3.0f);
+        const float each = (static_cast<float>(dw_all) - (most != 0 ? others * longer : 0.0f)) / kBackwardPairs;
+        dw_each = max(0, static_cast<int>(floorf(each)));
+        const int rest = dw_all - dw_each * kBackwardPairs;
+        dw_extra = rest / others;
+        dw_left = rest % others;
+    }
+    __device__ int dx_of(int pair) const { return dx_all / kBackwardPairs + (pair < most ? 1 : 0); }
+    // The i-th tile of dW of a pair, -1: no more.
+    __device__ int dw_of(int pair, int i) const {
+        if (i < dw_each) return i * kBackwardPairs + pair;
+        const int at = i - dw_each, who = pair - most, others = kBackwardPairs - most;
+        if (who < 0 || at > dw_extra || (at == dw_extra && who >= dw_left)) return -1;
+        return dw_each * kBackwardPairs + at * others + who;
     }
 
     struct Tile { int part, m0, n0, bn, k_stages, k_first, slot; };
@@ -380,33 +410,49 @@ struct HeadGradsWork {
         const HeadGradsWork& w;
         int pair, g, i;
         __device__ Tiles(const HeadGradsWork& work, int pr) : w(work), pair(pr), g(0), i(0) {}
+        // Entry u of a part: a whole tile, or a half of tile first + u / 2.
+        __device__ void set(Tile& t, int part, int u, bool half, int first) const {
+            const HeadGradParams& p = w.p;
+            const int tiles_n = (p.K + kTileCols - 1) / kTileCols;
+            t.part = part;
+            t.bn = half ? kTileCols / 2 : kTileCols;
+            int tile = half ? first + (u >> 1) : u;
+            t.slot = 0;
+            t.k_first = 0;
+            if (part == 0) {
+                // words' tiles next to one another, so that their dz comes from memory once (x stays in the L2)
+                t.k_stages = (max(w.rows, 1) + 63) / 64;
+                t.m0 = tile / tiles_n * 256;
+                t.n0 = tile % tiles_n * kTileCols;
+            } else {
+                // all tiles run along the vocabulary side by side
+                const int tiles_m = w.tiles_m(), tiles = tiles_m * tiles_n;
+                t.slot = tile / tiles;
+                tile -= t.slot * tiles;
+                t.k_first = t.slot * p.slot_stages;
+                t.k_stages = min(p.slot_stages, (p.cols + 63) / 64 - t.k_first);
+                t.m0 = tile % tiles_m * 256;
+                t.n0 = tile / tiles_m * kTileCols;
+            }
+            if (half) t.n0 += (u & 1) * (kTileCols / 2);
+        }
         __device__ bool next(Tile& t) {
             const HeadGradParams& p = w.p;
+            if (w.fewer_rows()) {                       // the host's plan is for all rows
+                if (i < w.dx_of(pair)) {
+                    set(t, 1, i * kBackwardPairs + pair, false, 0);
+                } else {
+                    const int u = w.dw_of(pair, i - w.dx_of(pair));
+                    if (u < 0) return false;
+                    set(t, 0, u, false, 0);
+                }
+                ++i;
+                return true;
+            }
             for (; g < p.plan.segments; ++g, i = 0) {
                 const BackwardSegment& sg = p.plan.seg[g];
-                while (i < sg.count(pair)) {
-                    const int u = sg.index(pair, i++);
-                    t.part = sg.part;
-                    t.bn = sg.half ? kTileCols / 2 : kTileCols;
-                    const int tiles_m = ((t.part == 0 ? p.cols : p.T) + 255) / 256;
-                    int tile = sg.half ? sg.first_tile + (u >> 1) : u;
-                    t.slot = 0;
-                    t.k_first = 0;
-                    if (t.part == 0) {
-                        t.k_stages = (max(w.rows, 1) + 63) / 64;
-                    } else {
-                        const int tiles = tiles_m * ((p.K + kTileCols - 1) / kTileCols);
-                        t.slot = tile / tiles;
-                        tile -= t.slot * tiles;
-                        t.k_first = t.slot * p.slot_stages;
-                        t.k_stages = min(p.slot_stages, (p.cols + 63) / 64 - t.k_first);
-                    }
-                    // dW: a group of words' tiles next to one another, so that its dz comes from memory once (x stays in the L2);
-                    // dx: all tiles run along the vocabulary side by side
-                    const int tiles_n = (p.K + kTileCols - 1) / kTileCols;
-                    t.m0 = (t.part == 0 ? tile / tiles_n : tile % tiles_m) * 256;
-                    t.n0 = (t.part == 0 ? tile % tiles_n : tile / tiles_m) * kTileCols + (sg.half ? (u & 1) * (kTileCols / 2) : 0);
-                    if (t.part == 1 && t.m0 >= w.rows) continue;            // rows left out
+                if (i < sg.count(pair)) {
+                    set(t, sg.part, sg.index(pair, i++), sg.half != 0, sg.first_tile);
                     return true;
                 }
             }
@@ -429,19 +475,16 @@ struct HeadGradsWork {
     __device__ uint64_t a_desc(const Tile& t, uint32_t s) const { return make_smem_desc(s, t.part == 0 ? 8192 : 16, 1024, kSwz128); }
     __device__ uint64_t b_desc(const Tile&, uint32_t s) const { return make_smem_desc(s, 8192, 1024, kSwz128); }
 
-    // Results go out through shared memory and TMA stores, which also clip what lies outside.  Stored by the threads themselves, a
-    // row each, every 16 bytes were a transaction of their own: 4 us per fp32 tile.
-    //   narrow  64 columns at a time: every warp puts its 32 rows x 32 columns into a buffer of the CTA (the 128-byte swizzle keeps the
-    //           rows' 16-byte pieces on different banks), one thread stores boxes of 128 rows x 128 bytes
-    //   wide    every warp has 2 KB of its own and stores boxes of 32 rows x 64 bytes (64-byte swizzle): nothing to wait for but itself
+    // Results go out through shared memory and TMA stores, which also clip what lies outside: every warp has 2 KB of its own (narrow
+    // tiles: twice) and stores boxes of 32 rows x 64 bytes.  Stored by the threads themselves, a row each, every 16 bytes were a
+    // transaction of their own: 4 us per fp32 tile.
     struct Epilogue {
         const HeadGradsWork& w;
-        int rank, quarter, parity, lane;                    // parity: `sub` of the loop
+        int rank, quarter, parity, lane;                    // parity: `sub` of the loop (narrow: even or odd chunks)
         uint32_t staging;
         __device__ Epilogue(const HeadGradsWork& work, int rk, int q, int sub, int ln, uint32_t st)
-            : w(work), rank(rk), quarter(q), parity(sub), lane(ln), staging(st + (WIDE ? static_cast<uint32_t>((sub * 4 + q) * kWarpBoxBytes) : 0u)) {}
+            : w(work), rank(rk), quarter(q), parity(sub), lane(ln), staging(st + static_cast<uint32_t>((sub * 4 + q) * kWarpBoxBytes)) {}
         __device__ void begin(const Tile&) {}
-        __device__ bool leader() const { return (WIDE || (quarter == 0 && parity == 0)) && lane == 0; }
 
         template <class Release>
         __device__ void run(const Tile& t, uint32_t taddr, Release&& release) {
@@ -484,69 +527,51 @@ struct HeadGradsWork {
                 tmem_ld_32x32b_x16(taddr + static_cast<uint32_t>(c * 16), v);
                 tmem_ld_wait();
                 if (c == 7) release();
-                // One tile of a launch adds to an element, and launches follow one another: the sum's order is fixed
-                store_warp_box(staging, lane, v, [&] {
-                    if (p.add) tma_add_3d(&w.maps.acc, n0 + c * 16, m, t.slot, staging);
-                    else tma_store_3d(&w.maps.acc, n0 + c * 16, m, t.slot, staging);
-                });
+                store_warp_box(staging, lane, v, [&] { store_sums(t, n0 + c * 16, m, staging); });
             }
         }
 
         template <class Release>
         __device__ void run_narrow(const Tile& t, uint32_t taddr, Release&& release) {
             const HeadGradParams& p = w.p;
-            const int m0 = t.m0 + rank * 128;
-            const bool rows_in = m0 < (t.part == 0 ? p.cols : w.rows);
-            const int pairs = t.bn >> 6;
-            const int row = quarter * 32 + lane;
+            const int m = t.m0 + rank * 128 + quarter * 32;
+            const int chunks = min(t.bn, p.K - t.n0) >> 5;          // K % 128 == 0
+            if (m >= (t.part == 0 ? p.cols : w.rows) || parity >= chunks) {
+                release();
+                return;
+            }
 #pragma unroll 1
-            for (int c = 0; c < pairs; ++c) {
+            for (int c = parity; c < chunks; c += 2) {
                 uint32_t v[32];
                 __syncwarp();
-                tmem_ld_32x32b_x32(taddr + static_cast<uint32_t>(c * 64 + parity * 32), v);
+                tmem_ld_32x32b_x32(taddr + static_cast<uint32_t>(c * 32), v);
                 tmem_ld_wait();
-                if (c + 1 == pairs) release();
-                const int n = t.n0 + c * 64;
-                if (!rows_in || n >= p.K) continue;         // the same for all warps; K % 64 == 0
-                if (leader()) {                             // the buffers' last stores have been read out (dW: the one before the last)
-                    if (t.part == 0 && c > 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-                    else asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-                }
-                epilogue_sync();
+                if (c + 2 >= chunks) release();
+                const int n = t.n0 + c * 32;
+                uint32_t o[16];
                 if (t.part == 0) {
-                    const uint32_t to = staging + static_cast<uint32_t>((c & 1) * 16384 + row * 128);
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        uint32_t o[4];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[i]) : "f"(__uint_as_float(v[8 * q + 2 * i + 1]) * w.scale), "f"(__uint_as_float(v[8 * q + 2 * i]) * w.scale));
-                        st_shared_16(to + (((parity * 4 + q) ^ (row & 7)) << 4), o[0], o[1], o[2], o[3]);
-                    }
+                    for (int i = 0; i < 16; ++i)
+                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[i]) : "f"(__uint_as_float(v[2 * i + 1]) * w.scale), "f"(__uint_as_float(v[2 * i]) * w.scale));
+                    store_warp_box(staging, lane, o, [&] { tma_store_2d(&w.maps.dw, n, m, staging); });
                 } else {
-                    const uint32_t to = staging + static_cast<uint32_t>(parity * 16384 + row * 128);
 #pragma unroll
-                    for (int q = 0; q < 8; ++q) st_shared_16(to + ((q ^ (row & 7)) << 4), v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
-                }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                epilogue_sync();
-                if (leader()) {
-                    if (t.part == 0) {
-                        tma_store_2d(&w.maps.dw, n, m0, staging + static_cast<uint32_t>((c & 1) * 16384));
-                    } else {
-                        // One tile of a launch adds to an element, and launches follow one another: the sum's order is fixed
+                    for (int h = 0; h < 2; ++h) {
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            if (p.add) tma_add_3d(&w.maps.acc, n + 32 * h, m0, t.slot, staging + static_cast<uint32_t>(h * 16384));
-                            else tma_store_3d(&w.maps.acc, n + 32 * h, m0, t.slot, staging + static_cast<uint32_t>(h * 16384));
-                        }
+                        for (int i = 0; i < 16; ++i) o[i] = v[16 * h + i];
+                        const uint32_t box = staging + static_cast<uint32_t>(h * 8 * kWarpBoxBytes);
+                        store_warp_box(box, lane, o, [&] { store_sums(t, n + 16 * h, m, box); }, h == 0);
                     }
-                    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                 }
             }
         }
+        // One tile of a launch adds to an element, and launches follow one another: the sum's order is fixed
+        __device__ void store_sums(const Tile& t, int n, int m, uint32_t box) const {
+            if (w.p.add) tma_add_3d(&w.maps.acc, n, m, t.slot, box);
+            else tma_store_3d(&w.maps.acc, n, m, t.slot, box);
+        }
         __device__ void finish() {
-            if (leader()) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
         }
     };
 };

@@ -9,6 +9,7 @@ namespace sbn {
 struct HeadPlan {
     bool few;                     // head_few_mma.cuh
     bool words;                   // logits by head_words_tcgen05.cuh, gradients as for any number of tokens
+    int tokens, groups, word_pairs;   // words: tokens per tile and groups of them, CTA pairs
     int slabs, ranges, per;       // its gradient kernel: 256-column slabs x ranges of `per` blocks of 16 words
     int bn, parts;                // forward: columns per tile, partial sums per row
     int piece;                    // backward: columns of dz at a time (a multiple of 256)
@@ -53,8 +54,15 @@ static HeadPlan head_plan(int T, int N, int K) {
     h.rows64 = head_up(T, 64);
     h.rows256 = head_up(T, 256);
     h.words = T <= kWordsTokens;
+    if (h.words) {
+        const int tiles = (N + 255) / 256;
+        h.groups = std::max(1, std::min(kBackwardPairs / tiles, (T + 31) / 32));
+        h.tokens = static_cast<int>(head_up((T + h.groups - 1) / h.groups, 32));
+        h.groups = (T + h.tokens - 1) / h.tokens;
+        h.word_pairs = std::min(tiles * h.groups, kBackwardPairs);
+    }
     h.bn = head_tile_columns(T, N, K);
-    h.parts = h.words ? 4 * std::min((N + 127) / 128, kNumSMs) : 2 * ((N + h.bn - 1) / h.bn);
+    h.parts = h.words ? 8 * h.word_pairs : 2 * ((N + h.bn - 1) / h.bn);
     long long cols = (128ll << 20) / (2 * h.rows256);
     cols = std::max(1024ll, cols / 512 * 512);
     const long long pieces = (N + cols - 1) / cols;
@@ -113,23 +121,18 @@ static HeadWs head_ws_layout(const HeadPlan& h, bool backward, int T, int K, int
     return w;
 }
 
-// Results leave in boxes of 128 rows x 128 bytes with the 128-byte swizzle in shared memory, or (wide tiles) 32 rows x 64 bytes with
-// the 64-byte swizzle: dW, bf16 [rows][cols], and the sums of dx, fp32 [slots][rows][cols].
-static bool encode_out(CUtensorMap* map, const void* base, bool bf16, uint64_t cols, uint64_t rows, uint64_t slots, bool wide) {
+// What leaves in boxes of 32 rows x 64 bytes, with the 64-byte swizzle in shared memory: dz and dW, bf16 [rows][cols], and the
+// sums of dx, fp32 [slots][rows][cols].
+static bool encode_out(CUtensorMap* map, const void* base, bool bf16, uint64_t cols, uint64_t rows, uint64_t slots) {
     EncodeTiledFn fn = get_encode_fn();
     if (!fn) return false;
     const uint64_t es = bf16 ? 2 : 4;
     cuuint64_t dims[3] = {cols, rows, slots};
     cuuint64_t strides[2] = {cols * es, cols * es * rows};
-    cuuint32_t box[3] = {static_cast<cuuint32_t>((wide ? 64 : 128) / es), wide ? 32u : 128u, 1};
+    cuuint32_t box[3] = {static_cast<cuuint32_t>(64 / es), 32u, 1};
     cuuint32_t estr[3] = {1, 1, 1};
     return fn(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, bf16 ? 2 : 3, const_cast<void*>(base), dims, strides, box, estr,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, wide ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
-              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-static bool encode_2d_bf16_out(CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, bool wide) { return encode_out(map, base, true, cols, rows, 1, wide); }
-static bool encode_3d_f32_out(CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, uint64_t slots, bool wide) {
-    return encode_out(map, base, false, cols, rows, slots, wide);
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // One call of either operator: top == 0 is the cross entropy.
@@ -149,7 +152,7 @@ struct HeadCall {
 static bool head_encode(const HeadCall& c, const HeadPlan& h, const HeadWs& w, int bn, HeadMaps* maps) {
     const uint64_t k = static_cast<uint64_t>(c.K);
     if (h.words)
-        return encode_2d_bf16_sw128(&maps->x, c.x, k, c.T, k, static_cast<uint32_t>(head_up(c.T, 16))) && encode_2d_bf16_sw128(&maps->w, c.head, k, c.N, k, 128);
+        return encode_2d_bf16_sw128(&maps->x, c.x, k, c.T, k, static_cast<uint32_t>(h.tokens / 2)) && encode_2d_bf16_sw128(&maps->w, c.head, k, c.N, k, 128);
     return encode_2d_bf16_sw128(&maps->x, c.x, k, c.T, k, 128) && encode_2d_bf16_sw128(&maps->xc, c.ws + w.xc, k, h.rows64, k, 128) &&
            encode_2d_bf16_sw128(&maps->w, c.head, k, c.N, k, bn / 2);
 }
@@ -173,9 +176,9 @@ static sbn_status launch_head_logits(const HeadMaps& maps, const HeadLogitsParam
 
 template <int MODE, bool LIST, bool DUAL>
 static sbn_status launch_head_words_as(const HeadMaps& maps, const HeadWordsParams& p, cudaStream_t stream) {
-    if (!ensure_dynamic_smem<head_words_kernel<MODE, LIST, DUAL>>(232448)) return SBN_ERR_CUDA;
-    const int ctas = std::min((p.p.v1 - p.p.v0 + 127) / 128, kNumSMs);
-    if (launch_kernel(head_words_kernel<MODE, LIST, DUAL>, dim3(ctas), dim3(kWordsThreads), words_smem_bytes(p.tok_pad), stream, maps, p) != cudaSuccess)
+    using Loop = PairLoop<HeadWordsWork<MODE, LIST, DUAL>>;
+    if (!ensure_dynamic_smem<head_words_kernel<MODE, LIST, DUAL>>(Loop::kSmemBytes)) return SBN_ERR_CUDA;
+    if (launch_kernel(head_words_kernel<MODE, LIST, DUAL>, dim3(2 * p.pairs), dim3(Loop::kThreads), Loop::kSmemBytes, stream, maps, p) != cudaSuccess)
         return SBN_ERR_CUDA;
     ++g_launch_count;
     return SBN_OK;
@@ -221,12 +224,17 @@ static sbn_status launch_head_losses(const HeadLossJob& j, cudaStream_t stream) 
     ++g_launch_count;
     return SBN_OK;
 }
-static sbn_status launch_head_dx(const HeadDxJob& j, cudaStream_t stream) {
-    const long long steps = (static_cast<long long>(j.T) * (j.K / 4) + kDxThreads - 1) / kDxThreads;
+template <int GROUPS>
+static sbn_status launch_head_dx_as(const HeadDxJob& j, cudaStream_t stream) {
+    constexpr int vecs = kDxThreads / GROUPS;
+    const long long steps = (static_cast<long long>(j.T) * (j.K / 4) + vecs - 1) / vecs;
     const int blocks = static_cast<int>(std::min<long long>(steps, 16ll * device_sm_count()));
-    if (launch_kernel(head_dx_kernel, dim3(blocks), dim3(kDxThreads), 0, stream, j) != cudaSuccess) return SBN_ERR_CUDA;
+    if (launch_kernel(head_dx_kernel<GROUPS>, dim3(blocks), dim3(kDxThreads), 0, stream, j) != cudaSuccess) return SBN_ERR_CUDA;
     ++g_launch_count;
     return SBN_OK;
+}
+static sbn_status launch_head_dx(const HeadDxJob& j, cudaStream_t stream) {
+    return j.slots > 4 ? launch_head_dx_as<8>(j, stream) : launch_head_dx_as<1>(j, stream);
 }
 
 // ---- few tokens ------------------------------------------------------------------------------------
@@ -325,8 +333,7 @@ static sbn_status head_forward(const HeadCall& c, float* loss0, float* loss1, fl
     p.z_ev = reinterpret_cast<float*>(c.ws + w.z_ev);
     p.parts = h.parts;
     p.skip_loads = g_test_break_waits;
-    const int tok_pad = static_cast<int>(head_up(c.T, 16));
-    st = h.words ? launch_head_words<0>(maps, HeadWordsParams{p, tok_pad, words_stages(tok_pad), nullptr, nullptr, HeadScale{}}, list, dual, stream)
+    st = h.words ? launch_head_words<0>(maps, HeadWordsParams{p, h.tokens, h.groups, h.word_pairs, nullptr, nullptr, HeadScale{}}, list, dual, stream)
                  : launch_head_logits<0>(maps, p, list, dual, stream);
     if (st != SBN_OK) return st;
     return launch_head_losses(HeadLossJob{p.tg, p.count, p.row_src, c.T, c.N, p.part, p.part1, p.z_ev, static_cast<const uint16_t*>(c.x),
@@ -352,12 +359,12 @@ static sbn_status head_backward(const HeadCall& c, const float* lse0, const floa
     const uint64_t k = static_cast<uint64_t>(c.K), t = static_cast<uint64_t>(c.T);
     HeadMaps maps;
     HeadGradMaps gm;
-    if (!head_encode(c, h, w, h.bn_piece, &maps) || !encode_out(&maps.dz, c.ws + w.dz, true, h.piece, h.rows256, 1, true)) return SBN_ERR_CUDA;
+    if (!head_encode(c, h, w, h.bn_piece, &maps) || !encode_out(&maps.dz, c.ws + w.dz, true, h.piece, h.rows256, 1)) return SBN_ERR_CUDA;
     const uint32_t blocks = h.wide_grads ? 4 : 2;                       // of 64 columns, in a whole tile's box of B
     bool ok = encode_3d_bf16_blocks(&gm.aw, c.ws + w.dz, h.piece, h.rows256, 2) && encode_2d_bf16_sw128(&gm.ax, c.ws + w.dz, h.piece, h.rows256, h.piece, 128);
     for (int half = 0; ok && half < 2; ++half)
         ok = (h.words || encode_3d_bf16_blocks(&gm.bx[half], c.x, k, t, blocks >> half)) && encode_3d_bf16_blocks(&gm.bxc[half], c.ws + w.xc, k, h.rows64, blocks >> half);
-    ok = ok && (!dx || encode_3d_f32_out(&gm.acc, c.ws + w.acc, k, t, h.slots, h.wide_grads));
+    ok = ok && (!dx || encode_out(&gm.acc, c.ws + w.acc, false, k, t, h.slots));
     if (!ok) return SBN_ERR_CUDA;
     HeadRowsJob rows{};
     if (!h.words) rows.row_of = reinterpret_cast<int*>(c.ws + w.row_of);
@@ -384,12 +391,14 @@ static sbn_status head_backward(const HeadCall& c, const float* lse0, const floa
     q.scale = p.scale;
     q.T = c.T; q.K = c.K;
     q.slot_stages = h.slot_stages;
+    q.want_dx = dx != nullptr;
+    q.want_dw = dhead != nullptr;
     q.skip_loads = g_test_break_waits;
-    const int tiles_k = h.wide_grads ? (c.K + 511) / 512 : (c.K + 255) / 256, tok_pad = static_cast<int>(head_up(c.T, 16));
+    const int tiles_k = h.wide_grads ? (c.K + 511) / 512 : (c.K + 255) / 256;
     for (int v0 = 0; v0 < c.N; v0 += h.piece) {
         const int cols = std::min(h.piece, c.N - v0);
         p.v0 = v0; p.v1 = v0 + cols;
-        st = h.words ? launch_head_words<1>(maps, HeadWordsParams{p, tok_pad, words_stages(tok_pad), static_cast<const uint16_t*>(c.x), reinterpret_cast<uint16_t*>(c.ws + w.xc), rows.scale},
+        st = h.words ? launch_head_words<1>(maps, HeadWordsParams{p, h.tokens, h.groups, h.word_pairs, static_cast<const uint16_t*>(c.x), reinterpret_cast<uint16_t*>(c.ws + w.xc), rows.scale},
                                             list, dual, stream)
                      : launch_head_logits<1>(maps, p, list, dual, stream);
         if (st != SBN_OK) return st;
@@ -398,7 +407,7 @@ static sbn_status head_backward(const HeadCall& c, const float* lse0, const floa
             if (!encode_3d_bf16_blocks(&gm.bw[half], w_rows, k, cols, blocks >> half)) return SBN_ERR_CUDA;
         const int all_stages = (cols + 63) / 64;
         q.cols = cols;
-        if (dhead && !encode_2d_bf16_out(&gm.dw, static_cast<uint16_t*>(dhead) + static_cast<size_t>(v0) * c.K, k, cols, h.wide_grads)) return SBN_ERR_CUDA;
+        if (dhead && !encode_out(&gm.dw, static_cast<uint16_t*>(dhead) + static_cast<size_t>(v0) * c.K, true, k, cols, 1)) return SBN_ERR_CUDA;
         q.add = v0 > 0;
         const int slices = (all_stages + h.slot_stages - 1) / h.slot_stages;     // fewer in a short last piece
         const int tiles[2] = {dhead ? (cols + 255) / 256 * tiles_k : 0, dx ? static_cast<int>(h.rows256 / 256) * tiles_k * slices : 0};

@@ -230,11 +230,11 @@ head_rows_kernel(const HeadRowsJob j, const int per) {
             // the rows that count, 16 bytes at a time, one row after another
             __syncthreads();
             const int vecs = j.K >> 3;
-            for (int i = 0; i < all; ++i) {
-                const int src = j.row_src[before + i];
-                const uint4* from = reinterpret_cast<const uint4*>(j.x + static_cast<size_t>(src) * j.K);
-                uint4* to = reinterpret_cast<uint4*>(j.xc + static_cast<size_t>(before + i) * j.K);
-                for (int v = tid; v < vecs; v += kRowsThreads) to[v] = __ldg(from + v);
+            uint4* to = reinterpret_cast<uint4*>(j.xc + static_cast<size_t>(before) * j.K);
+#pragma unroll 4
+            for (int v = tid; v < all * vecs; v += kRowsThreads) {           // at most 256 rows of 2^20 values: below 2^25
+                const int i = v / vecs;
+                to[v] = __ldg(reinterpret_cast<const uint4*>(j.x + static_cast<size_t>(j.row_src[before + i]) * j.K) + (v - i * vecs));
             }
         }
         before += all;
@@ -281,9 +281,11 @@ head_losses_kernel(const HeadLossJob j) {
         }
         const size_t p0 = static_cast<size_t>(r) * j.parts;
         float m = -INFINITY;
+#pragma unroll 8
         for (int i = lane; i < j.parts; i += 32) m = fmaxf(m, j.part[p0 + i].x);
         m = warp_max(m);
         double s0 = 0.0, s1 = 0.0;
+#pragma unroll 4
         for (int i = lane; i < j.parts; i += 32) {            // parts without columns of the vocabulary hold (-inf, 0)
             const float2 v = j.part[p0 + i];
             s0 += static_cast<double>(v.y) * static_cast<double>(expf((v.x - m) * static_cast<float>(j.inv_tau)));
@@ -301,6 +303,7 @@ head_losses_kernel(const HeadLossJob j) {
             const uint4* a = reinterpret_cast<const uint4*>(j.x + static_cast<size_t>(t) * j.K);
             const uint4* b = reinterpret_cast<const uint4*>(j.w + static_cast<size_t>(j.tg.labels[t]) * j.K);
             float lo = 0.0f, hi = 0.0f;
+#pragma unroll 4
             for (int i = lane; i < j.K >> 3; i += 32) {
                 const uint4 u = __ldg(a + i), v = __ldg(b + i);
                 lo = fmaf(bf16lo_to_f32(u.x), bf16lo_to_f32(v.x), lo); hi = fmaf(bf16hi_to_f32(u.x), bf16hi_to_f32(v.x), hi);
@@ -360,31 +363,51 @@ struct HeadDxJob {
 
 constexpr int kDxThreads = 256;
 
+// GROUPS threads per 4 values, each with every GROUPS-th slot; their sums are added in the groups' order.
+template <int GROUPS>
 __global__ void __launch_bounds__(kDxThreads)
 head_dx_kernel(const HeadDxJob j) {
+    constexpr int kVecs = kDxThreads / GROUPS;    // of a CTA and step
+    __shared__ float4 s_sum[GROUPS > 1 ? kDxThreads : 1];
     pdl_launch_dependents();
     pdl_wait();
-    const int vecs = j.K >> 2;                    // 4 values per thread and step
+    const int vecs = j.K >> 2, group = threadIdx.x / kVecs, mine = threadIdx.x % kVecs;
     const long long all = static_cast<long long>(j.T) * vecs;
     const size_t slot = static_cast<size_t>(j.T) * j.K;
     const float scale = *j.scale;
-    for (long long i = static_cast<long long>(blockIdx.x) * kDxThreads + threadIdx.x; i < all; i += static_cast<long long>(gridDim.x) * kDxThreads) {
+    for (long long first = static_cast<long long>(blockIdx.x) * kVecs; first < all; first += static_cast<long long>(gridDim.x) * kVecs) {
+        const long long i = first + mine;
         const int t = static_cast<int>(i / vecs), c = static_cast<int>(i - static_cast<long long>(t) * vecs);
-        const int r = j.row_of != nullptr ? j.row_of[t] : t;
         float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if (r >= 0) {
-            const float* a = j.acc + static_cast<size_t>(r) * j.K + 4 * c;
+        if (i < all) {
+            const int r = j.row_of != nullptr ? j.row_of[t] : t;
+            if (r >= 0) {
+                const float* a = j.acc + static_cast<size_t>(r) * j.K + 4 * c;
 #pragma unroll 8
-            for (int s = 0; s < j.slots; ++s) {
-                const float4 o = *reinterpret_cast<const float4*>(a + s * slot);
-                v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
+                for (int s = group; s < j.slots; s += GROUPS) {
+                    const float4 o = *reinterpret_cast<const float4*>(a + s * slot);
+                    v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
+                }
             }
         }
-        v.x *= scale; v.y *= scale; v.z *= scale; v.w *= scale;
-        uint2 o;
-        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o.x) : "f"(v.y), "f"(v.x));
-        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o.y) : "f"(v.w), "f"(v.z));
-        *reinterpret_cast<uint2*>(j.dx + static_cast<size_t>(t) * j.K + 4 * c) = o;
+        if constexpr (GROUPS > 1) {
+            s_sum[threadIdx.x] = v;
+            __syncthreads();
+            if (group == 0) {
+#pragma unroll
+                for (int g = 1; g < GROUPS; ++g) {
+                    const float4 o = s_sum[g * kVecs + mine];
+                    v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
+                }
+            }
+            __syncthreads();
+        }
+        if (group == 0 && i < all) {
+            uint2 o;
+            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o.x) : "f"(v.y * scale), "f"(v.x * scale));
+            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o.y) : "f"(v.w * scale), "f"(v.z * scale));
+            *reinterpret_cast<uint2*>(j.dx + static_cast<size_t>(t) * j.K + 4 * c) = o;
+        }
     }
 }
 
