@@ -142,7 +142,7 @@ def _stream():
 
 _NATIVE_CALLS = ["sbn_quant_act", "sbn_quant_act_expand68", "sbn_norm_quant_act", "sbn_norm_quant_act_expand68", "sbn_sparse_bitlinear",
                  "sbn_bitlinear", "sbn_sparse_bitlinear_packed", "sbn_quant_act_sparse_bitlinear", "sbn_quant_act_bitlinear",
-                 "sbn_head_cross_entropy", "sbn_head_cross_entropy_backward", "sbn_head_distill", "sbn_head_distill_backward"]
+                 "sbn_head_cross_entropy", "sbn_head_cross_entropy_backward", "sbn_head_distill", "sbn_head_distill_backward", "sbn_head_workspace_bytes"]
 
 
 def _load_native():
@@ -411,7 +411,7 @@ def alloc_gemm_ws(op: int, T: int, N: int, K: int, device="cuda"):
 
 def alloc_head_ws(T: int, N: int, K: int, top: int = 0, backward: bool = False, device="cuda"):
     """Workspace of a call at the output head (top = 0: cross entropy); its contents need no initialisation."""
-    n = sbn_head_workspace_bytes(T, N, K, top, backward)
+    n = _native.head_workspace_bytes(T, N, K, top, backward) if _native else sbn_head_workspace_bytes(T, N, K, top, backward)
     if n == 0:
         raise ValueError(f"unsupported sizes T = {T}, N = {N}, K = {K}, top = {top}")
     return torch.empty(n, dtype=torch.uint8, device=device)

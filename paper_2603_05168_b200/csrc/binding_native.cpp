@@ -21,6 +21,7 @@ decltype(&sbn_bitlinear) f_bitlinear;
 decltype(&sbn_sparse_bitlinear_packed) f_sparse_bitlinear_packed;
 decltype(&sbn_quant_act_sparse_bitlinear) f_quant_act_sparse_bitlinear;
 decltype(&sbn_quant_act_bitlinear) f_quant_act_bitlinear;
+decltype(&sbn_head_workspace_bytes) f_head_workspace_bytes;
 decltype(&sbn_head_cross_entropy) f_head_cross_entropy;
 decltype(&sbn_head_cross_entropy_backward) f_head_cross_entropy_backward;
 decltype(&sbn_head_distill) f_head_distill;
@@ -310,6 +311,18 @@ struct TeacherArgs {
     }
 };
 
+// (T, N, K, top, backward)
+PyObject* py_head_workspace_bytes(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!expect(n, 5)) return nullptr;
+    long long v[4];
+    for (int i = 0; i < 4; ++i) {
+        v[i] = PyLong_AsLongLong(a[i]);
+        if (v[i] == -1 && PyErr_Occurred()) return nullptr;
+        if (v[i] < 0 || v[i] > (1ll << 30)) return PyLong_FromLong(0);       // refused sizes
+    }
+    return PyLong_FromSize_t(f_head_workspace_bytes(PyObject_IsTrue(a[4]), static_cast<int>(v[0]), static_cast<int>(v[1]), static_cast<int>(v[2]), static_cast<int>(v[3])));
+}
+
 // (x, head, labels, loss, lse, ws)
 PyObject* py_head_cross_entropy(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!expect(n, 6)) return nullptr;
@@ -380,7 +393,7 @@ PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
         !take(d, "sbn_quant_act_sparse_bitlinear", f_quant_act_sparse_bitlinear) ||
         !take(d, "sbn_quant_act_bitlinear", f_quant_act_bitlinear) || !take(d, "sbn_head_cross_entropy", f_head_cross_entropy) ||
         !take(d, "sbn_head_cross_entropy_backward", f_head_cross_entropy_backward) || !take(d, "sbn_head_distill", f_head_distill) ||
-        !take(d, "sbn_head_distill_backward", f_head_distill_backward))
+        !take(d, "sbn_head_distill_backward", f_head_distill_backward) || !take(d, "sbn_head_workspace_bytes", f_head_workspace_bytes))
         return nullptr;
     keep(g_bfloat16, a[1]);
     keep(g_get_device, a[2]);
@@ -395,7 +408,7 @@ PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyMethodDef methods[] = {
     SBN_METHOD(bind), SBN_METHOD(quant_act), SBN_METHOD(norm_quant_act), SBN_METHOD(sparse_bitlinear), SBN_METHOD(bitlinear),
     SBN_METHOD(sparse_bitlinear_packed), SBN_METHOD(quant_act_sparse_bitlinear), SBN_METHOD(quant_act_bitlinear),
-    SBN_METHOD(head_cross_entropy), SBN_METHOD(head_cross_entropy_backward), SBN_METHOD(head_distill), SBN_METHOD(head_distill_backward),
+    SBN_METHOD(head_workspace_bytes), SBN_METHOD(head_cross_entropy), SBN_METHOD(head_cross_entropy_backward), SBN_METHOD(head_distill), SBN_METHOD(head_distill_backward),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_sbn_native", "Tensor arguments to the C ABI of libsbn.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 

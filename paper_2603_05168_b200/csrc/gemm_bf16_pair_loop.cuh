@@ -18,7 +18,8 @@
 //                chunks of 32; wide: accumulator sub / 2, columns 128 (sub % 2) .., that is 128 (sub / 2) + 256 (sub % 2) .. of the tile)
 //
 // A `Work` has the kernel's parameters and gives
-//   kWide, kStages, kStagingBytes  shape, stages, and shared memory behind them for the epilogue
+//   kWide, kStages, kStagingBytes  shape, stages of kStageBytes, and shared memory behind them for the epilogue
+//   stages(), stage_bytes()        the same, or more and smaller stages where a tile has few columns
 //   start()                        what it reads from memory for itself, after the dependency wait
 //   Tile                           a tile: at least { int k_stages; int bn; }
 //   Tiles(work, pair)              the tiles of a CTA pair in order: bool next(Tile&)
@@ -61,7 +62,8 @@ __host__ __device__ constexpr uint32_t make_idesc_bf16_any(int mma_m, int mma_n,
 
 template <class Work>
 __device__ __forceinline__ void bf16_pair_loop(Work& work, const bool skip_loads) {
-    constexpr int STAGES = Work::kStages, STAGE_BYTES = PairLoop<Work>::kStageBytes, EPI_WARPS = PairLoop<Work>::kEpiWarps;
+    constexpr int EPI_WARPS = PairLoop<Work>::kEpiWarps;
+    const int STAGES = work.stages(), STAGE_BYTES = work.stage_bytes();
     constexpr bool WIDE = Work::kWide;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = smem_u32(smem_raw);
@@ -69,7 +71,7 @@ __device__ __forceinline__ void bf16_pair_loop(Work& work, const bool skip_loads
         if (threadIdx.x == 0) atomicExch(&g_device_status, static_cast<int>(SBN_ERR_CUDA));
         return;
     }
-    const uint32_t staging = smem_base + STAGES * STAGE_BYTES;
+    const uint32_t staging = smem_base + static_cast<uint32_t>(STAGES * STAGE_BYTES);
     const uint32_t bar_full = staging + Work::kStagingBytes;
     const uint32_t bar_empty = bar_full + 8 * STAGES;
     const uint32_t bar_acc_full = bar_empty + 8 * STAGES;     // [2]
@@ -122,7 +124,7 @@ __device__ __forceinline__ void bf16_pair_loop(Work& work, const bool skip_loads
                     const uint32_t full_leader = map_to_cta(bar_full + 8 * stage, 0);
                     if (rank == 0) mbar_expect_tx(bar_full + 8 * stage, 2 * bytes_per_cta);
                     // rows or columns beyond the tensors are zero-filled by the hardware and still count their full size
-                    work.load(t, ks, rank, smem_base + stage * STAGE_BYTES, full_leader);
+                    work.load(t, ks, rank, smem_base + static_cast<uint32_t>(stage * STAGE_BYTES), full_leader);
                     if (++stage == STAGES) { stage = 0; phase ^= 1u; }
                 }
             }
@@ -147,7 +149,7 @@ __device__ __forceinline__ void bf16_pair_loop(Work& work, const bool skip_loads
                 for (int ks = 0; ks < t.k_stages; ++ks) {
                     if (!mbar_wait(bar_full + 8 * stage, phase, abort_flag)) { ok = false; break; }
                     tcgen05_fence_after();
-                    const uint32_t st = smem_base + stage * STAGE_BYTES;
+                    const uint32_t st = smem_base + static_cast<uint32_t>(stage * STAGE_BYTES);
                     const uint64_t a_desc = work.a_desc(t, st), b_desc = work.b_desc(t, st + kPairLoopStageA);
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {

@@ -23,8 +23,13 @@ static inline bool head_few_takes(int T, int K) { return T <= 8 ? K <= 4096 : T 
 constexpr int kFewHeadWarps = 16;
 constexpr int kFewHeadThreads = 32 * kFewHeadWarps;
 
+// Up to this many entries per token every CTA sorts the targets itself (16 tokens x 65 entries: 130 comparisons per thread), which
+// saves the launch of a kernel that takes 4 us; CTA 0 leaves them in memory for the kernels behind it.
+constexpr int kFewOwnEvents = 65;
+
 struct HeadFewParams {
     HeadTargets tg;
+    HeadTargetsJob job;           // index null: the targets are in memory
     const uint16_t* x;            // [T][K]
     const uint16_t* w;            // [N][K]
     int T, N, K;
@@ -68,6 +73,8 @@ head_few_kernel(const HeadFewParams p) {
     constexpr int kTok = 8 * NT;
     __shared__ float s_part[kFewHeadWarps][16][kTok];
     __shared__ int s_col[LIST ? kTok : 1][LIST ? kHeadMaxTop + 1 : 1];
+    __shared__ float s_w[LIST ? kTok : 1][LIST ? kFewOwnEvents : 1];
+    __shared__ int s_flags[kTok];
     pdl_launch_dependents();
     pdl_wait();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
@@ -86,11 +93,40 @@ head_few_kernel(const HeadFewParams p) {
 #pragma unroll
     for (int i = 0; i < KBW; ++i) load_block(i, blockIdx.x);
 
+    const bool own = LIST && p.job.index != nullptr;
+    if (own) {
+        if (warp < p.T) {
+            // (the room of the parts, which nobody has yet)
+            int* col = reinterpret_cast<int*>(&s_part[0][0][0]) + warp * 2 * kFewOwnEvents;
+            const int flags = warp_targets(p.job, warp, lane, col, reinterpret_cast<float*>(col + kFewOwnEvents), [&](int place, int c, float v) {
+                s_col[LIST ? warp : 0][place] = c;
+                s_w[LIST ? warp : 0][place] = v;
+                if (blockIdx.x == 0) {
+                    p.job.ev_col[warp * p.tg.events + place] = c;
+                    p.job.ev_w[warp * p.tg.events + place] = v;
+                }
+            });
+            if (lane == 0) {
+                s_flags[warp] = flags;
+                if (blockIdx.x == 0) {
+                    p.job.flags[warp] = static_cast<unsigned char>(flags);
+                    report_bad(flags);
+                }
+            }
+        }
+    } else if (tid < p.T) {
+        s_flags[tid] = head_token_flags(p.tg, tid, p.N);
+    }
+    if (LIST && !own) {
+        for (int i = tid; i < p.T * p.tg.events; i += kFewHeadThreads) s_col[i / p.tg.events][i % p.tg.events] = p.tg.ev_col[i];
+    }
+    __syncthreads();
+
     uint4 x[KBW][NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         const int t = nt * 8 + g;
-        const bool there = t < p.T && (head_token_flags(p.tg, t, p.N) & (kRowDistill | kRowLabel));
+        const bool there = t < p.T && (s_flags[t] & (kRowDistill | kRowLabel));
 #pragma unroll
         for (int i = 0; i < KBW; ++i) {
             const int kb = warp + kFewHeadWarps * i;
@@ -98,13 +134,10 @@ head_few_kernel(const HeadFewParams p) {
             if (there && kb < kbs) x[i][nt] = __ldg(reinterpret_cast<const uint4*>(p.x + static_cast<size_t>(t) * p.K + kb * 32 + t4 * 8));
         }
     }
-    if constexpr (LIST) {
-        for (int i = tid; i < p.T * p.tg.events; i += kFewHeadThreads) s_col[i / p.tg.events][i % p.tg.events] = p.tg.ev_col[i];
-    }
     // the word and token of this thread in every block
     const int tok = tid % kTok, slot = tid / kTok;
     const bool mine = slot < 16 && tok < p.T;
-    const int flags = mine ? head_token_flags(p.tg, tok, p.N) : 0;
+    const int flags = mine ? s_flags[tok] : 0;
     const bool asked = (flags & (kRowDistill | kRowLabel)) != 0;
     const int label = !LIST && asked ? static_cast<int>(p.tg.labels[tok]) : -1;
     constexpr float kLog2e = 1.4426950408889634f;
@@ -112,7 +145,7 @@ head_few_kernel(const HeadFewParams p) {
     float l0 = -INFINITY, l1 = -INFINITY, g0 = 0.0f, g1 = 0.0f;
     if constexpr (MODE == 1) {
         if (!LIST && blockIdx.x == 0 && mine) report_bad(flags);
-        const float unit = head_scale_unit(warp_max(lane < p.T ? head_scale_share(p.scale, p.tg, lane, p.N) : 0.0f));
+        const float unit = head_scale_unit(warp_max(lane < p.T ? head_scale_share(p.scale, LIST, s_flags[lane], lane) : 0.0f));
         const float inv_scale = 1.0f / unit;
         if (blockIdx.x == 0 && tid == 0) p.scale.out[0] = unit;
         if (LIST ? (flags & kRowDistill) != 0 : asked) {
@@ -170,7 +203,7 @@ head_few_kernel(const HeadFewParams p) {
                         if (MODE == 0) {
                             p.z_ev[at] = z;
                         } else {
-                            const float q = p.tg.ev_w[at];
+                            const float q = own ? s_w[tok][lo] : p.tg.ev_w[at];
                             v -= q < 0.0f ? g1 : q * g0;
                         }
                     }

@@ -39,11 +39,12 @@ __device__ __forceinline__ void tma_add_3d(const CUtensorMap* map, int c0, int c
 }
 
 // 32 rows x 64 bytes of a warp (lane = row) through kWarpBoxBytes of shared memory of its own: the 16-byte pieces q of a row at
-// q ^ (row / 2 % 4), as the 64-byte swizzle has them; store() issues the TMA store.  Waits for the warp's stores before it to be read out.
+// q ^ (row / 2 % 4), as the 64-byte swizzle has them; store() issues the TMA store.  Waits until no more than
+// PENDING stores of the warp are still to be read out: one box, or two in turn.
 constexpr int kWarpBoxBytes = 2048;
-template <class Store>
-__device__ __forceinline__ void store_warp_box(uint32_t box, int lane, const uint32_t (&v)[16], Store&& store, bool wait = true) {
-    if (wait && lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+template <int PENDING = 0, class Store>
+__device__ __forceinline__ void store_warp_box(uint32_t box, int lane, const uint32_t (&v)[16], Store&& store) {
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(PENDING) : "memory");
     __syncwarp();
     const uint32_t to = box + static_cast<uint32_t>(lane * 64), x = static_cast<uint32_t>(lane >> 1) & 3u;
 #pragma unroll
@@ -229,6 +230,8 @@ template <int MODE, bool LIST, bool DUAL>
 struct HeadLogitsWork {
     static constexpr bool kWide = false;
     static constexpr int kStages = MODE == 0 ? 7 : 6, kStagingBytes = MODE == 0 ? 0 : 8 * kWarpBoxBytes;
+    __device__ static constexpr int stages() { return kStages; }
+    __device__ static constexpr int stage_bytes() { return PairLoop<HeadLogitsWork>::kStageBytes; }
     const HeadMaps& maps;
     const HeadLogitsParams& p;
     int rows, tiles_m, tiles_v;
@@ -363,6 +366,8 @@ template <bool WIDE>
 struct HeadGradsWork {
     static constexpr bool kWide = WIDE;
     static constexpr int kStages = WIDE ? 4 : 6, kStagingBytes = 16 * kWarpBoxBytes, kTileCols = WIDE ? 512 : 256;
+    __device__ static constexpr int stages() { return kStages; }
+    __device__ static constexpr int stage_bytes() { return PairLoop<HeadGradsWork>::kStageBytes; }
     const HeadGradMaps& maps;
     const HeadGradParams& p;
     int rows;
@@ -553,14 +558,15 @@ struct HeadGradsWork {
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
                         asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[i]) : "f"(__uint_as_float(v[2 * i + 1]) * w.scale), "f"(__uint_as_float(v[2 * i]) * w.scale));
-                    store_warp_box(staging, lane, o, [&] { tma_store_2d(&w.maps.dw, n, m, staging); });
+                    const uint32_t box = staging + static_cast<uint32_t>(((c >> 1) & 1) * 8 * kWarpBoxBytes);
+                    store_warp_box<1>(box, lane, o, [&] { tma_store_2d(&w.maps.dw, n, m, box); });
                 } else {
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
 #pragma unroll
                         for (int i = 0; i < 16; ++i) o[i] = v[16 * h + i];
                         const uint32_t box = staging + static_cast<uint32_t>(h * 8 * kWarpBoxBytes);
-                        store_warp_box(box, lane, o, [&] { store_sums(t, n + 16 * h, m, box); }, h == 0);
+                        store_warp_box<1>(box, lane, o, [&] { store_sums(t, n + 16 * h, m, box); });
                     }
                 }
             }

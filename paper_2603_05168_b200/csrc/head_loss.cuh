@@ -177,8 +177,8 @@ static sbn_status launch_head_logits(const HeadMaps& maps, const HeadLogitsParam
 template <int MODE, bool LIST, bool DUAL>
 static sbn_status launch_head_words_as(const HeadMaps& maps, const HeadWordsParams& p, cudaStream_t stream) {
     using Loop = PairLoop<HeadWordsWork<MODE, LIST, DUAL>>;
-    if (!ensure_dynamic_smem<head_words_kernel<MODE, LIST, DUAL>>(Loop::kSmemBytes)) return SBN_ERR_CUDA;
-    if (launch_kernel(head_words_kernel<MODE, LIST, DUAL>, dim3(2 * p.pairs), dim3(Loop::kThreads), Loop::kSmemBytes, stream, maps, p) != cudaSuccess)
+    if (!ensure_dynamic_smem<head_words_kernel<MODE, LIST, DUAL>>(232448)) return SBN_ERR_CUDA;
+    if (launch_kernel(head_words_kernel<MODE, LIST, DUAL>, dim3(2 * p.pairs), dim3(Loop::kThreads), words_smem_bytes(p.tokens), stream, maps, p) != cudaSuccess)
         return SBN_ERR_CUDA;
     ++g_launch_count;
     return SBN_OK;
@@ -190,16 +190,21 @@ static sbn_status launch_head_words(const HeadMaps& maps, const HeadWordsParams&
 }
 
 // What is asked of the tokens: the labels themselves, or for a distillation the sorted targets of every token.
-static sbn_status launch_head_targets(const HeadCall& c, const HeadWs& w, HeadTargets* tg, cudaStream_t stream) {
+// `later`: the job for a kernel that does it itself.
+static sbn_status launch_head_targets(const HeadCall& c, const HeadWs& w, HeadTargets* tg, cudaStream_t stream, HeadTargetsJob* later = nullptr) {
     *tg = HeadTargets{c.labels, nullptr, nullptr, nullptr, 1};
     if (!c.top) return SBN_OK;
     HeadTargetsJob t{c.top_index, c.top_logits, c.top_bf16, c.top, c.T, c.N, static_cast<float>(1.0 / static_cast<double>(c.tau)), c.labels,
                      reinterpret_cast<unsigned char*>(c.ws + w.flags), reinterpret_cast<int*>(c.ws + w.ev_col),
                      reinterpret_cast<float*>(c.ws + w.ev_w)};
+    *tg = HeadTargets{c.labels, t.flags, t.ev_col, t.ev_w, c.top + (c.labels ? 1 : 0)};
+    if (later && tg->events <= kFewOwnEvents) {
+        *later = t;
+        return SBN_OK;
+    }
     const int blocks = std::min((c.T + kTargetWarps - 1) / kTargetWarps, 16 * device_sm_count());
     if (launch_kernel(head_targets_kernel, dim3(blocks), dim3(32 * kTargetWarps), 0, stream, t) != cudaSuccess) return SBN_ERR_CUDA;
     ++g_launch_count;
-    *tg = HeadTargets{c.labels, t.flags, t.ev_col, t.ev_w, c.top + (c.labels ? 1 : 0)};
     return SBN_OK;
 }
 
@@ -219,8 +224,8 @@ static sbn_status launch_head_rows(const HeadCall& c, const HeadWs& w, HeadRowsJ
 }
 
 static sbn_status launch_head_losses(const HeadLossJob& j, cudaStream_t stream) {
-    const int blocks = std::min((j.T + kLossWarps - 1) / kLossWarps, 8 * device_sm_count());
-    if (launch_kernel(head_losses_kernel, dim3(blocks), dim3(32 * kLossWarps), 0, stream, j) != cudaSuccess) return SBN_ERR_CUDA;
+    const int blocks = std::min(j.T, 16 * device_sm_count());
+    if (launch_kernel(head_losses_kernel, dim3(blocks), dim3(kLossThreads), 0, stream, j) != cudaSuccess) return SBN_ERR_CUDA;
     ++g_launch_count;
     return SBN_OK;
 }
@@ -269,10 +274,12 @@ static HeadFewParams head_few_params(const HeadCall& c, const HeadTargets& tg) {
 static sbn_status head_few_forward(const HeadCall& c, const HeadPlan& h, float* loss0, float* loss1, float* lse0, float* lse1, cudaStream_t stream) {
     const HeadWs w = head_ws_layout(h, false, c.T, c.K, c.top);
     HeadTargets tg;
-    sbn_status st = launch_head_targets(c, w, &tg, stream);
+    HeadTargetsJob job{};
+    sbn_status st = launch_head_targets(c, w, &tg, stream, &job);
     if (st != SBN_OK) return st;
     const bool list = c.top != 0, dual = list && c.labels;
     HeadFewParams p = head_few_params(c, tg);
+    p.job = job;
     p.part = reinterpret_cast<float2*>(c.ws + w.part);
     p.part1 = dual ? reinterpret_cast<float*>(c.ws + w.part1) : nullptr;
     p.z_ev = reinterpret_cast<float*>(c.ws + w.z_ev);
@@ -286,10 +293,12 @@ static sbn_status head_few_backward(const HeadCall& c, const HeadPlan& h, const 
                                     void* dhead, cudaStream_t stream) {
     const HeadWs w = head_ws_layout(h, true, c.T, c.K, c.top);
     HeadTargets tg;
-    sbn_status st = launch_head_targets(c, w, &tg, stream);
+    HeadTargetsJob job{};
+    sbn_status st = launch_head_targets(c, w, &tg, stream, &job);
     if (st != SBN_OK) return st;
     const bool list = c.top != 0, dual = list && c.labels;
     HeadFewParams p = head_few_params(c, tg);
+    p.job = job;
     p.lse0 = lse0; p.lse1 = lse1;
     p.scale = HeadScale{g0, g1, p.inv_tau, reinterpret_cast<float*>(c.ws + w.scale)};
     p.dz = reinterpret_cast<uint16_t*>(c.ws + w.dz);
@@ -333,7 +342,7 @@ static sbn_status head_forward(const HeadCall& c, float* loss0, float* loss1, fl
     p.z_ev = reinterpret_cast<float*>(c.ws + w.z_ev);
     p.parts = h.parts;
     p.skip_loads = g_test_break_waits;
-    st = h.words ? launch_head_words<0>(maps, HeadWordsParams{p, h.tokens, h.groups, h.word_pairs, nullptr, nullptr, HeadScale{}}, list, dual, stream)
+    st = h.words ? launch_head_words<0>(maps, HeadWordsParams{p, words_stages(h.tokens), h.tokens, h.groups, h.word_pairs, nullptr, nullptr, HeadScale{}}, list, dual, stream)
                  : launch_head_logits<0>(maps, p, list, dual, stream);
     if (st != SBN_OK) return st;
     return launch_head_losses(HeadLossJob{p.tg, p.count, p.row_src, c.T, c.N, p.part, p.part1, p.z_ev, static_cast<const uint16_t*>(c.x),
@@ -398,7 +407,7 @@ static sbn_status head_backward(const HeadCall& c, const float* lse0, const floa
     for (int v0 = 0; v0 < c.N; v0 += h.piece) {
         const int cols = std::min(h.piece, c.N - v0);
         p.v0 = v0; p.v1 = v0 + cols;
-        st = h.words ? launch_head_words<1>(maps, HeadWordsParams{p, h.tokens, h.groups, h.word_pairs, static_cast<const uint16_t*>(c.x), reinterpret_cast<uint16_t*>(c.ws + w.xc), rows.scale},
+        st = h.words ? launch_head_words<1>(maps, HeadWordsParams{p, words_stages(h.tokens), h.tokens, h.groups, h.word_pairs, static_cast<const uint16_t*>(c.x), reinterpret_cast<uint16_t*>(c.ws + w.xc), rows.scale},
                                             list, dual, stream)
                      : launch_head_logits<1>(maps, p, list, dual, stream);
         if (st != SBN_OK) return st;

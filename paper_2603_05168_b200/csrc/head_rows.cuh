@@ -59,11 +59,10 @@ struct HeadScale {
     float inv_tau;
     float* out;                                   // [2]
 };
-// A thread's share of the maximum: tokens tid, tid + threads, ...; those that nothing is asked of do not count.
-__device__ __forceinline__ float head_scale_share(const HeadScale& s, const HeadTargets& tg, int t, int N) {
-    const int flags = head_token_flags(tg, t, N);
+// A token's part in the maximum; what is not asked of it does not count.
+__device__ __forceinline__ float head_scale_share(const HeadScale& s, bool distill, int flags, int t) {
     float m = 0.0f;
-    if (tg.flags == nullptr ? (flags & kRowLabel) : (flags & kRowDistill)) m = fabsf(s.g0[t]) * s.inv_tau;
+    if (flags & (distill ? kRowDistill : kRowLabel)) m = fabsf(s.g0[t]) * s.inv_tau;
     if (s.g1 != nullptr && (flags & kRowLabel)) m = fmaxf(m, fabsf(s.g1[t]));
     return m;
 }
@@ -80,10 +79,58 @@ struct HeadTargetsJob {
     float* ev_w;
 };
 
+// A token's targets, by a warp: flags; put(place, column, weight) gets the entries in order.  col, val: shared memory for top + 1
+// and top entries.  The place of an entry is the number of entries before it (column, then position): top is at most 256, so
+// counting costs less than a sorting network's exchanges would.
+template <class Put>
+__device__ __forceinline__ int warp_targets(const HeadTargetsJob& j, long long t, int lane, int* col, float* val, Put&& put) {
+    const int events = j.top + (j.labels != nullptr ? 1 : 0);
+    const long long* index = j.index + t * j.top;
+    float top_val = -INFINITY;
+    int bad = 0, any = 0;
+    for (int i = lane; i < j.top; i += 32) {
+        const long long c = index[i];
+        const float l = j.logits_bf16 ? __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t*>(j.logits)[t * j.top + i]) << 16)
+                                      : static_cast<const float*>(j.logits)[t * j.top + i];
+        const bool there = c >= 0 && c < j.N;
+        bad |= c >= j.N;
+        any |= there && !(l == -INFINITY);                   // a NaN counts, and shows in the loss
+        col[i] = there ? static_cast<int>(c) : kNoColumn;
+        val[i] = there ? l : -INFINITY;
+        if (there) top_val = fmaxf(top_val, l);
+    }
+    top_val = warp_max(top_val);
+    bad = __any_sync(0xFFFFFFFFu, bad);
+    any = __any_sync(0xFFFFFFFFu, any) && !bad;
+    float sum = 0.0f;
+    for (int i = lane; i < j.top; i += 32) {
+        // the difference first: the type's lowest value, divided by a small temperature, would become -inf
+        const float e = val[i] == -INFINITY ? 0.0f : expf((val[i] - top_val) * j.inv_tau);
+        val[i] = e;
+        sum += e;
+        if (!any) col[i] = kNoColumn;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+    int flags = (any ? kRowDistill : 0) | (bad ? kRowBadTeacher : 0);
+    if (j.labels != nullptr) {
+        const long long y = j.labels[t];
+        flags |= y < 0 ? 0 : (y < j.N ? kRowLabel : kRowBadLabel);
+        if (lane == 0) col[j.top] = (flags & kRowLabel) ? static_cast<int>(y) : kNoColumn;
+    }
+    __syncwarp();
+    for (int i = lane; i < events; i += 32) {
+        const int c = col[i];
+        int place = 0;
+        for (int o = 0; o < events; ++o) place += (col[o] < c || (col[o] == c && o < i)) ? 1 : 0;
+        put(place, c, i == j.top ? -1.0f : (c == kNoColumn ? 0.0f : val[i] / sum));
+    }
+    return flags;
+}
+
 constexpr int kTargetWarps = 4;
 
-// A warp per token.  The rank of an entry is the number of entries before it (column, then position): top is at most 256,
-// so counting costs less than a sorting network's exchanges would.
+// A warp per token.
 __global__ void __launch_bounds__(32 * kTargetWarps)
 head_targets_kernel(const HeadTargetsJob j) {
     __shared__ int s_col[kTargetWarps][kHeadMaxTop + 1];
@@ -91,56 +138,14 @@ head_targets_kernel(const HeadTargetsJob j) {
     pdl_launch_dependents();
     pdl_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    int* col = s_col[warp];
-    float* val = s_val[warp];
     const int events = j.top + (j.labels != nullptr ? 1 : 0);
     for (long long t = static_cast<long long>(blockIdx.x) * kTargetWarps + warp; t < j.T; t += static_cast<long long>(gridDim.x) * kTargetWarps) {
-        const long long* index = j.index + t * j.top;
-        float top_val = -INFINITY;
-        int bad = 0, any = 0;
-        for (int i = lane; i < j.top; i += 32) {
-            const long long c = index[i];
-            const float l = j.logits_bf16 ? __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t*>(j.logits)[t * j.top + i]) << 16)
-                                          : static_cast<const float*>(j.logits)[t * j.top + i];
-            const bool there = c >= 0 && c < j.N;
-            bad |= c >= j.N;
-            any |= there && !(l == -INFINITY);               // a NaN counts, and shows in the loss
-            col[i] = there ? static_cast<int>(c) : kNoColumn;
-            val[i] = there ? l : -INFINITY;
-            if (there) top_val = fmaxf(top_val, l);
-        }
-        top_val = warp_max(top_val);
-        bad = __any_sync(0xFFFFFFFFu, bad);
-        any = __any_sync(0xFFFFFFFFu, any) && !bad;
-        float sum = 0.0f;
-        for (int i = lane; i < j.top; i += 32) {
-            // the difference first: the type's lowest value, divided by a small temperature, would become -inf
-            const float e = val[i] == -INFINITY ? 0.0f : expf((val[i] - top_val) * j.inv_tau);
-            val[i] = e;
-            sum += e;
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-        unsigned char flags = static_cast<unsigned char>((any ? kRowDistill : 0) | (bad ? kRowBadTeacher : 0));
-        if (j.labels != nullptr) {
-            const long long y = j.labels[t];
-            if (y >= 0 && y < j.N) flags |= kRowLabel;
-            if (y >= j.N) flags |= kRowBadLabel;
-            if (lane == 0) col[j.top] = (flags & kRowLabel) ? static_cast<int>(y) : kNoColumn;
-        }
-        __syncwarp();
-        for (int i = lane; i < j.top; i += 32)
-            if (!any) col[i] = kNoColumn;
-        __syncwarp();
-        for (int i = lane; i < events; i += 32) {
-            const int c = col[i];
-            int rank = 0;
-            for (int o = 0; o < events; ++o) rank += (col[o] < c || (col[o] == c && o < i)) ? 1 : 0;
-            j.ev_col[t * events + rank] = c;
-            j.ev_w[t * events + rank] = i == j.top ? -1.0f : (c == kNoColumn ? 0.0f : val[i] / sum);
-        }
+        const int flags = warp_targets(j, t, lane, s_col[warp], s_val[warp], [&](int place, int c, float w) {
+            j.ev_col[t * events + place] = c;
+            j.ev_w[t * events + place] = w;
+        });
         if (lane == 0) {
-            j.flags[t] = flags;
+            j.flags[t] = static_cast<unsigned char>(flags);
             report_bad(flags);
         }
         __syncwarp();
@@ -189,7 +194,7 @@ head_rows_kernel(const HeadRowsJob j, const int per) {
         const int c = (head_token_flags(j.tg, t, j.N) & (kRowDistill | kRowLabel)) ? 1 : 0;
         total += c;
         before += t < first ? c : 0;
-        if (blockIdx.x == 0 && j.scale.out != nullptr) largest = fmaxf(largest, head_scale_share(j.scale, j.tg, t, j.N));
+        if (blockIdx.x == 0 && j.scale.out != nullptr) largest = fmaxf(largest, head_scale_share(j.scale, j.tg.flags != nullptr, head_token_flags(j.tg, t, j.N), t));
     }
     if (blockIdx.x == 0 && j.scale.out != nullptr) {
         largest = warp_max(largest);
@@ -262,94 +267,133 @@ struct HeadLossJob {
     float *loss0, *loss1, *lse0, *lse1;           // at the tokens' own rows: distillation, label.  Cross entropy: loss1 and lse0
 };
 
-constexpr int kLossWarps = 4;
+constexpr int kLossThreads = 128;
 
-// A warp per row.  In double: a loss is the small difference of two numbers near each other, and this is a few hundred
-// operations per token.
-__global__ void __launch_bounds__(32 * kLossWarps)
+// A CTA per row, everything it reads under way at once: a call with few rows waits for latencies only.  Sums in double: a loss
+// is the small difference of two numbers near each other, and this is a few hundred operations per token.
+__global__ void __launch_bounds__(kLossThreads)
 head_losses_kernel(const HeadLossJob j) {
+    constexpr int kWarps = kLossThreads / 32;
+    __shared__ float s_f[2][kWarps];
+    __shared__ double s_d[4][kWarps];
     pdl_launch_dependents();
     pdl_wait();
-    const int lane = threadIdx.x & 31;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rows = j.count != nullptr ? *j.count : j.T;
-    for (int r = blockIdx.x * kLossWarps + (threadIdx.x >> 5); r < rows; r += gridDim.x * kLossWarps) {
+    const float tau_f = static_cast<float>(j.inv_tau);
+    for (int r = blockIdx.x; r < rows; r += gridDim.x) {
         const int t = j.count != nullptr ? j.row_src[r] : r;
         const int flags = head_token_flags(j.tg, t, j.N);
         if (!(flags & (kRowDistill | kRowLabel))) {           // few tokens only: rows left out are no rows otherwise
-            if (lane == 0) write_left_out(j.loss0, j.loss1, j.lse0, j.lse1, t, flags);
+            if (tid == 0) write_left_out(j.loss0, j.loss1, j.lse0, j.lse1, t, flags);
             continue;
         }
         const size_t p0 = static_cast<size_t>(r) * j.parts;
-        float m = -INFINITY;
-#pragma unroll 8
-        for (int i = lane; i < j.parts; i += 32) m = fmaxf(m, j.part[p0 + i].x);
-        m = warp_max(m);
-        double s0 = 0.0, s1 = 0.0;
-#pragma unroll 4
-        for (int i = lane; i < j.parts; i += 32) {            // parts without columns of the vocabulary hold (-inf, 0)
-            const float2 v = j.part[p0 + i];
-            s0 += static_cast<double>(v.y) * static_cast<double>(expf((v.x - m) * static_cast<float>(j.inv_tau)));
-            if (j.part1 != nullptr) s1 += static_cast<double>(j.part1[p0 + i]) * static_cast<double>(expf(v.x - m));
-        }
+        // maxima and sums, as many parts per thread as there are; parts without columns of the vocabulary hold (-inf, 0)
+        float m = -INFINITY, s0 = 0.0f, s1 = 0.0f;
+        const float2 none = make_float2(-INFINITY, 0.0f);
+        for (int i = tid; i < j.parts; i += 4 * kLossThreads) {
+            float2 v[4];
+            float w[4];
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            s0 += __shfl_xor_sync(0xFFFFFFFFu, s0, o);
-            s1 += __shfl_xor_sync(0xFFFFFFFFu, s1, o);
+            for (int q = 0; q < 4; ++q) {
+                const bool in = i + q * kLossThreads < j.parts;
+                v[q] = in ? j.part[p0 + i + q * kLossThreads] : none;
+                w[q] = in && j.part1 != nullptr ? j.part1[p0 + i + q * kLossThreads] : 0.0f;
+            }
+            const float top = fmaxf(fmaxf(fmaxf(v[0].x, v[1].x), fmaxf(v[2].x, v[3].x)), m);
+            if (top == -INFINITY) {                           // nothing yet; a sum that is no number stays one
+                s0 += (v[0].y + v[1].y) + (v[2].y + v[3].y);
+                continue;
+            }
+            s0 *= expf((m - top) * tau_f);
+            s1 *= expf(m - top);
+            m = top;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                s0 += v[q].y * expf((v[q].x - m) * tau_f);
+                s1 += w[q] * expf(v[q].x - m);
+            }
         }
         // The label's logit once more, in fp32 on the ordinary units: the tensor cores cut every partial sum off, always
         // towards zero, which is no matter in lse but shows in the difference (relative error of the loss 2e-6, now 5e-7).
-        float z_label = 0.0f;
+        float dot = 0.0f;
         if (j.x != nullptr && (flags & kRowLabel)) {
             const uint4* a = reinterpret_cast<const uint4*>(j.x + static_cast<size_t>(t) * j.K);
             const uint4* b = reinterpret_cast<const uint4*>(j.w + static_cast<size_t>(j.tg.labels[t]) * j.K);
             float lo = 0.0f, hi = 0.0f;
 #pragma unroll 4
-            for (int i = lane; i < j.K >> 3; i += 32) {
+            for (int i = tid; i < j.K >> 3; i += kLossThreads) {
                 const uint4 u = __ldg(a + i), v = __ldg(b + i);
                 lo = fmaf(bf16lo_to_f32(u.x), bf16lo_to_f32(v.x), lo); hi = fmaf(bf16hi_to_f32(u.x), bf16hi_to_f32(v.x), hi);
                 lo = fmaf(bf16lo_to_f32(u.y), bf16lo_to_f32(v.y), lo); hi = fmaf(bf16hi_to_f32(u.y), bf16hi_to_f32(v.y), hi);
                 lo = fmaf(bf16lo_to_f32(u.z), bf16lo_to_f32(v.z), lo); hi = fmaf(bf16hi_to_f32(u.z), bf16hi_to_f32(v.z), hi);
                 lo = fmaf(bf16lo_to_f32(u.w), bf16lo_to_f32(v.w), lo); hi = fmaf(bf16hi_to_f32(u.w), bf16hi_to_f32(v.w), hi);
             }
-            z_label = lo + hi;
+            dot = lo + hi;
+        }
+        // the teacher's entries: sum of q, and of q (log q - z / tau), to which q lse is added in the end
+        double q_sum = 0.0, kd = 0.0;
+        float z_ev = 0.0f;
+        if (j.tg.flags != nullptr) {
+            for (int i = tid; i < j.tg.events; i += kLossThreads) {
+                if (j.tg.ev_col[static_cast<size_t>(t) * j.tg.events + i] == kNoColumn) continue;
+                const float q = j.tg.ev_w[static_cast<size_t>(t) * j.tg.events + i];
+                if (q < 0.0f) {                               // the label's entry
+                    if (j.x == nullptr) z_ev = j.z_ev[static_cast<size_t>(r) * j.tg.events + i];
+                } else if (!(q == 0.0f)) {
+                    const double z = static_cast<double>(j.z_ev[static_cast<size_t>(r) * j.tg.events + i]);
+                    q_sum += static_cast<double>(q);
+                    kd += static_cast<double>(q) * (static_cast<double>(logf(q)) - z * j.inv_tau);
+                }
+            }
+        } else if (j.x == nullptr && tid == 0) {
+            z_ev = j.z_ev[r];
+        }
+        dot += z_ev;
+        const float m_warp = warp_max(m);
+        if (lane == 0) s_f[0][warp] = m_warp;
+        __syncthreads();
+        float top = s_f[0][0];
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) z_label += __shfl_xor_sync(0xFFFFFFFFu, z_label, o);
-        }
-        const double lse0 = static_cast<double>(m) * j.inv_tau + log(s0);
-        if (j.tg.flags == nullptr) {                          // cross entropy
-            if (lane == 0) {
-                j.lse0[t] = static_cast<float>(lse0);
-                j.loss1[t] = static_cast<float>(lse0 - static_cast<double>(j.x != nullptr ? z_label : j.z_ev[r]));
-            }
-            continue;
-        }
-        const double lse1 = static_cast<double>(m) + (j.part1 != nullptr ? log(s1) : 0.0);
-        double kd = 0.0, ce = 0.0;
-        for (int i = lane; i < j.tg.events; i += 32) {
-            if (j.tg.ev_col[static_cast<size_t>(t) * j.tg.events + i] == kNoColumn) continue;
-            const float q = j.tg.ev_w[static_cast<size_t>(t) * j.tg.events + i];
-            if (q < 0.0f && j.x != nullptr) {
-                ce = lse1 - static_cast<double>(z_label);
-                continue;
-            }
-            const double z = static_cast<double>(j.z_ev[static_cast<size_t>(r) * j.tg.events + i]);
-            if (q < 0.0f) ce = lse1 - z;
-            else if (!(q == 0.0f)) kd += static_cast<double>(q) * (static_cast<double>(logf(q)) - z * j.inv_tau + lse0);
-        }
+        for (int w = 1; w < kWarps; ++w) top = fmaxf(top, s_f[0][w]);
+        const float down = m == -INFINITY ? 1.0f : expf((m - top) * tau_f);      // no part: s0 is 0 or no number
+        double sums[4] = {static_cast<double>(s0) * static_cast<double>(down), m == -INFINITY ? 0.0 : static_cast<double>(s1) * static_cast<double>(expf(m - top)), q_sum, kd};
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) {
-            kd += __shfl_xor_sync(0xFFFFFFFFu, kd, o);
-            ce += __shfl_xor_sync(0xFFFFFFFFu, ce, o);
+            dot += __shfl_xor_sync(0xFFFFFFFFu, dot, o);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sums[k] += __shfl_xor_sync(0xFFFFFFFFu, sums[k], o);
         }
         if (lane == 0) {
-            const float bad = __uint_as_float(0x7FC00000u);
-            j.loss0[t] = (flags & kRowBadTeacher) ? bad : static_cast<float>(kd);
-            j.lse0[t] = (flags & kRowDistill) ? static_cast<float>(lse0) : 0.0f;
-            if (j.loss1 != nullptr) {
-                j.loss1[t] = (flags & kRowBadLabel) ? bad : static_cast<float>(ce);
-                j.lse1[t] = (flags & kRowLabel) ? static_cast<float>(lse1) : 0.0f;
+            s_f[1][warp] = dot;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) s_d[k][warp] = sums[k];
+        }
+        __syncthreads();
+        if (tid == 0) {
+#pragma unroll
+            for (int w = 1; w < kWarps; ++w) {
+                dot += s_f[1][w];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) sums[k] += s_d[k][w];
+            }
+            const double lse0 = static_cast<double>(top) * j.inv_tau + log(sums[0]);
+            if (j.tg.flags == nullptr) {                      // cross entropy
+                j.lse0[t] = static_cast<float>(lse0);
+                j.loss1[t] = static_cast<float>(lse0 - static_cast<double>(dot));
+            } else {
+                const float bad = __uint_as_float(0x7FC00000u);
+                j.loss0[t] = (flags & kRowBadTeacher) ? bad : ((flags & kRowDistill) ? static_cast<float>(sums[3] + sums[2] * lse0) : 0.0f);
+                j.lse0[t] = (flags & kRowDistill) ? static_cast<float>(lse0) : 0.0f;
+                if (j.loss1 != nullptr) {
+                    const double lse1 = static_cast<double>(top) + log(sums[1]);
+                    j.loss1[t] = (flags & kRowBadLabel) ? bad : ((flags & kRowLabel) ? static_cast<float>(lse1 - static_cast<double>(dot)) : 0.0f);
+                    j.lse1[t] = (flags & kRowLabel) ? static_cast<float>(lse1) : 0.0f;
+                }
             }
         }
+        __syncthreads();
     }
 }
 

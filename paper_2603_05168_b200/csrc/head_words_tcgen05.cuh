@@ -21,8 +21,18 @@ constexpr int kWordsTurnBytes = 8 * kWordsSquare * 4;
 constexpr int kWordsStateBytes = 8 * 3 * kWordsTokens * 4;                 // stats: [warp][m, s0, s1][token]; grad: the warps' boxes
 static_assert(kWordsTurnBytes % 1024 == 0 && kWordsStateBytes >= 8 * kWarpBoxBytes, "alignment and room of the boxes");
 
+// What a CTA has per stage: 128 words, half the tokens.
+__host__ __device__ constexpr int words_stage_bytes(int tokens) { return kPairLoopStageA + tokens / 2 * 128; }
+// Few tokens leave room for more stages: it is the bytes under way that the words stream with.
+constexpr int words_stages(int tokens) {
+    const int room = (232448 - kBarrierBytes - kWordsTurnBytes - kWordsStateBytes) / words_stage_bytes(tokens);
+    return room < 10 ? room : 10;
+}
+constexpr int words_smem_bytes(int tokens) { return words_stages(tokens) * words_stage_bytes(tokens) + kWordsTurnBytes + kWordsStateBytes + kBarrierBytes; }
+
 struct HeadWordsParams {
     HeadLogitsParams p;           // rows are tokens: count, row_src, bn unused; parts = 8 x pairs
+    int stages;
     int tokens, groups;           // tokens per tile (a multiple of 32), groups of them
     int pairs;
     const uint16_t* x;            // grad: copied to xc [T up to a multiple of 64][K]
@@ -33,7 +43,9 @@ struct HeadWordsParams {
 template <int MODE, bool LIST, bool DUAL>
 struct HeadWordsWork {
     static constexpr bool kWide = false;
-    static constexpr int kStages = 5, kStagingBytes = kWordsTurnBytes + kWordsStateBytes;
+    static constexpr int kStages = 5, kStagingBytes = kWordsTurnBytes + kWordsStateBytes;    // (at 256 tokens)
+    __device__ int stages() const { return wp.stages; }
+    __device__ int stage_bytes() const { return words_stage_bytes(wp.tokens); }
     const HeadMaps& maps;
     const HeadWordsParams& wp;
     const HeadLogitsParams& p;
@@ -92,7 +104,7 @@ struct HeadWordsWork {
                 }
             } else {
                 float largest = 0.0f;                                       // every warp for itself
-                for (int t = lane; t < p.T; t += 32) largest = fmaxf(largest, head_scale_share(w.wp.scale, p.tg, t, p.N));
+                for (int t = lane; t < p.T; t += 32) largest = fmaxf(largest, head_scale_share(w.wp.scale, LIST, head_token_flags(p.tg, t, p.N), t));
                 const float unit = head_scale_unit(warp_max(largest));
                 inv_scale = 1.0f / unit;
                 const int tid = static_cast<int>(threadIdx.x) - 64;
