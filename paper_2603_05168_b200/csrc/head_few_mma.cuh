@@ -1,24 +1,25 @@
 // Losses at the output head for up to 16 tokens: the head streams by once per pass and every product is small beside it, so
-// the operands go from memory straight into the registers of warp-level MMAs (m16n8k16), no tensor memory, no staging.
+// the operands go from memory straight into the registers of warp-level MMAs, no tensor memory, no staging of words.
 //
-//   head_few_kernel<stats | grad>   z of 16 words at a time: the 16 warps of a CTA split K, add their parts in shared memory, and
-//                                   a thread per word and token goes on with the maximum and sum it keeps (stats), or with
-//                                   dz in bf16 (grad; T x N of them, a few MB)
-//   head_few_grads_kernel           dW = dz^T x and dx = dz W from one more look at W, last words first: what the grad
-//                                   kernel read last is still in the L2
+//   head_few_forward_kernel    z of 16 words at a time: the 16 warps of a CTA split K, add their parts in shared memory, and a thread per
+//                              word and token goes on with the maximum and sum it keeps
+//   head_few_backward_kernel   8 words at a time, everything from one look at them: z as above, dz in bf16 in shared memory, then
+//                              every warp forms dW's rows of its columns and adds to its columns of dx, which it keeps in
+//                              registers for the whole kernel (one partial sum per CTA for head_dx_kernel).  With dz kept in
+//                              memory and the words read a second time for dx, 7 tokens x 3968 x 139152 took 630 us
 //
-// Rows of x that nothing is asked of enter as zeros.  Operands of both kernels are read as 16 bytes per lane: lane (g, t) =
-// (lane / 4, lane % 4) takes columns 8 t .. 8 t + 7 of a block of 32 from rows g and g + 8.  Which column an MMA calls which
-// index of its contraction is free as long as both operands agree, so the registers serve as they are; where the columns
-// are not contracted over (dx, dW) `movmatrix` transposes registers as 8 x 8 tiles, whose columns then come out as 8 t + 2 j.
+// Rows of x that nothing is asked of enter as zeros.  Operands are read as 16 bytes per lane: lane (g, t) = (lane / 4, lane % 4)
+// takes columns 8 t .. 8 t + 7 of a block of 32 from row g (and g + 8).  Which column an MMA calls which index of its contraction
+// is free as long as both operands agree, so the registers serve as they are; where the columns are not contracted over (dx,
+// dW) `movmatrix` transposes registers as 8 x 8 tiles, whose columns then come out as 8 t + 2 j.
 #pragma once
 
 #include "head_words_tcgen05.cuh"
 
 namespace sbn {
 
-// What fits: the registers of a thread hold its share of the tokens' rows and of 16 words (and the same share of the next 16
-// words under way), 80 of 128 registers for 16 tokens x 2560 or 96 for 8 tokens x 4096.
+// What fits the 128 registers of a thread: forward its share of the tokens' rows and of 16 words, 80 for 16 tokens x 2560 or 96
+// for 8 tokens x 4096; backward its share of dx and of 8 words, 100 and 96.
 static inline bool head_few_takes(int T, int K) { return T <= 8 ? K <= 4096 : T <= 16 && K <= 2560; }
 constexpr int kFewHeadWarps = 16;
 constexpr int kFewHeadThreads = 32 * kFewHeadWarps;
@@ -39,12 +40,8 @@ struct HeadFewParams {
     float* z_ev;                  // [T][events]
     const float *lse0, *lse1;
     HeadScale scale;
-    uint16_t* dz;                 // grad: [T][ldz]
-    int ldz;
-    // gradients
     uint16_t* dw;                 // [N][K] or null
-    float* acc;                   // [ranges][T][K] or null
-    int slabs, per;               // 256-column slabs; blocks of 16 words per range
+    float* acc;                   // [CTAs][T][K] or null
 };
 
 __device__ __forceinline__ void mma_bf16_k16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -66,15 +63,71 @@ __device__ __forceinline__ uint4 load_stream(const uint16_t* p) {
     return v;
 }
 
-// KBW: blocks of 32 columns per warp (K <= 512 KBW).  NT: groups of 8 tokens.  MODE, LIST, DUAL as in head_gemm_tcgen05.cuh.
-template <int KBW, int NT, int MODE, bool LIST, bool DUAL>
+// What is asked of the tokens, for a CTA: flags, and the sorted targets of a distillation.
+template <int NT, bool LIST>
+struct FewTargets {
+    int flags[8 * NT];
+    int col[LIST ? 8 * NT : 1][LIST ? kHeadMaxTop + 1 : 1];
+    float w[LIST ? 8 * NT : 1][LIST ? kFewOwnEvents : 1];
+};
+// `room`: 2 kFewOwnEvents words per token, free until the barrier that the caller puts behind this.
+template <int NT, bool LIST>
+__device__ __forceinline__ void few_targets(const HeadFewParams& p, FewTargets<NT, LIST>& s, int* room) {
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (LIST && p.job.index != nullptr) {
+        if (warp < p.T) {
+            int* col = room + warp * 2 * kFewOwnEvents;
+            const int flags = warp_targets(p.job, warp, lane, col, reinterpret_cast<float*>(col + kFewOwnEvents), [&](int place, int c, float v) {
+                s.col[LIST ? warp : 0][place] = c;
+                s.w[LIST ? warp : 0][place] = v;
+                if (blockIdx.x == 0) {
+                    p.job.ev_col[warp * p.tg.events + place] = c;
+                    p.job.ev_w[warp * p.tg.events + place] = v;
+                }
+            });
+            if (lane == 0) {
+                s.flags[warp] = flags;
+                if (blockIdx.x == 0) {
+                    p.job.flags[warp] = static_cast<unsigned char>(flags);
+                    report_bad(flags);
+                }
+            }
+        }
+    } else {
+        if (tid < p.T) s.flags[tid] = head_token_flags(p.tg, tid, p.N);
+        if constexpr (LIST)
+            for (int i = tid; i < p.T * p.tg.events; i += kFewHeadThreads) s.col[i / p.tg.events][i % p.tg.events] = p.tg.ev_col[i];
+    }
+}
+// A thread's way through the targets of its token, along words that ascend.
+template <int NT, bool LIST>
+struct FewCursor {
+    int e, next;
+    __device__ FewCursor(const HeadFewParams& p, const FewTargets<NT, LIST>& s, int tok, bool asked) : e(0), next(kNoColumn) {
+        if (LIST && asked) next = s.col[tok][0];
+    }
+    // Calls at(e) for every target that is word n, one of the WORDS from `first` on.
+    template <int WORDS, class At>
+    __device__ __forceinline__ void visit(const HeadFewParams& p, const FewTargets<NT, LIST>& s, int tok, int first, int n, At&& at) {
+        if constexpr (LIST) {
+            while (next < first) { ++e; next = e < p.tg.events ? s.col[tok][e] : kNoColumn; }
+            for (int f = e, c = next; c < first + WORDS;) {
+                if (c == n) at(f);
+                ++f;
+                c = f < p.tg.events ? s.col[tok][f] : kNoColumn;
+            }
+        }
+    }
+};
+
+// KBW: blocks of 32 columns per warp (K <= 512 KBW).  NT: groups of 8 tokens.  LIST, DUAL as in head_gemm_tcgen05.cuh.
+template <int KBW, int NT, bool LIST, bool DUAL>
 __global__ void __launch_bounds__(kFewHeadThreads, 1)
-head_few_kernel(const HeadFewParams p) {
+head_few_forward_kernel(const HeadFewParams p) {
     constexpr int kTok = 8 * NT;
+    constexpr float kLog2e = 1.4426950408889634f;
     __shared__ float s_part[kFewHeadWarps][16][kTok];
-    __shared__ int s_col[LIST ? kTok : 1][LIST ? kHeadMaxTop + 1 : 1];
-    __shared__ float s_w[LIST ? kTok : 1][LIST ? kFewOwnEvents : 1];
-    __shared__ int s_flags[kTok];
+    __shared__ FewTargets<NT, LIST> s_tg;
     pdl_launch_dependents();
     pdl_wait();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
@@ -92,41 +145,14 @@ head_few_kernel(const HeadFewParams p) {
     };
 #pragma unroll
     for (int i = 0; i < KBW; ++i) load_block(i, blockIdx.x);
-
-    const bool own = LIST && p.job.index != nullptr;
-    if (own) {
-        if (warp < p.T) {
-            // (the room of the parts, which nobody has yet)
-            int* col = reinterpret_cast<int*>(&s_part[0][0][0]) + warp * 2 * kFewOwnEvents;
-            const int flags = warp_targets(p.job, warp, lane, col, reinterpret_cast<float*>(col + kFewOwnEvents), [&](int place, int c, float v) {
-                s_col[LIST ? warp : 0][place] = c;
-                s_w[LIST ? warp : 0][place] = v;
-                if (blockIdx.x == 0) {
-                    p.job.ev_col[warp * p.tg.events + place] = c;
-                    p.job.ev_w[warp * p.tg.events + place] = v;
-                }
-            });
-            if (lane == 0) {
-                s_flags[warp] = flags;
-                if (blockIdx.x == 0) {
-                    p.job.flags[warp] = static_cast<unsigned char>(flags);
-                    report_bad(flags);
-                }
-            }
-        }
-    } else if (tid < p.T) {
-        s_flags[tid] = head_token_flags(p.tg, tid, p.N);
-    }
-    if (LIST && !own) {
-        for (int i = tid; i < p.T * p.tg.events; i += kFewHeadThreads) s_col[i / p.tg.events][i % p.tg.events] = p.tg.ev_col[i];
-    }
+    few_targets(p, s_tg, reinterpret_cast<int*>(&s_part[0][0][0]));
     __syncthreads();
 
     uint4 x[KBW][NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         const int t = nt * 8 + g;
-        const bool there = t < p.T && (s_flags[t] & (kRowDistill | kRowLabel));
+        const bool there = t < p.T && (s_tg.flags[t] & (kRowDistill | kRowLabel));
 #pragma unroll
         for (int i = 0; i < KBW; ++i) {
             const int kb = warp + kFewHeadWarps * i;
@@ -136,27 +162,10 @@ head_few_kernel(const HeadFewParams p) {
     }
     // the word and token of this thread in every block
     const int tok = tid % kTok, slot = tid / kTok;
-    const bool mine = slot < 16 && tok < p.T;
-    const int flags = mine ? s_flags[tok] : 0;
-    const bool asked = (flags & (kRowDistill | kRowLabel)) != 0;
+    const bool asked = slot < 16 && tok < p.T && (s_tg.flags[tok] & (kRowDistill | kRowLabel));
     const int label = !LIST && asked ? static_cast<int>(p.tg.labels[tok]) : -1;
-    constexpr float kLog2e = 1.4426950408889634f;
     float m = -INFINITY, s0 = 0.0f, s1 = 0.0f;
-    float l0 = -INFINITY, l1 = -INFINITY, g0 = 0.0f, g1 = 0.0f;
-    if constexpr (MODE == 1) {
-        if (!LIST && blockIdx.x == 0 && mine) report_bad(flags);
-        const float unit = head_scale_unit(warp_max(lane < p.T ? head_scale_share(p.scale, LIST, s_flags[lane], lane) : 0.0f));
-        const float inv_scale = 1.0f / unit;
-        if (blockIdx.x == 0 && tid == 0) p.scale.out[0] = unit;
-        if (LIST ? (flags & kRowDistill) != 0 : asked) {
-            l0 = -p.lse0[tok] * kLog2e;
-            g0 = p.scale.g0[tok] * p.inv_tau * inv_scale;
-        }
-        if (DUAL && (flags & kRowLabel)) {
-            l1 = -p.lse1[tok] * kLog2e;
-            g1 = p.scale.g1[tok] * inv_scale;
-        }
-    }
+    FewCursor<NT, LIST> cursor(p, s_tg, tok, asked);
 
     for (int nb = blockIdx.x; nb < blocks; nb += gridDim.x) {
         float d[NT][4] = {};
@@ -176,191 +185,262 @@ head_few_kernel(const HeadFewParams p) {
         }
         __syncthreads();
         const int n = nb * 16 + slot;
-        if (mine) {
+        if (asked && n < p.N) {
             float z = 0.0f;
 #pragma unroll
             for (int v = 0; v < kFewHeadWarps; ++v) z += s_part[v][slot][tok];
-            if (MODE == 0 && n < p.N && asked) {
-                const float m_new = fmaxf(m, z);
-                s0 = s0 * ex2_approx((m - m_new) * p.c0) + ex2_approx((z - m_new) * p.c0);
-                if (DUAL) s1 = s1 * ex2_approx((m - m_new) * kLog2e) + ex2_approx((z - m_new) * kLog2e);
-                m = m_new;
-            }
-            float v = 0.0f;
-            if (MODE == 1 && n < p.N) {
-                v = ex2_approx(fmaf(z, p.c0, l0)) * g0;
-                if (DUAL) v = fmaf(ex2_approx(fmaf(z, kLog2e, l1)), g1, v);
-            }
-            if constexpr (LIST) {
-                if (asked && n < p.N) {
-                    int lo = 0, hi = p.tg.events;
-                    while (lo < hi) {
-                        const int mid = (lo + hi) >> 1;
-                        if (s_col[tok][mid] < n) lo = mid + 1; else hi = mid;
-                    }
-                    for (; lo < p.tg.events && s_col[tok][lo] == n; ++lo) {
-                        const size_t at = static_cast<size_t>(tok) * p.tg.events + lo;
-                        if (MODE == 0) {
-                            p.z_ev[at] = z;
-                        } else {
-                            const float q = own ? s_w[tok][lo] : p.tg.ev_w[at];
-                            v -= q < 0.0f ? g1 : q * g0;
-                        }
-                    }
-                }
-            } else if (n == label) {
-                if (MODE == 0) p.z_ev[tok] = z;
-                else v -= g0;
-            }
-            if (MODE == 1) {
-                unsigned short o;
-                asm("cvt.rn.bf16.f32 %0, %1;" : "=h"(o) : "f"(v));
-                p.dz[static_cast<size_t>(tok) * p.ldz + n] = o;
-            }
+            const float m_new = fmaxf(m, z);
+            s0 = s0 * ex2_approx((m - m_new) * p.c0) + ex2_approx((z - m_new) * p.c0);
+            if (DUAL) s1 = s1 * ex2_approx((m - m_new) * kLog2e) + ex2_approx((z - m_new) * kLog2e);
+            m = m_new;
+            cursor.template visit<16>(p, s_tg, tok, nb * 16, n, [&](int e) { p.z_ev[static_cast<size_t>(tok) * p.tg.events + e] = z; });
+            if (!LIST && n == label) p.z_ev[tok] = z;
         }
         __syncthreads();
     }
-    if constexpr (MODE == 0) {
-        float* red = &s_part[0][0][0];                              // [3][16][kTok]
-        if (slot < 16) {
-            red[slot * kTok + tok] = m;
-            red[(16 + slot) * kTok + tok] = s0;
-            red[(32 + slot) * kTok + tok] = s1;
+    float* red = &s_part[0][0][0];                                  // [3][16][kTok]
+    if (slot < 16) {
+        red[slot * kTok + tok] = m;
+        red[(16 + slot) * kTok + tok] = s0;
+        red[(32 + slot) * kTok + tok] = s1;
+    }
+    __syncthreads();
+    if (tid < kTok && tid < p.T) {
+        float mm = -INFINITY;
+        for (int q = 0; q < 16; ++q) mm = fmaxf(mm, red[q * kTok + tid]);
+        float a0 = 0.0f, a1 = 0.0f;
+        for (int q = 0; q < 16; ++q) {
+            const float mq = red[q * kTok + tid], sq = red[(16 + q) * kTok + tid];
+            if (mq == -INFINITY && sq == 0.0f) continue;           // a slot without words
+            a0 += sq * ex2_approx((mq - mm) * p.c0);
+            if (DUAL) a1 += red[(32 + q) * kTok + tid] * ex2_approx((mq - mm) * kLog2e);
         }
-        __syncthreads();
-        if (tid < kTok && tid < p.T) {
-            float mm = -INFINITY;
-            for (int q = 0; q < 16; ++q) mm = fmaxf(mm, red[q * kTok + tid]);
-            float a0 = 0.0f, a1 = 0.0f;
-            for (int q = 0; q < 16; ++q) {
-                const float mq = red[q * kTok + tid], sq = red[(16 + q) * kTok + tid];
-                if (mq == -INFINITY && sq == 0.0f) continue;       // a slot without words
-                a0 += sq * ex2_approx((mq - mm) * p.c0);
-                if (DUAL) a1 += red[(32 + q) * kTok + tid] * ex2_approx((mq - mm) * kLog2e);
-            }
-            const size_t at = static_cast<size_t>(tid) * gridDim.x + blockIdx.x;
-            p.part[at] = make_float2(mm, a0);
-            if (DUAL) p.part1[at] = a1;
-        }
+        const size_t at = static_cast<size_t>(tid) * gridDim.x + blockIdx.x;
+        p.part[at] = make_float2(mm, a0);
+        if (DUAL) p.part1[at] = a1;
     }
 }
 
-// CTA: 256 columns x a range of words.  Warp (column group of 64, part): blocks of 16 words part, part + 4, ... of the range.
-template <int NT>
+// Dynamic shared memory: the tokens' rows, 16 bytes apart from a multiple of 128 (an 8 x 8 tile's rows then lie on different
+// banks), before that the room of few_targets.  Of every 32 columns the pairs 8 t + 2 j, 8 t + 2 j + 1 lie at 8 j + 2 t: tile j of
+// `ldmatrix` is then register j of a lane's 16 bytes, and its transposed form what movmatrix would make of it.
+static inline int head_few_x_bytes(int T, int K) { return (T <= 8 ? 8 : 16) * std::max(2 * K + 16, 2 * kFewOwnEvents * 4); }
+
+template <bool TRANS>
+__device__ __forceinline__ void ldmatrix_x4(uint32_t (&r)[4], uint32_t addr) {
+    if constexpr (TRANS)
+        asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+    else
+        asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+
+// The shares of 512 columns that a launch is made for, and the words per step that go with them.
+static inline int head_few_shares(int K) { return K <= 1024 ? 2 : (K <= 2560 ? 5 : 8); }
+__host__ __device__ constexpr int few_backward_words(int kbw, int nt) { return kbw * (8 + 8 * nt) <= 100 ? 16 : 8; }    // dx and words: 4 bytes x this per thread
+static inline int head_few_words(int T, int K) { return few_backward_words(head_few_shares(K), T <= 8 ? 1 : 2); }
+
+// Words per step: 16 where the registers hold them beside dx (a 16-row MMA is full then, and a step's barriers are spread over twice
+// the words), else 8.
+template <int KBW, int NT, bool LIST, bool DUAL>
 __global__ void __launch_bounds__(kFewHeadThreads, 1)
-head_few_grads_kernel(const HeadFewParams p) {
-    constexpr int kTok = 8 * NT, kDepth = 3;
-    __shared__ float s_dx[256][kTok + 1];
+head_few_backward_kernel(const HeadFewParams p) {
+    constexpr int H = few_backward_words(KBW, NT) / 8;
+    constexpr int kTok = 8 * NT, kWords = 8 * H;
+    constexpr int kParts = kFewHeadThreads / (kWords * kTok) < 4 ? kFewHeadThreads / (kWords * kTok) : 4;   // threads per sum of the warps' parts
+    constexpr int kRow = kWords + 2, kPart = kTok * kRow + 2;       // of the parts, in floats: what is read or written at once lies on all banks
+    constexpr float kLog2e = 1.4426950408889634f;
+    __shared__ float s_part[kFewHeadWarps * kPart];
+    __shared__ FewTargets<NT, LIST> s_tg;
+    __shared__ float4 s_k[kTok];                                    // -lse log2(e) and gradient per loss (registers are for dx)
+    __shared__ int s_label[kTok];
+    __shared__ int2 s_cursor[kFewHeadWarps];                        // a warp's token's next target and its word
+    __shared__ __align__(16) uint16_t s_dz[kTok][kWords];           // B operand of dx: pairs of words of a token
+    __shared__ __align__(16) uint16_t s_dzt[kWords][kTok];          // A operand of dW: pairs of tokens of a word
+    extern __shared__ __align__(16) uint8_t s_x[];
     pdl_launch_dependents();
     pdl_wait();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
-    const int part = warp >> 2;
-    const int slab = static_cast<int>(blockIdx.x) % p.slabs, range = static_cast<int>(blockIdx.x) / p.slabs;
-    const int col0 = slab * 256 + (warp & 3) * 64;
-    const bool live = col0 < p.K;                                   // K % 64 == 0: a group is in or out as a whole
-    const int all = (p.N + 15) >> 4;
-    const int first = range * p.per, last = min(all, first + p.per);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
+    const int blocks = (p.N + kWords - 1) / kWords, kbs = p.K >> 5, pitch = 2 * p.K + 16;
 
-    // x^T as the B operand of dW: contraction over tokens, columns 8 t + 2 j of each block of 32
-    uint32_t xt[2][4][NT];
+    uint4 w[KBW][H];
+    auto load_block = [&](int i, int nb) {
+        const int kb = warp + kFewHeadWarps * i;
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        const int t = nt * 8 + g;
-        const bool there = live && t < p.T && (head_token_flags(p.tg, t, p.N) & (kRowDistill | kRowLabel));
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            uint4 v = make_uint4(0u, 0u, 0u, 0u);
-            if (there) v = __ldg(reinterpret_cast<const uint4*>(p.x + static_cast<size_t>(t) * p.K + col0 + kb * 32 + t4 * 8));
-            xt[kb][0][nt] = transpose_8x8(v.x);
-            xt[kb][1][nt] = transpose_8x8(v.y);
-            xt[kb][2][nt] = transpose_8x8(v.z);
-            xt[kb][3][nt] = transpose_8x8(v.w);
-        }
-    }
-    const float scale = p.scale.out[0];
-    float acc[2][2][NT][4] = {};
-    uint4 w[kDepth][2][2];
-    uint32_t dz[kDepth][NT][2];
-    // the range's blocks from its end: i-th of this warp
-    auto block_at = [&](int i) { return last - 1 - part - 4 * i; };
-    auto load = [&](int s, int nb) {
-        const bool in = live && nb >= first;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int n = nb * 16 + h * 8 + g;
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb) {
-                w[s][kb][h] = make_uint4(0u, 0u, 0u, 0u);
-                if (in && n < p.N && p.acc != nullptr) w[s][kb][h] = load_stream(p.w + static_cast<size_t>(n) * p.K + col0 + kb * 32 + t4 * 8);
-            }
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                const int t = nt * 8 + g;
-                dz[s][nt][h] = 0u;
-                if (in && t < p.T) dz[s][nt][h] = __ldg(reinterpret_cast<const uint32_t*>(p.dz + static_cast<size_t>(t) * p.ldz + nb * 16 + h * 8 + 2 * t4));
-            }
+        for (int h = 0; h < H; ++h) {
+            const int n = nb * kWords + h * 8 + g;
+            w[i][h] = make_uint4(0u, 0u, 0u, 0u);
+            if (kb < kbs && nb < blocks && n < p.N) w[i][h] = load_stream(p.w + static_cast<size_t>(n) * p.K + kb * 32 + t4 * 8);
         }
     };
-    const int mine = last - 1 - part < first ? 0 : (last - 1 - part - first) / 4 + 1;
 #pragma unroll
-    for (int s = 0; s < kDepth; ++s) load(s, block_at(s));
-#pragma unroll 1
-    for (int i = 0; i < mine; i += kDepth) {
+    for (int i = 0; i < KBW; ++i) load_block(i, blockIdx.x);
+    few_targets(p, s_tg, reinterpret_cast<int*>(s_x));
+    __syncthreads();
+    const float unit = head_scale_unit(warp_max(lane < p.T ? head_scale_share(p.scale, LIST, s_tg.flags[lane], lane) : 0.0f));
+    if (blockIdx.x == 0 && tid == 0) p.scale.out[0] = unit;
+    const int vecs = p.K >> 3;
+    for (int i = tid; i < kTok * vecs; i += kFewHeadThreads) {
+        const int t = i / vecs, c = i - t * vecs;
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (t < p.T && (s_tg.flags[t] & (kRowDistill | kRowLabel))) v = __ldg(reinterpret_cast<const uint4*>(p.x + static_cast<size_t>(t) * p.K) + c);
+        uint32_t* to = reinterpret_cast<uint32_t*>(s_x + t * pitch + (c >> 2) * 64 + (c & 3) * 4);
+        to[0] = v.x; to[4] = v.y; to[8] = v.z; to[12] = v.w;
+    }
+    if (tid < kTok) {
+        const int flags = tid < p.T ? s_tg.flags[tid] : 0;
+        float4 k = make_float4(-INFINITY, 0.0f, -INFINITY, 0.0f);
+        if (!LIST && blockIdx.x == 0) report_bad(flags);
+        if (flags & (LIST ? kRowDistill : kRowLabel)) {
+            k.x = -p.lse0[tid] * kLog2e;
+            k.y = p.scale.g0[tid] * p.inv_tau / unit;
+        }
+        if (DUAL && (flags & kRowLabel)) {
+            k.z = -p.lse1[tid] * kLog2e;
+            k.w = p.scale.g1[tid] / unit;
+        }
+        s_k[tid] = k;
+        s_label[tid] = !LIST && (flags & kRowLabel) ? static_cast<int>(p.tg.labels[tid]) : -1;
+    }
+    if (LIST && lane == 0 && tid < kTok * kWords * kParts) {
+        const int tok = tid / (kWords * kParts);
+        s_cursor[warp] = make_int2(0, tok < p.T && s_tg.flags[tok] != 0 ? s_tg.col[LIST ? tok : 0][0] : kNoColumn);
+    }
+    __syncthreads();
+
+    // ldmatrix: lane's row lane % 8 (a token) of tile lane / 8
+    const uint32_t x_lane = smem_u32(s_x) + static_cast<uint32_t>((lane & 7) * pitch + (lane >> 3) * 16);
+    float acc[KBW][2][NT][4] = {};
+    for (int nb = blockIdx.x; nb < blocks; nb += gridDim.x) {
+        {
+            // the words after the next ones: on their way from memory to the L2 while these are worked on
+            const long long n = (static_cast<long long>(nb) + 2ll * gridDim.x) * kWords + tid;
+            if (tid < kWords && n < p.N) prefetch_l2_bulk(p.w + static_cast<size_t>(n) * p.K, static_cast<uint32_t>(2 * p.K));
+        }
+        float d[H][2][4] = {};                                      // D rows: tokens g, g + 8; columns: words 2 t, 2 t + 1; two chains
 #pragma unroll
-        for (int s = 0; s < kDepth; ++s) {
-            if (i + s >= mine) break;                               // the same for the whole warp
-            const int nb = block_at(i + s);
-            __syncwarp();
-            if (p.acc != nullptr) {
+        for (int i = 0; i < KBW; ++i) {
+            const int kb = warp + kFewHeadWarps * i;
+            if (kb < kbs) {
+                uint32_t a[4], b[4] = {};
+                ldmatrix_x4<false>(a, x_lane + kb * 64);
+                if (NT == 2) ldmatrix_x4<false>(b, x_lane + 8 * pitch + kb * 64);
 #pragma unroll
-                for (int kb = 0; kb < 2; ++kb) {
-                    const uint32_t lo[4] = {w[s][kb][0].x, w[s][kb][0].y, w[s][kb][0].z, w[s][kb][0].w};
-                    const uint32_t hi[4] = {w[s][kb][1].x, w[s][kb][1].y, w[s][kb][1].z, w[s][kb][1].w};
+                for (int h = 0; h < H; ++h) {
+                    mma_bf16_k16(d[h][0], a[0], b[0], a[1], b[1], w[i][h].x, w[i][h].y);
+                    mma_bf16_k16(d[h][1], a[2], b[2], a[3], b[3], w[i][h].z, w[i][h].w);
+                }
+            }
+        }
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+            float* to = &s_part[warp * kPart + g * kRow + h * 8 + 2 * t4];
+            *reinterpret_cast<float2*>(to) = make_float2(d[h][0][0] + d[h][1][0], d[h][0][1] + d[h][1][1]);
+            if (NT == 2) *reinterpret_cast<float2*>(to + 8 * kRow) = make_float2(d[h][0][2] + d[h][1][2], d[h][0][3] + d[h][1][3]);
+        }
+        __syncthreads();
+        if (tid < kTok * kWords * kParts) {                         // whole warps, a token each
+            const int tok = tid / (kWords * kParts), slot = tid / kParts % kWords, part = tid % kParts;
+            const int n = nb * kWords + slot;
+            float z = 0.0f;
+#pragma unroll
+            for (int q = 0; q < kFewHeadWarps / kParts; ++q) z += s_part[(kFewHeadWarps / kParts * part + q) * kPart + tok * kRow + slot];
+#pragma unroll
+            for (int o = 1; o < kParts; o <<= 1) z += __shfl_xor_sync(0xFFFFFFFFu, z, o);
+            const float4 k = s_k[tok];
+            float v = ex2_approx(fmaf(z, p.c0, k.x)) * k.y;
+            if (DUAL) v = fmaf(ex2_approx(fmaf(z, kLog2e, k.z)), k.w, v);
+            if constexpr (LIST) {
+                int2 cur = s_cursor[warp];
+                if (cur.y < (nb + 1) * kWords) {                    // the same for the warp
+                    while (cur.y < nb * kWords) { ++cur.x; cur.y = cur.x < p.tg.events ? s_tg.col[tok][cur.x] : kNoColumn; }
+                    for (int f = cur.x, c = cur.y; c < (nb + 1) * kWords;) {
+                        if (c == n) {
+                            const float q = p.job.index != nullptr ? s_tg.w[tok][f] : p.tg.ev_w[static_cast<size_t>(tok) * p.tg.events + f];
+                            v -= q < 0.0f ? k.w : q * k.y;
+                        }
+                        ++f;
+                        c = f < p.tg.events ? s_tg.col[tok][f] : kNoColumn;
+                    }
+                    __syncwarp();
+                    if (lane == 0) s_cursor[warp] = cur;
+                }
+            } else if (n == s_label[tok]) {
+                v -= k.y;
+            }
+            if (n >= p.N || (k.y == 0.0f && k.w == 0.0f)) v = 0.0f;   // behind the vocabulary; nothing asked (z may be anything)
+            unsigned short o;
+            asm("cvt.rn.bf16.f32 %0, %1;" : "=h"(o) : "f"(v));
+            if (part == 0) {
+                s_dz[tok][slot] = o;
+                s_dzt[slot][tok] = o;
+            }
+        }
+        __syncthreads();
+        uint32_t dz[NT][H], dzt[NT][2] = {};
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int h = 0; h < H; ++h) {
+                dz[nt][h] = *reinterpret_cast<const uint32_t*>(&s_dz[nt * 8 + g][h * 8 + 2 * t4]);
+                dzt[nt][h] = *reinterpret_cast<const uint32_t*>(&s_dzt[h * 8 + g][nt * 8 + 2 * t4]);
+            }
+#pragma unroll
+        for (int i = 0; i < KBW; ++i) {
+            const int kb = warp + kFewHeadWarps * i;
+            if (kb < kbs) {                                         // the same for the whole warp
+                if (p.acc != nullptr) {
+                    const uint32_t lo[4] = {w[i][0].x, w[i][0].y, w[i][0].z, w[i][0].w};
+                    const uint32_t hi[4] = {w[i][H - 1].x, w[i][H - 1].y, w[i][H - 1].z, w[i][H - 1].w};
 #pragma unroll
                     for (int q = 0; q < 2; ++q) {
                         const uint32_t a0 = transpose_8x8(lo[2 * q]), a1 = transpose_8x8(lo[2 * q + 1]);
-                        const uint32_t a2 = transpose_8x8(hi[2 * q]), a3 = transpose_8x8(hi[2 * q + 1]);
+                        if constexpr (H == 2) {
+                            const uint32_t a2 = transpose_8x8(hi[2 * q]), a3 = transpose_8x8(hi[2 * q + 1]);
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) mma_bf16_k16(acc[kb][q][nt], a0, a1, a2, a3, dz[s][nt][0], dz[s][nt][1]);
+                            for (int nt = 0; nt < NT; ++nt) mma_bf16_k16(acc[i][q][nt], a0, a1, a2, a3, dz[nt][0], dz[nt][H - 1]);
+                        } else {
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) mma_bf16_k8(acc[i][q][nt], a0, a1, dz[nt][0]);
+                        }
                     }
                 }
-            }
-            if (p.dw != nullptr) {
-                uint32_t a[NT][2];
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    a[nt][0] = transpose_8x8(dz[s][nt][0]);
-                    a[nt][1] = transpose_8x8(dz[s][nt][1]);
-                }
-#pragma unroll
-                for (int kb = 0; kb < 2; ++kb) {
-                    uint32_t o[2][4];
+                load_block(i, nb + static_cast<int>(gridDim.x));
+                if (p.dw != nullptr) {
+                    uint32_t lo[4], hi[4];
+                    ldmatrix_x4<true>(lo, x_lane + kb * 64);
+                    if (NT == 2) ldmatrix_x4<true>(hi, x_lane + 8 * pitch + kb * 64);
+                    uint32_t o[H][4];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        float d[4] = {};
-                        if constexpr (NT == 1) mma_bf16_k8(d, a[0][0], a[0][1], xt[kb][j][0]);
-                        else mma_bf16_k16(d, a[0][0], a[0][1], a[NT - 1][0], a[NT - 1][1], xt[kb][j][0], xt[kb][j][NT - 1]);
-                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[0][j]) : "f"(d[1] * scale), "f"(d[0] * scale));
-                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[1][j]) : "f"(d[3] * scale), "f"(d[2] * scale));
+                        float e[4] = {};
+                        if constexpr (NT == 1) mma_bf16_k8(e, dzt[0][0], dzt[0][1], lo[j]);
+                        else mma_bf16_k16(e, dzt[0][0], dzt[0][1], dzt[NT - 1][0], dzt[NT - 1][1], lo[j], hi[j]);
+#pragma unroll
+                        for (int h = 0; h < H; ++h)
+                            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[h][j]) : "f"(e[2 * h + 1] * unit), "f"(e[2 * h] * unit));
                     }
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int n = nb * 16 + h * 8 + g;
-                        if (live && n < p.N)
-                            *reinterpret_cast<uint4*>(p.dw + static_cast<size_t>(n) * p.K + col0 + kb * 32 + t4 * 8) = make_uint4(o[h][0], o[h][1], o[h][2], o[h][3]);
+                    for (int h = 0; h < H; ++h) {
+                        const int n = nb * kWords + h * 8 + g;
+                        if (n < p.N) *reinterpret_cast<uint4*>(p.dw + static_cast<size_t>(n) * p.K + kb * 32 + t4 * 8) = make_uint4(o[h][0], o[h][1], o[h][2], o[h][3]);
                     }
+                    __syncwarp();
                 }
             }
-            load(s, block_at(i + s + kDepth));
         }
     }
     if (p.acc == nullptr) return;
-    // the four parts one after another: a fixed order
-#pragma unroll 1
-    for (int turn = 0; turn < 4; ++turn) {
-        if (part == turn) {
+    // The sums of 4 NT tokens at a time through shared memory (where x was), so that rows leave whole: as the lanes have them, 8 bytes
+    // of a sector at a time, they took 17 us for 16 tokens x 2560.
+    float* rows = reinterpret_cast<float*>(s_x);
+    float* to = p.acc + static_cast<size_t>(blockIdx.x) * p.T * p.K;
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
+    for (int half = 0; half < 2; ++half) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < KBW; ++i) {
+            const int kb = warp + kFewHeadWarps * i;
+            if (kb < kbs) {
 #pragma unroll
                 for (int q = 0; q < 2; ++q)
 #pragma unroll
@@ -368,16 +448,15 @@ head_few_grads_kernel(const HeadFewParams p) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             // D row g or g + 8 = j 2 q or 2 q + 1, its column g / 2 * 8 + 2 j + g % 2 of the block; D column = token
-                            const int c = (warp & 3) * 64 + kb * 32 + (g >> 1) * 8 + 2 * (2 * q + (e >> 1)) + (g & 1);
-                            float& to = s_dx[c][nt * 8 + 2 * t4 + (e & 1)];
-                            to = turn == 0 ? acc[kb][q][nt][e] : to + acc[kb][q][nt][e];
+                            const int c = kb * 32 + (g >> 1) * 8 + 2 * (2 * q + (e >> 1)) + (g & 1), t = nt * 8 + 2 * t4 + (e & 1) - half * 4 * NT;
+                            if (t >= 0 && t < 4 * NT) rows[t * p.K + c] = acc[i][q][nt][e];
                         }
+            }
         }
         __syncthreads();
-    }
-    for (int i = threadIdx.x; i < 256 * p.T; i += kFewHeadThreads) {
-        const int c = i & 255, t = i >> 8;
-        if (slab * 256 + c < p.K) p.acc[(static_cast<size_t>(range) * p.T + t) * p.K + slab * 256 + c] = s_dx[c][t];
+        const int count = min(4 * NT, p.T - half * 4 * NT) * (p.K >> 2);
+        float4* out = reinterpret_cast<float4*>(to + static_cast<size_t>(half) * 4 * NT * p.K);
+        for (int i = tid; i < count; i += kFewHeadThreads) out[i] = reinterpret_cast<const float4*>(rows)[i];
     }
 }
 

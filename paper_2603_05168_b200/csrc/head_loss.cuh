@@ -10,7 +10,6 @@ struct HeadPlan {
     bool few;                     // head_few_mma.cuh
     bool words;                   // logits by head_words_tcgen05.cuh, gradients as for any number of tokens
     int tokens, groups, word_pairs;   // words: tokens per tile and groups of them, CTA pairs
-    int slabs, ranges, per;       // its gradient kernel: 256-column slabs x ranges of `per` blocks of 16 words
     int bn, parts;                // forward: columns per tile, partial sums per row
     int piece;                    // backward: columns of dz at a time (a multiple of 256)
     int bn_piece;                 // columns per tile of the pieces' logits
@@ -42,13 +41,8 @@ static HeadPlan head_plan(int T, int N, int K) {
     HeadPlan h{};
     h.few = head_few_takes(T, K);
     if (h.few) {
-        const int blocks = (N + 15) / 16;
-        h.parts = std::min(blocks, kNumSMs);
-        h.slabs = (K + 255) / 256;
-        h.per = (blocks + kNumSMs / h.slabs - 1) / (kNumSMs / h.slabs);
-        h.ranges = (blocks + h.per - 1) / h.per;
-        h.slots = h.ranges;
-        h.piece = static_cast<int>(head_up(N, 16));
+        h.parts = std::min((N + 15) / 16, kNumSMs);
+        h.slots = std::min((N + head_few_words(T, K) - 1) / head_few_words(T, K), kNumSMs);
         return h;
     }
     h.rows64 = head_up(T, 64);
@@ -114,7 +108,7 @@ static HeadWs head_ws_layout(const HeadPlan& h, bool backward, int T, int K, int
         w.part = take(8 * t * h.parts);
         if (top) w.part1 = take(4 * t * h.parts);
     } else {
-        w.dz = take(2 * static_cast<size_t>(h.few ? T : h.rows256) * h.piece);
+        if (!h.few) w.dz = take(2 * static_cast<size_t>(h.rows256) * h.piece);
         w.acc = take(4 * static_cast<size_t>(h.slots) * t * K);
     }
     w.total = at;
@@ -243,22 +237,34 @@ static sbn_status launch_head_dx(const HeadDxJob& j, cudaStream_t stream) {
 }
 
 // ---- few tokens ------------------------------------------------------------------------------------
-template <int KBW, int NT, int MODE>
-static sbn_status launch_head_few_as(const HeadFewParams& p, int ctas, bool list, bool dual, cudaStream_t stream) {
-    auto* kernel = !list ? head_few_kernel<KBW, NT, MODE, false, false> : (dual ? head_few_kernel<KBW, NT, MODE, true, true> : head_few_kernel<KBW, NT, MODE, true, false>);
-    if (launch_kernel(kernel, dim3(ctas), dim3(kFewHeadThreads), 0, stream, p) != cudaSuccess) return SBN_ERR_CUDA;
+template <bool BACKWARD, int KBW, int NT, bool LIST, bool DUAL>
+static sbn_status launch_head_few_as(const HeadFewParams& p, int ctas, cudaStream_t stream) {
+    cudaError_t err;
+    if constexpr (BACKWARD) {
+        if (!ensure_dynamic_smem<head_few_backward_kernel<KBW, NT, LIST, DUAL>>(160 * 1024)) return SBN_ERR_CUDA;
+        err = launch_kernel(head_few_backward_kernel<KBW, NT, LIST, DUAL>, dim3(ctas), dim3(kFewHeadThreads), head_few_x_bytes(p.T, p.K), stream, p);
+    } else {
+        err = launch_kernel(head_few_forward_kernel<KBW, NT, LIST, DUAL>, dim3(ctas), dim3(kFewHeadThreads), 0, stream, p);
+    }
+    if (err != cudaSuccess) return SBN_ERR_CUDA;
     ++g_launch_count;
     return SBN_OK;
 }
-template <int MODE>
+template <bool BACKWARD, int KBW, int NT>
+static sbn_status launch_head_few_of(const HeadFewParams& p, int ctas, bool list, bool dual, cudaStream_t stream) {
+    if (!list) return launch_head_few_as<BACKWARD, KBW, NT, false, false>(p, ctas, stream);
+    return dual ? launch_head_few_as<BACKWARD, KBW, NT, true, true>(p, ctas, stream) : launch_head_few_as<BACKWARD, KBW, NT, true, false>(p, ctas, stream);
+}
+template <bool BACKWARD>
 static sbn_status launch_head_few(const HeadFewParams& p, int ctas, bool list, bool dual, cudaStream_t stream) {
+    const int shares = head_few_shares(p.K);
     if (p.T <= 8) {
-        if (p.K <= 1024) return launch_head_few_as<2, 1, MODE>(p, ctas, list, dual, stream);
-        if (p.K <= 2560) return launch_head_few_as<5, 1, MODE>(p, ctas, list, dual, stream);
-        return launch_head_few_as<8, 1, MODE>(p, ctas, list, dual, stream);
+        if (shares == 2) return launch_head_few_of<BACKWARD, 2, 1>(p, ctas, list, dual, stream);
+        if (shares == 5) return launch_head_few_of<BACKWARD, 5, 1>(p, ctas, list, dual, stream);
+        return launch_head_few_of<BACKWARD, 8, 1>(p, ctas, list, dual, stream);
     }
-    if (p.K <= 1024) return launch_head_few_as<2, 2, MODE>(p, ctas, list, dual, stream);
-    return launch_head_few_as<5, 2, MODE>(p, ctas, list, dual, stream);
+    if (shares == 2) return launch_head_few_of<BACKWARD, 2, 2>(p, ctas, list, dual, stream);
+    return launch_head_few_of<BACKWARD, 5, 2>(p, ctas, list, dual, stream);
 }
 static HeadFewParams head_few_params(const HeadCall& c, const HeadTargets& tg) {
     HeadFewParams p{};
@@ -283,7 +289,7 @@ static sbn_status head_few_forward(const HeadCall& c, const HeadPlan& h, float* 
     p.part = reinterpret_cast<float2*>(c.ws + w.part);
     p.part1 = dual ? reinterpret_cast<float*>(c.ws + w.part1) : nullptr;
     p.z_ev = reinterpret_cast<float*>(c.ws + w.z_ev);
-    st = launch_head_few<0>(p, h.parts, list, dual, stream);
+    st = launch_head_few<false>(p, h.parts, list, dual, stream);
     if (st != SBN_OK) return st;
     return launch_head_losses(HeadLossJob{tg, nullptr, nullptr, c.T, c.N, p.part, p.part1, p.z_ev, nullptr, nullptr, c.K, h.parts, 1.0 / static_cast<double>(c.tau), loss0, loss1, lse0, lse1},
                               stream);
@@ -301,17 +307,10 @@ static sbn_status head_few_backward(const HeadCall& c, const HeadPlan& h, const 
     p.job = job;
     p.lse0 = lse0; p.lse1 = lse1;
     p.scale = HeadScale{g0, g1, p.inv_tau, reinterpret_cast<float*>(c.ws + w.scale)};
-    p.dz = reinterpret_cast<uint16_t*>(c.ws + w.dz);
-    p.ldz = h.piece;
-    st = launch_head_few<1>(p, h.parts, list, dual, stream);
-    if (st != SBN_OK) return st;
     p.dw = static_cast<uint16_t*>(dhead);
     p.acc = dx ? reinterpret_cast<float*>(c.ws + w.acc) : nullptr;
-    p.slabs = h.slabs;
-    p.per = h.per;
-    auto* kernel = c.T <= 8 ? head_few_grads_kernel<1> : head_few_grads_kernel<2>;
-    if (launch_kernel(kernel, dim3(h.slabs * h.ranges), dim3(kFewHeadThreads), 0, stream, p) != cudaSuccess) return SBN_ERR_CUDA;
-    ++g_launch_count;
+    st = launch_head_few<true>(p, h.slots, list, dual, stream);
+    if (st != SBN_OK) return st;
     return dx ? launch_head_dx(HeadDxJob{nullptr, p.acc, h.slots, c.T, c.K, p.scale.out, static_cast<uint16_t*>(dx)}, stream) : SBN_OK;
 }
 

@@ -126,8 +126,8 @@ def test_cross_entropy_no_row_left_out(T, N, K):
 
 # few tokens: the register-fed kernels' widths (up to 8 or 16 tokens; K in one, two, five, eight shares of 512, ragged) and the
 # sizes on either side of them
-@pytest.mark.parametrize("top", [0, 7])
-@pytest.mark.parametrize("T,N,K", [(1, 4099, 1024), (1, 17, 4096), (3, 2500, 640), (7, 1000, 2560), (8, 16, 512), (8, 5003, 1152), (8, 999, 3200), (9, 15, 128),
+@pytest.mark.parametrize("top", [0, 7, 64, 65, 100])
+@pytest.mark.parametrize("T,N,K", [(16, 4001, 128), (8, 1300, 256), (1, 4099, 1024), (1, 17, 4096), (3, 2500, 640), (7, 1000, 2560), (8, 16, 512), (8, 5003, 1152), (8, 999, 3200), (9, 15, 128),
                                    (9, 3000, 2560), (13, 1601, 1024), (16, 2401, 2560), (16, 700, 2688), (9, 700, 4096), (8, 300, 4224), (17, 333, 512)])
 def test_few_tokens(T, N, K, top):
     check(make(T, N, K, seed=T + N + K, top=top))
