@@ -77,7 +77,8 @@ __device__ __forceinline__ void few_targets(const HeadFewParams& p, FewTargets<N
     if (LIST && p.job.index != nullptr) {
         if (warp < p.T) {
             int* col = room + warp * 2 * kFewOwnEvents;
-            const int flags = warp_targets(p.job, warp, lane, col, reinterpret_cast<float*>(col + kFewOwnEvents), [&](int place, int c, float v) {
+            int heaviest;                                       // (for nobody: with few tokens every logit is summed well enough)
+            const int flags = warp_targets(p.job, warp, lane, col, reinterpret_cast<float*>(col + kFewOwnEvents), &heaviest, [&](int place, int c, float v) {
                 s.col[LIST ? warp : 0][place] = c;
                 s.w[LIST ? warp : 0][place] = v;
                 if (blockIdx.x == 0) {

@@ -84,7 +84,7 @@ static HeadPlan head_plan(int T, int N, int K) {
 
 // Workspace of a call, in bytes from its start.
 struct HeadWs {
-    size_t count, scale, row_src, row_of, flags, ev_col, ev_w, xc, z_ev, part, part1, dz, acc, total;
+    size_t count, scale, row_src, row_of, flags, ev_col, ev_w, ev_top, xc, z_ev, part, part1, dz, acc, total;
 };
 static HeadWs head_ws_layout(const HeadPlan& h, bool backward, int T, int K, int top) {
     HeadWs w{};
@@ -101,6 +101,7 @@ static HeadWs head_ws_layout(const HeadPlan& h, bool backward, int T, int K, int
         w.flags = take(t);
         w.ev_col = take(4 * t * events);
         w.ev_w = take(4 * t * events);
+        w.ev_top = take(4 * t);
     }
     if (!h.few && !(h.words && !backward)) w.xc = take(2 * static_cast<size_t>(h.rows64) * K);
     if (!backward) {
@@ -186,12 +187,12 @@ static sbn_status launch_head_words(const HeadMaps& maps, const HeadWordsParams&
 // What is asked of the tokens: the labels themselves, or for a distillation the sorted targets of every token.
 // `later`: the job for a kernel that does it itself.
 static sbn_status launch_head_targets(const HeadCall& c, const HeadWs& w, HeadTargets* tg, cudaStream_t stream, HeadTargetsJob* later = nullptr) {
-    *tg = HeadTargets{c.labels, nullptr, nullptr, nullptr, 1};
+    *tg = HeadTargets{c.labels, nullptr, nullptr, nullptr, nullptr, 1};
     if (!c.top) return SBN_OK;
     HeadTargetsJob t{c.top_index, c.top_logits, c.top_bf16, c.top, c.T, c.N, static_cast<float>(1.0 / static_cast<double>(c.tau)), c.labels,
                      reinterpret_cast<unsigned char*>(c.ws + w.flags), reinterpret_cast<int*>(c.ws + w.ev_col),
-                     reinterpret_cast<float*>(c.ws + w.ev_w)};
-    *tg = HeadTargets{c.labels, t.flags, t.ev_col, t.ev_w, c.top + (c.labels ? 1 : 0)};
+                     reinterpret_cast<float*>(c.ws + w.ev_w), reinterpret_cast<int*>(c.ws + w.ev_top)};
+    *tg = HeadTargets{c.labels, t.flags, t.ev_col, t.ev_w, t.ev_top, c.top + (c.labels ? 1 : 0)};
     if (later && tg->events <= kFewOwnEvents) {
         *later = t;
         return SBN_OK;

@@ -30,6 +30,7 @@ struct HeadTargets {
     const unsigned char* flags;                   // [T], distillation only
     const int* ev_col;                            // [T][events]
     const float* ev_w;
+    const int* ev_top;                            // [T]: the entry with the largest probability
     int events;
 };
 
@@ -77,13 +78,14 @@ struct HeadTargetsJob {
     unsigned char* flags;
     int* ev_col;
     float* ev_w;
+    int* ev_top;
 };
 
-// A token's targets, by a warp: flags; put(place, column, weight) gets the entries in order.  col, val: shared memory for top + 1
+// A token's targets, by a warp: flags; put(place, column, weight) gets the entries in order; *top_place: of the heaviest one.  col, val: shared memory for top + 1
 // and top entries.  The place of an entry is the number of entries before it (column, then position): top is at most 256, so
 // counting costs less than a sorting network's exchanges would.
 template <class Put>
-__device__ __forceinline__ int warp_targets(const HeadTargetsJob& j, long long t, int lane, int* col, float* val, Put&& put) {
+__device__ __forceinline__ int warp_targets(const HeadTargetsJob& j, long long t, int lane, int* col, float* val, int* top_place, Put&& put) {
     const int events = j.top + (j.labels != nullptr ? 1 : 0);
     const long long* index = j.index + t * j.top;
     float top_val = -INFINITY;
@@ -119,12 +121,16 @@ __device__ __forceinline__ int warp_targets(const HeadTargetsJob& j, long long t
         if (lane == 0) col[j.top] = (flags & kRowLabel) ? static_cast<int>(y) : kNoColumn;
     }
     __syncwarp();
+    int heaviest = kNoColumn;
     for (int i = lane; i < events; i += 32) {
         const int c = col[i];
         int place = 0;
         for (int o = 0; o < events; ++o) place += (col[o] < c || (col[o] == c && o < i)) ? 1 : 0;
         put(place, c, i == j.top ? -1.0f : (c == kNoColumn ? 0.0f : val[i] / sum));
+        if (i < j.top && c != kNoColumn && val[i] == 1.0f) heaviest = min(heaviest, place);    // exp of nothing: the largest logit
     }
+    heaviest = __reduce_min_sync(0xFFFFFFFFu, heaviest);
+    *top_place = heaviest < events ? heaviest : 0;           // (none if a logit is no number)
     return flags;
 }
 
@@ -140,12 +146,14 @@ head_targets_kernel(const HeadTargetsJob j) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int events = j.top + (j.labels != nullptr ? 1 : 0);
     for (long long t = static_cast<long long>(blockIdx.x) * kTargetWarps + warp; t < j.T; t += static_cast<long long>(gridDim.x) * kTargetWarps) {
-        const int flags = warp_targets(j, t, lane, s_col[warp], s_val[warp], [&](int place, int c, float w) {
+        int heaviest;
+        const int flags = warp_targets(j, t, lane, s_col[warp], s_val[warp], &heaviest, [&](int place, int c, float w) {
             j.ev_col[t * events + place] = c;
             j.ev_w[t * events + place] = w;
         });
         if (lane == 0) {
             j.flags[t] = static_cast<unsigned char>(flags);
+            j.ev_top[t] = heaviest;
             report_bad(flags);
         }
         __syncwarp();
@@ -269,13 +277,29 @@ struct HeadLossJob {
 
 constexpr int kLossThreads = 128;
 
+// A thread's share of x[t] . w[word].
+__device__ __forceinline__ float head_logit_share(const HeadLossJob& j, int t, long long word, int tid) {
+    const uint4* a = reinterpret_cast<const uint4*>(j.x + static_cast<size_t>(t) * j.K);
+    const uint4* b = reinterpret_cast<const uint4*>(j.w + static_cast<size_t>(word) * j.K);
+    float lo = 0.0f, hi = 0.0f;
+#pragma unroll 4
+    for (int i = tid; i < j.K >> 3; i += kLossThreads) {
+        const uint4 u = __ldg(a + i), v = __ldg(b + i);
+        lo = fmaf(bf16lo_to_f32(u.x), bf16lo_to_f32(v.x), lo); hi = fmaf(bf16hi_to_f32(u.x), bf16hi_to_f32(v.x), hi);
+        lo = fmaf(bf16lo_to_f32(u.y), bf16lo_to_f32(v.y), lo); hi = fmaf(bf16hi_to_f32(u.y), bf16hi_to_f32(v.y), hi);
+        lo = fmaf(bf16lo_to_f32(u.z), bf16lo_to_f32(v.z), lo); hi = fmaf(bf16hi_to_f32(u.z), bf16hi_to_f32(v.z), hi);
+        lo = fmaf(bf16lo_to_f32(u.w), bf16lo_to_f32(v.w), lo); hi = fmaf(bf16hi_to_f32(u.w), bf16hi_to_f32(v.w), hi);
+    }
+    return lo + hi;
+}
+
 // A CTA per row, everything it reads under way at once: a call with few rows waits for latencies only.  Sums in double: a loss
 // is the small difference of two numbers near each other, and this is a few hundred operations per token.
 __global__ void __launch_bounds__(kLossThreads)
 head_losses_kernel(const HeadLossJob j) {
     constexpr int kWarps = kLossThreads / 32;
     __shared__ float s_f[2][kWarps];
-    __shared__ double s_d[4][kWarps];
+    __shared__ double s_d[6][kWarps];
     pdl_launch_dependents();
     pdl_wait();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -315,26 +339,21 @@ head_losses_kernel(const HeadLossJob j) {
                 s1 += w[q] * expf(v[q].x - m);
             }
         }
-        // The label's logit once more, in fp32 on the ordinary units: the tensor cores cut every partial sum off, always
-        // towards zero, which is no matter in lse but shows in the difference (relative error of the loss 2e-6, now 5e-7).
-        float dot = 0.0f;
-        if (j.x != nullptr && (flags & kRowLabel)) {
-            const uint4* a = reinterpret_cast<const uint4*>(j.x + static_cast<size_t>(t) * j.K);
-            const uint4* b = reinterpret_cast<const uint4*>(j.w + static_cast<size_t>(j.tg.labels[t]) * j.K);
-            float lo = 0.0f, hi = 0.0f;
-#pragma unroll 4
-            for (int i = tid; i < j.K >> 3; i += kLossThreads) {
-                const uint4 u = __ldg(a + i), v = __ldg(b + i);
-                lo = fmaf(bf16lo_to_f32(u.x), bf16lo_to_f32(v.x), lo); hi = fmaf(bf16hi_to_f32(u.x), bf16hi_to_f32(v.x), hi);
-                lo = fmaf(bf16lo_to_f32(u.y), bf16lo_to_f32(v.y), lo); hi = fmaf(bf16hi_to_f32(u.y), bf16hi_to_f32(v.y), hi);
-                lo = fmaf(bf16lo_to_f32(u.z), bf16lo_to_f32(v.z), lo); hi = fmaf(bf16hi_to_f32(u.z), bf16hi_to_f32(v.z), hi);
-                lo = fmaf(bf16lo_to_f32(u.w), bf16lo_to_f32(v.w), lo); hi = fmaf(bf16hi_to_f32(u.w), bf16hi_to_f32(v.w), hi);
+        // The logits of the label and of the teacher's heaviest entry once more, in fp32 on the ordinary units: the tensor cores cut
+        // every partial sum off, always towards zero, which is no matter in lse but shows in the difference to a large logit
+        // (relative error of the losses 2e-6, with this 5e-7).
+        float dot = 0.0f, dot_top = 0.0f;
+        int heaviest = -1;
+        if (j.x != nullptr) {
+            if (flags & kRowLabel) dot = head_logit_share(j, t, j.tg.labels[t], tid);
+            if (j.tg.flags != nullptr && (flags & kRowDistill)) {
+                heaviest = j.tg.ev_top[t];
+                dot_top = head_logit_share(j, t, j.tg.ev_col[static_cast<size_t>(t) * j.tg.events + heaviest], tid);
             }
-            dot = lo + hi;
         }
         // the teacher's entries: sum of q, and of q (log q - z / tau), to which q lse is added in the end
         double q_sum = 0.0, kd = 0.0;
-        float z_ev = 0.0f;
+        float z_ev = 0.0f, q_top = 0.0f;
         if (j.tg.flags != nullptr) {
             for (int i = tid; i < j.tg.events; i += kLossThreads) {
                 if (j.tg.ev_col[static_cast<size_t>(t) * j.tg.events + i] == kNoColumn) continue;
@@ -342,9 +361,10 @@ head_losses_kernel(const HeadLossJob j) {
                 if (q < 0.0f) {                               // the label's entry
                     if (j.x == nullptr) z_ev = j.z_ev[static_cast<size_t>(r) * j.tg.events + i];
                 } else if (!(q == 0.0f)) {
-                    const double z = static_cast<double>(j.z_ev[static_cast<size_t>(r) * j.tg.events + i]);
+                    const double z = i == heaviest ? 0.0 : static_cast<double>(j.z_ev[static_cast<size_t>(r) * j.tg.events + i]);
                     q_sum += static_cast<double>(q);
                     kd += static_cast<double>(q) * (static_cast<double>(logf(q)) - z * j.inv_tau);
+                    if (i == heaviest) q_top = q;
                 }
             }
         } else if (j.x == nullptr && tid == 0) {
@@ -358,17 +378,18 @@ head_losses_kernel(const HeadLossJob j) {
 #pragma unroll
         for (int w = 1; w < kWarps; ++w) top = fmaxf(top, s_f[0][w]);
         const float down = m == -INFINITY ? 1.0f : expf((m - top) * tau_f);      // no part: s0 is 0 or no number
-        double sums[4] = {static_cast<double>(s0) * static_cast<double>(down), m == -INFINITY ? 0.0 : static_cast<double>(s1) * static_cast<double>(expf(m - top)), q_sum, kd};
+        double sums[6] = {static_cast<double>(s0) * static_cast<double>(down), m == -INFINITY ? 0.0 : static_cast<double>(s1) * static_cast<double>(expf(m - top)), q_sum, kd,
+                          static_cast<double>(dot_top), static_cast<double>(q_top)};
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) {
             dot += __shfl_xor_sync(0xFFFFFFFFu, dot, o);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) sums[k] += __shfl_xor_sync(0xFFFFFFFFu, sums[k], o);
+            for (int k = 0; k < 6; ++k) sums[k] += __shfl_xor_sync(0xFFFFFFFFu, sums[k], o);
         }
         if (lane == 0) {
             s_f[1][warp] = dot;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) s_d[k][warp] = sums[k];
+            for (int k = 0; k < 6; ++k) s_d[k][warp] = sums[k];
         }
         __syncthreads();
         if (tid == 0) {
@@ -376,7 +397,7 @@ head_losses_kernel(const HeadLossJob j) {
             for (int w = 1; w < kWarps; ++w) {
                 dot += s_f[1][w];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) sums[k] += s_d[k][w];
+                for (int k = 0; k < 6; ++k) sums[k] += s_d[k][w];
             }
             const double lse0 = static_cast<double>(top) * j.inv_tau + log(sums[0]);
             if (j.tg.flags == nullptr) {                      // cross entropy
@@ -384,7 +405,7 @@ head_losses_kernel(const HeadLossJob j) {
                 j.loss1[t] = static_cast<float>(lse0 - static_cast<double>(dot));
             } else {
                 const float bad = __uint_as_float(0x7FC00000u);
-                j.loss0[t] = (flags & kRowBadTeacher) ? bad : ((flags & kRowDistill) ? static_cast<float>(sums[3] + sums[2] * lse0) : 0.0f);
+                j.loss0[t] = (flags & kRowBadTeacher) ? bad : ((flags & kRowDistill) ? static_cast<float>(sums[3] - sums[5] * sums[4] * j.inv_tau + sums[2] * lse0) : 0.0f);
                 j.lse0[t] = (flags & kRowDistill) ? static_cast<float>(lse0) : 0.0f;
                 if (j.loss1 != nullptr) {
                     const double lse1 = static_cast<double>(top) + log(sums[1]);
