@@ -394,12 +394,21 @@ struct HeadGradsWork {
         dx_all = tiles_m() * tiles_n * slices;
         most = dx_all % kBackwardPairs;
         const int others = kBackwardPairs - most;
-        const float longer = (static_cast<float>(p.slot_stages) + 3.0f) / (fmaxf(static_cast<float>((rows + 63) / 64), 7.5f) + 3.0f);
-        const float each = (static_cast<float>(dw_all) - (most != 0 ? others * longer : 0.0f)) / kBackwardPairs;
-        dw_each = max(0, static_cast<int>(floorf(each)));
-        const int rest = dw_all - dw_each * kBackwardPairs;
-        dw_extra = rest / others;
-        dw_left = rest % others;
+        // stages of a tile, with its turnaround; a tile of dW takes as long as it takes to write
+        const float dx_cost = static_cast<float>(p.slot_stages) + 3.0f, dw_cost = fmaxf(static_cast<float>((rows + 63) / 64), 7.5f) + 3.0f;
+        const float each = (static_cast<float>(dw_all) - (most != 0 ? others * dx_cost / dw_cost : 0.0f)) / kBackwardPairs;
+        float best = INFINITY;
+        for (int up = 0; up < 2; ++up) {                // the even share, rounded down or up: whichever ends sooner
+            const int n = min(max(0, static_cast<int>(floorf(each)) + up), dw_all / kBackwardPairs);
+            const int rest = dw_all - n * kBackwardPairs, extra = rest / others, left = rest % others;
+            const float end = fmaxf((n + extra + (left != 0 ? 1 : 0)) * dw_cost, most != 0 ? dx_cost + n * dw_cost : 0.0f);
+            if (end < best) {
+                best = end;
+                dw_each = n;
+                dw_extra = extra;
+                dw_left = left;
+            }
+        }
     }
     __device__ int dx_of(int pair) const { return dx_all / kBackwardPairs + (pair < most ? 1 : 0); }
     // The i-th tile of dW of a pair, -1: no more.
