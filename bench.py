@@ -1075,6 +1075,53 @@ def run_backward(args):
                       "peak_source": f"{peaks['source']} bf16 burst {peaks['bf16_tflops']} TFLOP/s", "gpu_launches": b.sbn_launch_count()}))
 
 
+def run_head(args):
+    """The losses at the output head of a 2B-shaped model (hidden 2560, vocabulary 32000, bf16 head): cross entropy and distillation
+    from a teacher's 32 largest logits, forward and backward calls for 1 to 4096 tokens, cold L2; --only-step: 1024 tokens alone (the
+    small case for profiler runs).  TFLOP/s count 2 T N K operations forward and 6 T N K backward (dx, dW and z once more)."""
+    import torch
+    from paper_2603_05168_b200 import binding as b
+    from paper_2603_05168_b200 import build as sbn_build
+    sbn_build.build()
+    torch.cuda.set_device(int(os.environ.get("LOCAL_RANK", "0")))
+    if int(os.environ.get("RANK", "0")) != 0:
+        return
+    peaks = load_peaks()
+    stream = torch.cuda.current_stream()
+    flush = torch.empty(512 * 1024 * 1024, dtype=torch.uint8, device="cuda")
+    time_cold, iters = _cold_timer(torch, stream, flush), 3 if args.only_step else 12
+    K, N, top, tau = inputs.SHAPES_2B[1][1], 32000, 32, 2.0
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    head = (torch.randn(N, K, generator=gen, device="cuda") * 0.02).to(torch.bfloat16)
+    dhead = torch.empty_like(head)
+    rows = []
+    for T in ([1024] if args.only_step else [1, 16, 128, 1024, 4096]):
+        x = torch.randn(T, K, generator=gen, device="cuda").to(torch.bfloat16)
+        labels = torch.randint(0, N, (T,), generator=gen, device="cuda")
+        index = torch.randint(0, N, (T, top), generator=gen, device="cuda")
+        logits = torch.randn(T, top, generator=gen, device="cuda")
+        loss, lse, dx, d = torch.empty(T, device="cuda"), torch.empty(1, T, device="cuda"), torch.empty_like(x), torch.full((T,), 1.0 / T, device="cuda")
+        ws = [b.alloc_head_ws(T, N, K, top=k, backward=w) for k in (0, top) for w in (False, True)]
+        calls = {
+            "cross_entropy_us": lambda: b.sbn_head_cross_entropy(x, head, labels, loss, lse[0], ws=ws[0]),
+            "cross_entropy_backward_us": lambda: b.sbn_head_cross_entropy_backward(x, head, labels, lse[0], d, dx=dx, dhead=dhead, ws=ws[1]),
+            "distill_us": lambda: b.sbn_head_distill(x, head, index, logits, tau, loss, lse, ws=ws[2]),
+            "distill_backward_us": lambda: b.sbn_head_distill_backward(x, head, index, logits, tau, lse, d, dx=dx, dhead=dhead, ws=ws[3]),
+        }
+        row = {"tokens": T}
+        for name, fn in calls.items():
+            for _ in range(2):
+                fn()
+            row[name] = round(time_cold(fn, iters), 2)
+        row["forward_tflops"] = round(2.0 * T * N * K / row["cross_entropy_us"] / 1e6, 1)
+        row["backward_tflops"] = round(6.0 * T * N * K / row["cross_entropy_backward_us"] / 1e6, 1)
+        rows.append(row)
+    b.sbn_check_status()
+    print(json.dumps({"metric": "losses at the output head (cross entropy, distillation from a teacher's top logits) and their gradients", "unit": "us",
+                      "workload": "head", "hidden": K, "vocabulary": N, "teacher_entries": top, "rows": rows,
+                      "peak_source": f"{peaks['source']} bf16 burst {peaks['bf16_tflops']} TFLOP/s", "gpu_launches": b.sbn_launch_count()}))
+
+
 def run_mma_probe(args):
     """What the K-loop of the large-T GEMM kernel costs, piece by piece (timing only: with a probe flag set
     the kernel's results are wrong).  One tile per CTA pair (74 feature tiles x one token tile), so nothing
@@ -1163,14 +1210,15 @@ def main():
     ap.add_argument("--no-cpu-baseline", action="store_true")
     ap.add_argument("--no-extras", action="store_true",
                     help="headline line only: skip the 7B-class isolated GEMMs, the sustained run and the few-token rows")
-    ap.add_argument("--workload", default="2b", choices=sorted(WORKLOADS) + ["decode", "decode7b", "dyn", "p68", "mmaprobe", "bwd"],
+    ap.add_argument("--workload", default="2b", choices=sorted(WORKLOADS) + ["decode", "decode7b", "dyn", "p68", "mmaprobe", "bwd", "head"],
                     help="2b = the headline workload; 7b / down7b = 7B-class shapes (down7b: one layer, for profiling); "
                          "decode = small-T sweep (T in 1..512), sparse vs dense, cold L2 and streamed; "
                          "decode7b = the same on 7B-class matrices at T <= 64, with the 2-bit packed weights as a third arm; "
                          "dyn = dynamic-mask training step: re-pack 30 x 7 matrices + forward at T=2048; "
                          "p68 = the 6:8 pattern next to 2:4 and dense on the same matrices; "
                          "mmaprobe = timing experiments on the large-T kernel's K-loop (loads, metadata copies, MMA issue); "
-                         "bwd = the layer's backward (dual straight-through estimator) on the 2B shapes")
+                         "bwd = the layer's backward (dual straight-through estimator) on the 2B shapes; "
+                         "head = the losses at the output head of a 2B-shaped model, forward and backward")
     ap.add_argument("--masters", default="fp32", choices=["fp32", "bf16"],
                     help="precision of the master weights the pack kernel reads (default fp32, the configuration of the metric)")
     ap.add_argument("--only-step", action="store_true", help="time the step only (used for profiler runs)")
@@ -1187,6 +1235,8 @@ def main():
         run_mma_probe(args)
     elif args.workload == "bwd":
         run_backward(args)
+    elif args.workload == "head":
+        run_head(args)
     else:
         run_ours(args)
 

@@ -292,7 +292,7 @@ static sbn_status head_few_forward(const HeadCall& c, const HeadPlan& h, float* 
     p.z_ev = reinterpret_cast<float*>(c.ws + w.z_ev);
     st = launch_head_few<false>(p, h.parts, list, dual, stream);
     if (st != SBN_OK) return st;
-    return launch_head_losses(HeadLossJob{tg, nullptr, nullptr, c.T, c.N, p.part, p.part1, p.z_ev, nullptr, nullptr, c.K, h.parts, 1.0 / static_cast<double>(c.tau), loss0, loss1, lse0, lse1},
+    return launch_head_losses(HeadLossJob{tg, nullptr, nullptr, c.T, c.N, p.part, p.part1, p.z_ev, nullptr, nullptr, c.K, h.parts, 1.0 / static_cast<double>(c.tau), 1.0, loss0, loss1, lse0, lse1},
                               stream);
 }
 
@@ -336,7 +336,8 @@ static sbn_status head_forward(const HeadCall& c, float* loss0, float* loss1, fl
     }
     p.T = c.T; p.N = c.N; p.K = c.K;
     p.v0 = 0; p.v1 = c.N; p.bn = h.bn;
-    p.c0 = static_cast<float>(1.4426950408889634 / static_cast<double>(c.tau));
+    p.c0 = static_cast<float>(1.4426950408889634 * head_logit_scale(c.K) / static_cast<double>(c.tau));
+    p.c1 = static_cast<float>(1.4426950408889634 * head_logit_scale(c.K));
     p.part = reinterpret_cast<float2*>(c.ws + w.part);
     p.part1 = dual ? reinterpret_cast<float*>(c.ws + w.part1) : nullptr;
     p.z_ev = reinterpret_cast<float*>(c.ws + w.z_ev);
@@ -346,8 +347,8 @@ static sbn_status head_forward(const HeadCall& c, float* loss0, float* loss1, fl
                  : launch_head_logits<0>(maps, p, list, dual, stream);
     if (st != SBN_OK) return st;
     return launch_head_losses(HeadLossJob{p.tg, p.count, p.row_src, c.T, c.N, p.part, p.part1, p.z_ev, static_cast<const uint16_t*>(c.x),
-                                          static_cast<const uint16_t*>(c.head), c.K, h.parts, 1.0 / static_cast<double>(c.tau), loss0, loss1, lse0,
-                                          lse1}, stream);
+                                          static_cast<const uint16_t*>(c.head), c.K, h.parts, 1.0 / static_cast<double>(c.tau),
+                                          head_logit_scale(c.K), loss0, loss1, lse0, lse1}, stream);
 }
 
 template <bool WIDE>
@@ -391,7 +392,8 @@ static sbn_status head_backward(const HeadCall& c, const float* lse0, const floa
     }
     p.T = c.T; p.N = c.N; p.K = c.K;
     p.bn = h.bn_piece;
-    p.c0 = static_cast<float>(1.4426950408889634 / static_cast<double>(c.tau));
+    p.c0 = static_cast<float>(1.4426950408889634 * head_logit_scale(c.K) / static_cast<double>(c.tau));
+    p.c1 = static_cast<float>(1.4426950408889634 * head_logit_scale(c.K));
     p.inv_tau = static_cast<float>(1.0 / static_cast<double>(c.tau));
     p.lse0 = lse0; p.lse1 = lse1; p.g0 = g0; p.g1 = g1;
     p.skip_loads = g_test_break_waits;

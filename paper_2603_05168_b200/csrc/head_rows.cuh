@@ -272,6 +272,7 @@ struct HeadLossJob {
     int K;
     int parts;
     double inv_tau;
+    double z_scale;                               // of the logits in part and z_ev (head_logit_scale)
     float *loss0, *loss1, *lse0, *lse1;           // at the tokens' own rows: distillation, label.  Cross entropy: loss1 and lse0
 };
 
@@ -304,7 +305,7 @@ head_losses_kernel(const HeadLossJob j) {
     pdl_wait();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rows = j.count != nullptr ? *j.count : j.T;
-    const float tau_f = static_cast<float>(j.inv_tau);
+    const float tau_f = static_cast<float>(j.inv_tau * j.z_scale), one_f = static_cast<float>(j.z_scale);
     for (int r = blockIdx.x; r < rows; r += gridDim.x) {
         const int t = j.count != nullptr ? j.row_src[r] : r;
         const int flags = head_token_flags(j.tg, t, j.N);
@@ -331,12 +332,12 @@ head_losses_kernel(const HeadLossJob j) {
                 continue;
             }
             s0 *= expf((m - top) * tau_f);
-            s1 *= expf(m - top);
+            s1 *= expf((m - top) * one_f);
             m = top;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 s0 += v[q].y * expf((v[q].x - m) * tau_f);
-                s1 += w[q] * expf(v[q].x - m);
+                s1 += w[q] * expf((v[q].x - m) * one_f);
             }
         }
         // The logits of the label and of the teacher's heaviest entry once more, in fp32 on the ordinary units: the tensor cores cut
@@ -361,7 +362,7 @@ head_losses_kernel(const HeadLossJob j) {
                 if (q < 0.0f) {                               // the label's entry
                     if (j.x == nullptr) z_ev = j.z_ev[static_cast<size_t>(r) * j.tg.events + i];
                 } else if (!(q == 0.0f)) {
-                    const double z = i == heaviest ? 0.0 : static_cast<double>(j.z_ev[static_cast<size_t>(r) * j.tg.events + i]);
+                    const double z = i == heaviest ? 0.0 : static_cast<double>(j.z_ev[static_cast<size_t>(r) * j.tg.events + i]) * j.z_scale;
                     q_sum += static_cast<double>(q);
                     kd += static_cast<double>(q) * (static_cast<double>(logf(q)) - z * j.inv_tau);
                     if (i == heaviest) q_top = q;
@@ -378,7 +379,7 @@ head_losses_kernel(const HeadLossJob j) {
 #pragma unroll
         for (int w = 1; w < kWarps; ++w) top = fmaxf(top, s_f[0][w]);
         const float down = m == -INFINITY ? 1.0f : expf((m - top) * tau_f);      // no part: s0 is 0 or no number
-        double sums[6] = {static_cast<double>(s0) * static_cast<double>(down), m == -INFINITY ? 0.0 : static_cast<double>(s1) * static_cast<double>(expf(m - top)), q_sum, kd,
+        double sums[6] = {static_cast<double>(s0) * static_cast<double>(down), m == -INFINITY ? 0.0 : static_cast<double>(s1) * static_cast<double>(expf((m - top) * one_f)), q_sum, kd,
                           static_cast<double>(dot_top), static_cast<double>(q_top)};
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) {
@@ -399,7 +400,7 @@ head_losses_kernel(const HeadLossJob j) {
 #pragma unroll
                 for (int k = 0; k < 6; ++k) sums[k] += s_d[k][w];
             }
-            const double lse0 = static_cast<double>(top) * j.inv_tau + log(sums[0]);
+            const double lse0 = static_cast<double>(top) * j.z_scale * j.inv_tau + log(sums[0]);
             if (j.tg.flags == nullptr) {                      // cross entropy
                 j.lse0[t] = static_cast<float>(lse0);
                 j.loss1[t] = static_cast<float>(lse0 - static_cast<double>(dot));
@@ -408,7 +409,7 @@ head_losses_kernel(const HeadLossJob j) {
                 j.loss0[t] = (flags & kRowBadTeacher) ? bad : ((flags & kRowDistill) ? static_cast<float>(sums[3] - sums[5] * sums[4] * j.inv_tau + sums[2] * lse0) : 0.0f);
                 j.lse0[t] = (flags & kRowDistill) ? static_cast<float>(lse0) : 0.0f;
                 if (j.loss1 != nullptr) {
-                    const double lse1 = static_cast<double>(top) + log(sums[1]);
+                    const double lse1 = static_cast<double>(top) * j.z_scale + log(sums[1]);
                     j.loss1[t] = (flags & kRowBadLabel) ? bad : ((flags & kRowLabel) ? static_cast<float>(lse1 - static_cast<double>(dot)) : 0.0f);
                     j.lse1[t] = (flags & kRowLabel) ? static_cast<float>(lse1) : 0.0f;
                 }
