@@ -34,7 +34,7 @@ struct HeadFewParams {
     const uint16_t* x;            // [T][K]
     const uint16_t* w;            // [N][K]
     int T, N, K;
-    float c0, inv_tau;
+    float c0, c1, inv_tau;        // log2(e) / tau and log2(e), times head_logit_scale
     float2* part;                 // stats: [T][parts], parts = CTAs
     float* part1;
     float* z_ev;                  // [T][events]
@@ -77,7 +77,7 @@ __device__ __forceinline__ void few_targets(const HeadFewParams& p, FewTargets<N
     if (LIST && p.job.index != nullptr) {
         if (warp < p.T) {
             int* col = room + warp * 2 * kFewOwnEvents;
-            int heaviest;                                       // (for nobody: with few tokens every logit is summed well enough)
+            int heaviest;
             const int flags = warp_targets(p.job, warp, lane, col, reinterpret_cast<float*>(col + kFewOwnEvents), &heaviest, [&](int place, int c, float v) {
                 s.col[LIST ? warp : 0][place] = c;
                 s.w[LIST ? warp : 0][place] = v;
@@ -90,6 +90,7 @@ __device__ __forceinline__ void few_targets(const HeadFewParams& p, FewTargets<N
                 s.flags[warp] = flags;
                 if (blockIdx.x == 0) {
                     p.job.flags[warp] = static_cast<unsigned char>(flags);
+                    p.job.ev_top[warp] = heaviest;
                     report_bad(flags);
                 }
             }
@@ -126,7 +127,6 @@ template <int KBW, int NT, bool LIST, bool DUAL>
 __global__ void __launch_bounds__(kFewHeadThreads, 1)
 head_few_forward_kernel(const HeadFewParams p) {
     constexpr int kTok = 8 * NT;
-    constexpr float kLog2e = 1.4426950408889634f;
     __shared__ float s_part[kFewHeadWarps][16][kTok];
     __shared__ FewTargets<NT, LIST> s_tg;
     pdl_launch_dependents();
@@ -164,7 +164,6 @@ head_few_forward_kernel(const HeadFewParams p) {
     // the word and token of this thread in every block
     const int tok = tid % kTok, slot = tid / kTok;
     const bool asked = slot < 16 && tok < p.T && (s_tg.flags[tok] & (kRowDistill | kRowLabel));
-    const int label = !LIST && asked ? static_cast<int>(p.tg.labels[tok]) : -1;
     float m = -INFINITY, s0 = 0.0f, s1 = 0.0f;
     FewCursor<NT, LIST> cursor(p, s_tg, tok, asked);
 
@@ -192,10 +191,9 @@ head_few_forward_kernel(const HeadFewParams p) {
             for (int v = 0; v < kFewHeadWarps; ++v) z += s_part[v][slot][tok];
             const float m_new = fmaxf(m, z);
             s0 = s0 * ex2_approx((m - m_new) * p.c0) + ex2_approx((z - m_new) * p.c0);
-            if (DUAL) s1 = s1 * ex2_approx((m - m_new) * kLog2e) + ex2_approx((z - m_new) * kLog2e);
+            if (DUAL) s1 = s1 * ex2_approx((m - m_new) * p.c1) + ex2_approx((z - m_new) * p.c1);
             m = m_new;
             cursor.template visit<16>(p, s_tg, tok, nb * 16, n, [&](int e) { p.z_ev[static_cast<size_t>(tok) * p.tg.events + e] = z; });
-            if (!LIST && n == label) p.z_ev[tok] = z;
         }
         __syncthreads();
     }
@@ -214,7 +212,7 @@ head_few_forward_kernel(const HeadFewParams p) {
             const float mq = red[q * kTok + tid], sq = red[(16 + q) * kTok + tid];
             if (mq == -INFINITY && sq == 0.0f) continue;           // a slot without words
             a0 += sq * ex2_approx((mq - mm) * p.c0);
-            if (DUAL) a1 += red[(32 + q) * kTok + tid] * ex2_approx((mq - mm) * kLog2e);
+            if (DUAL) a1 += red[(32 + q) * kTok + tid] * ex2_approx((mq - mm) * p.c1);
         }
         const size_t at = static_cast<size_t>(tid) * gridDim.x + blockIdx.x;
         p.part[at] = make_float2(mm, a0);
@@ -349,7 +347,7 @@ head_few_backward_kernel(const HeadFewParams p) {
             for (int o = 1; o < kParts; o <<= 1) z += __shfl_xor_sync(0xFFFFFFFFu, z, o);
             const float4 k = s_k[tok];
             float v = ex2_approx(fmaf(z, p.c0, k.x)) * k.y;
-            if (DUAL) v = fmaf(ex2_approx(fmaf(z, kLog2e, k.z)), k.w, v);
+            if (DUAL) v = fmaf(ex2_approx(fmaf(z, p.c1, k.z)), k.w, v);
             if constexpr (LIST) {
                 int2 cur = s_cursor[warp];
                 if (cur.y < (nb + 1) * kWords) {                    // the same for the warp

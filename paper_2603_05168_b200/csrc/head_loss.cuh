@@ -105,7 +105,7 @@ static HeadWs head_ws_layout(const HeadPlan& h, bool backward, int T, int K, int
     }
     if (!h.few && !(h.words && !backward)) w.xc = take(2 * static_cast<size_t>(h.rows64) * K);
     if (!backward) {
-        w.z_ev = take(4 * t * events);
+        if (top) w.z_ev = take(4 * t * events);
         w.part = take(8 * t * h.parts);
         if (top) w.part1 = take(4 * t * h.parts);
     } else {
@@ -273,7 +273,8 @@ static HeadFewParams head_few_params(const HeadCall& c, const HeadTargets& tg) {
     p.x = static_cast<const uint16_t*>(c.x);
     p.w = static_cast<const uint16_t*>(c.head);
     p.T = c.T; p.N = c.N; p.K = c.K;
-    p.c0 = static_cast<float>(1.4426950408889634 / static_cast<double>(c.tau));
+    p.c0 = static_cast<float>(1.4426950408889634 * head_logit_scale(c.K / kFewHeadWarps) / static_cast<double>(c.tau));     // a warp sums that much
+    p.c1 = static_cast<float>(1.4426950408889634 * head_logit_scale(c.K / kFewHeadWarps));
     p.inv_tau = static_cast<float>(1.0 / static_cast<double>(c.tau));
     return p;
 }
@@ -292,7 +293,8 @@ static sbn_status head_few_forward(const HeadCall& c, const HeadPlan& h, float* 
     p.z_ev = reinterpret_cast<float*>(c.ws + w.z_ev);
     st = launch_head_few<false>(p, h.parts, list, dual, stream);
     if (st != SBN_OK) return st;
-    return launch_head_losses(HeadLossJob{tg, nullptr, nullptr, c.T, c.N, p.part, p.part1, p.z_ev, nullptr, nullptr, c.K, h.parts, 1.0 / static_cast<double>(c.tau), 1.0, loss0, loss1, lse0, lse1},
+    return launch_head_losses(HeadLossJob{tg, nullptr, nullptr, c.T, c.N, p.part, p.part1, p.z_ev, p.x, p.w, c.K, h.parts, 1.0 / static_cast<double>(c.tau),
+                                          head_logit_scale(c.K / kFewHeadWarps), loss0, loss1, lse0, lse1},
                               stream);
 }
 

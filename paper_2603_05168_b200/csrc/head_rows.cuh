@@ -267,8 +267,8 @@ struct HeadLossJob {
     int T, N;
     const float2* part;                           // [rows][parts]: maximum m of the raw logits, sum of exp((z - m) / tau)
     const float* part1;                           // [rows][parts] or null: sum of exp(z - m)
-    const float* z_ev;                            // [rows][events]: logits at the teacher's entries; few tokens: at the label too
-    const uint16_t *x, *w;                        // null: few tokens
+    const float* z_ev;                            // [rows][events]: logits at the teacher's entries
+    const uint16_t *x, *w;
     int K;
     int parts;
     double inv_tau;
@@ -345,33 +345,26 @@ head_losses_kernel(const HeadLossJob j) {
         // (relative error of the losses 2e-6, with this 5e-7).
         float dot = 0.0f, dot_top = 0.0f;
         int heaviest = -1;
-        if (j.x != nullptr) {
-            if (flags & kRowLabel) dot = head_logit_share(j, t, j.tg.labels[t], tid);
-            if (j.tg.flags != nullptr && (flags & kRowDistill)) {
-                heaviest = j.tg.ev_top[t];
-                dot_top = head_logit_share(j, t, j.tg.ev_col[static_cast<size_t>(t) * j.tg.events + heaviest], tid);
-            }
+        if (flags & kRowLabel) dot = head_logit_share(j, t, j.tg.labels[t], tid);
+        if (flags & kRowDistill) {
+            heaviest = j.tg.ev_top[t];
+            dot_top = head_logit_share(j, t, j.tg.ev_col[static_cast<size_t>(t) * j.tg.events + heaviest], tid);
         }
         // the teacher's entries: sum of q, and of q (log q - z / tau), to which q lse is added in the end
         double q_sum = 0.0, kd = 0.0;
-        float z_ev = 0.0f, q_top = 0.0f;
+        float q_top = 0.0f;
         if (j.tg.flags != nullptr) {
             for (int i = tid; i < j.tg.events; i += kLossThreads) {
                 if (j.tg.ev_col[static_cast<size_t>(t) * j.tg.events + i] == kNoColumn) continue;
                 const float q = j.tg.ev_w[static_cast<size_t>(t) * j.tg.events + i];
-                if (q < 0.0f) {                               // the label's entry
-                    if (j.x == nullptr) z_ev = j.z_ev[static_cast<size_t>(r) * j.tg.events + i];
-                } else if (!(q == 0.0f)) {
+                if (!(q <= 0.0f)) {                           // (negative: the label's entry)
                     const double z = i == heaviest ? 0.0 : static_cast<double>(j.z_ev[static_cast<size_t>(r) * j.tg.events + i]) * j.z_scale;
                     q_sum += static_cast<double>(q);
                     kd += static_cast<double>(q) * (static_cast<double>(logf(q)) - z * j.inv_tau);
                     if (i == heaviest) q_top = q;
                 }
             }
-        } else if (j.x == nullptr && tid == 0) {
-            z_ev = j.z_ev[r];
         }
-        dot += z_ev;
         const float m_warp = warp_max(m);
         if (lane == 0) s_f[0][warp] = m_warp;
         __syncthreads();
