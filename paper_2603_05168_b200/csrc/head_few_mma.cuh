@@ -253,8 +253,12 @@ head_few_backward_kernel(const HeadFewParams p) {
     __shared__ float4 s_k[kTok];                                    // -lse log2(e) and gradient per loss (registers are for dx)
     __shared__ int s_label[kTok];
     __shared__ int2 s_cursor[kFewHeadWarps];                        // a warp's token's next target and its word
-    __shared__ __align__(16) uint16_t s_dz[kTok][kWords];           // B operand of dx: pairs of words of a token
-    __shared__ __align__(16) uint16_t s_dzt[kWords][kTok];          // A operand of dW: pairs of tokens of a word
+    // dz in bf16, and what that leaves off as well, in bf16 again: with few tokens a value of dW is a few products, and a gradient's
+    // own rounding to bf16 should be the only one that shows (1.7e-3 instead of 1.7e-3 to 3.6e-3 in the 2-norm; 8 tokens leave
+    // half of an MMA's indices free for it, 4 % of the time of a step).  Not for 16 tokens of more than 1024 columns: no registers
+    constexpr int kSplit = NT == 1 || KBW == 2 ? 2 : 1;
+    __shared__ __align__(16) uint16_t s_dz[kSplit][kTok][kWords];   // B operand of dx: pairs of words of a token
+    __shared__ __align__(16) uint16_t s_dzt[kSplit][kWords][kTok];  // A operand of dW: pairs of tokens of a word
     extern __shared__ __align__(16) uint8_t s_x[];
     pdl_launch_dependents();
     pdl_wait();
@@ -367,22 +371,28 @@ head_few_backward_kernel(const HeadFewParams p) {
                 v -= k.y;
             }
             if (n >= p.N || (k.y == 0.0f && k.w == 0.0f)) v = 0.0f;   // behind the vocabulary; nothing asked (z may be anything)
-            unsigned short o;
-            asm("cvt.rn.bf16.f32 %0, %1;" : "=h"(o) : "f"(v));
-            if (part == 0) {
-                s_dz[tok][slot] = o;
-                s_dzt[slot][tok] = o;
+#pragma unroll
+            for (int q = 0; q < kSplit; ++q) {
+                unsigned short o;
+                asm("cvt.rn.bf16.f32 %0, %1;" : "=h"(o) : "f"(v));
+                if (part == 0) {
+                    s_dz[q][tok][slot] = o;
+                    s_dzt[q][slot][tok] = o;
+                }
+                v -= __uint_as_float(static_cast<uint32_t>(o) << 16);
             }
         }
         __syncthreads();
-        uint32_t dz[NT][H], dzt[NT][2] = {};
+        uint32_t dz[kSplit][NT][H], dzt[kSplit][NT][2] = {};
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int q = 0; q < kSplit; ++q)
 #pragma unroll
-            for (int h = 0; h < H; ++h) {
-                dz[nt][h] = *reinterpret_cast<const uint32_t*>(&s_dz[nt * 8 + g][h * 8 + 2 * t4]);
-                dzt[nt][h] = *reinterpret_cast<const uint32_t*>(&s_dzt[h * 8 + g][nt * 8 + 2 * t4]);
-            }
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int h = 0; h < H; ++h) {
+                    dz[q][nt][h] = *reinterpret_cast<const uint32_t*>(&s_dz[q][nt * 8 + g][h * 8 + 2 * t4]);
+                    dzt[q][nt][h] = *reinterpret_cast<const uint32_t*>(&s_dzt[q][h * 8 + g][nt * 8 + 2 * t4]);
+                }
 #pragma unroll
         for (int i = 0; i < KBW; ++i) {
             const int kb = warp + kFewHeadWarps * i;
@@ -396,10 +406,15 @@ head_few_backward_kernel(const HeadFewParams p) {
                         if constexpr (H == 2) {
                             const uint32_t a2 = transpose_8x8(hi[2 * q]), a3 = transpose_8x8(hi[2 * q + 1]);
 #pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) mma_bf16_k16(acc[i][q][nt], a0, a1, a2, a3, dz[nt][0], dz[nt][H - 1]);
+                            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                for (int k = 0; k < kSplit; ++k) mma_bf16_k16(acc[i][q][nt], a0, a1, a2, a3, dz[k][nt][0], dz[k][nt][H - 1]);
                         } else {
 #pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) mma_bf16_k8(acc[i][q][nt], a0, a1, dz[nt][0]);
+                            for (int nt = 0; nt < NT; ++nt) {
+                                if constexpr (kSplit == 2) mma_bf16_k16(acc[i][q][nt], a0, a1, a0, a1, dz[0][nt][0], dz[kSplit - 1][nt][0]);
+                                else mma_bf16_k8(acc[i][q][nt], a0, a1, dz[0][nt][0]);
+                            }
                         }
                     }
                 }
@@ -412,8 +427,12 @@ head_few_backward_kernel(const HeadFewParams p) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         float e[4] = {};
-                        if constexpr (NT == 1) mma_bf16_k8(e, dzt[0][0], dzt[0][1], lo[j]);
-                        else mma_bf16_k16(e, dzt[0][0], dzt[0][1], dzt[NT - 1][0], dzt[NT - 1][1], lo[j], hi[j]);
+                        if constexpr (NT == 1) {
+                            mma_bf16_k16(e, dzt[0][0][0], dzt[0][0][1], dzt[kSplit - 1][0][0], dzt[kSplit - 1][0][1], lo[j], lo[j]);
+                        } else {
+#pragma unroll
+                            for (int k = 0; k < kSplit; ++k) mma_bf16_k16(e, dzt[k][0][0], dzt[k][0][1], dzt[k][NT - 1][0], dzt[k][NT - 1][1], lo[j], hi[j]);
+                        }
 #pragma unroll
                         for (int h = 0; h < H; ++h)
                             asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[h][j]) : "f"(e[2 * h + 1] * unit), "f"(e[2 * h] * unit));
