@@ -207,10 +207,11 @@ def test_which_rows_count(where):
     check(c)
 
 
-def test_labels_outside_the_vocabulary_are_reported():
-    c = make(100, 300, 128, seed=17, ignored=0.1)
+@pytest.mark.parametrize("T", [9, 100, 700])
+def test_labels_outside_the_vocabulary_are_reported(T):
+    c = make(T, 300, 128, seed=17, ignored=0.1)
     o, bd = reference(c)
-    bad = torch.tensor([3, 64, 99], device="cuda")
+    bad = torch.tensor([3, T // 2, T - 1], device="cuda")
     c["labels"][bad] = torch.tensor([300, 2 ** 31, 2 ** 40], device="cuda")
     f = forward(c)
     with pytest.raises(b.SbnError) as err:
@@ -218,7 +219,7 @@ def test_labels_outside_the_vocabulary_are_reported():
     assert err.value.code == 9
     b.sbn_check_status()                                            # reported once
     assert torch.isnan(f["ce"][bad]).all() and not f["lse"][bad].any()
-    rest = torch.ones(100, dtype=torch.bool, device="cuda")
+    rest = torch.ones(T, dtype=torch.bool, device="cuda")
     rest[bad] = False
     assert_near("ce", f["ce"][rest], o["ce"][rest], bd["ce"][rest])
     dx, dhead = backward(c, f["lse"])
@@ -289,8 +290,9 @@ def test_distill_masked_entries():
             assert not dx[8].any() and not dx[11].any()
 
 
-def test_distill_index_outside_the_vocabulary():
-    c = make(50, 300, 128, seed=37, top=6, ignored=0.0, absent=0.0)
+@pytest.mark.parametrize("T", [14, 50, 600])
+def test_distill_index_outside_the_vocabulary(T):
+    c = make(T, 300, 128, seed=37, top=6, ignored=0.0, absent=0.0)
     ref = dict(c, top_index=c["top_index"].clone())
     c["top_index"][7, 2] = 300
     c["top_index"][8, 0] = 2 ** 40
@@ -309,6 +311,72 @@ def test_distill_index_outside_the_vocabulary():
         b.sbn_check_status()
     assert_near("dx", dx, o["dx"], bd["dx"])
     assert_near("dhead", dhead, o["dhead"], bd["dhead"])
+
+
+@pytest.mark.parametrize("T", [5, 16, 90, 400])
+def test_a_teacher_logit_that_is_no_number_stays_in_its_row(T):
+    c = make(T, 600, 128, seed=91, top=5, ignored=0.0, absent=0.0)
+    clean, o = forward(c), None
+    bad = [1, T - 1]
+    c["top_logits"][bad[0], 2] = NAN
+    c["top_logits"][bad[1], :] = INF
+    f = forward(c)
+    b.sbn_check_status()
+    rest = torch.ones(T, dtype=torch.bool, device="cuda")
+    rest[bad] = False
+    assert torch.isnan(f["distill"][bad]).all() and torch.equal(f["distill"][rest], clean["distill"][rest])
+    assert torch.equal(f["ce"], clean["ce"]) and torch.equal(f["lse"], clean["lse"])
+    dx, _ = backward(c, f["lse"], dhead=False)
+    assert torch.isfinite(dx[rest]).all()
+
+
+@pytest.mark.parametrize("T", [3, 20, 300])
+def test_heads_past_two_to_the_31_elements(T):
+    N, K = 540001, 4096
+    g = torch.Generator(device="cuda").manual_seed(97)
+    head = torch.empty(N, K, dtype=BF16, device="cuda").normal_(0.0, 0.02, generator=g)
+    x = torch.randn(T, K, generator=g, device="cuda").to(BF16)
+    labels = torch.randint(0, N, (T,), generator=g, device="cuda")
+    labels[0], labels[1] = N - 1, -1
+    d = torch.rand(T, generator=g, device="cuda")
+    c = dict(T=T, N=N, K=K, x=x, head=head, labels=labels, d_ce=d)
+    f = forward(c, dirty=False)
+    dx, dhead = backward(c, f["lse"], dirty=False)
+    b.sbn_check_status()
+    X = torch.where((labels >= 0)[:, None], x, torch.zeros_like(x)).double()
+    Z = torch.cat([X @ head[a:a + 40000].double().T for a in range(0, N, 40000)], 1)
+    lse = torch.logsumexp(Z, 1)
+    has = labels >= 0
+    want = torch.where(has, lse - Z.gather(1, labels.clamp(min=0)[:, None])[:, 0], 0.0)
+    # one rounding or cut to 24 bits per 16 columns, of running sums below 8: 256 * 2^-23 * 8 = 2.5e-4, for lse and for the label's logit
+    assert float((f["ce"].double() - want).abs().max()) < 5e-4
+    P = torch.exp(Z - lse[:, None]) * torch.where(has, d, 0.0).double()[:, None]
+    P[torch.arange(T, device="cuda")[has], labels[has]] -= d[has].double()
+    ref = sum(P[:, a:a + 40000] @ head[a:a + 40000].double() for a in range(0, N, 40000))
+    assert float((dx.double() - ref).norm() / ref.norm()) < 2.0 ** -7 and not dx[1].any()
+    for a, e in ((0, 300), (N // 2, N // 2 + 300), (N - 300, N)):
+        r = P[:, a:e].T @ X
+        assert float((dhead[a:e].double() - r).norm() / r.norm()) < 2.0 ** -7, (a, e)
+
+
+def test_two_streams_at_once():
+    # two steps on two streams with workspaces of their own, no order between them: both right
+    cs = [make(300, 5000, 512, seed=101), make(60, 9000, 1024, seed=103, top=6), make(4, 7000, 512, seed=107)]
+    refs = [reference(c) for c in cs]
+    streams = [torch.cuda.Stream() for _ in cs]
+    torch.cuda.synchronize()
+    got = []
+    for rep in range(3):
+        for c, s in zip(cs, streams):
+            with torch.cuda.stream(s):
+                f = forward(c, dirty=False)
+                got.append((c, f, *backward(c, f["lse"], dirty=False)))
+    torch.cuda.synchronize()
+    for i, (c, f, dx, dhead) in enumerate(got):
+        o, bd = refs[i % 3]
+        assert_near("ce", f["ce"], o["ce"], bd["ce"])
+        assert_near("dx", dx, o["dx"], bd["dx"])
+        assert_near("dhead", dhead, o["dhead"], bd["dhead"])
 
 
 def test_distill_with_one_entry_is_cross_entropy():
