@@ -11,7 +11,7 @@ struct HeadPlan {
     bool words;                   // logits by head_words_tcgen05.cuh, gradients as for any number of tokens
     int tokens, groups, word_pairs;   // words: tokens per tile and groups of them, CTA pairs
     int bn, parts;                // forward: columns per tile, partial sums per row
-    int piece;                    // backward: columns of dz at a time (a multiple of 256)
+    int piece;                    // backward: columns of dz at a time (a multiple of 512)
     int bn_piece;                 // columns per tile of the pieces' logits
     bool wide_grads;              // gradients in tiles of 512 columns, else 256
     int slots, slot_stages;       // slices of dx's contraction over a piece, and 64-column stages of each
@@ -75,8 +75,9 @@ static HeadPlan head_plan(int T, int N, int K) {
         if (g_force_token_tile < 0) h.wide_grads = g_force_token_tile <= -512;
     }
     const int tile_cols = h.wide_grads ? 512 : 256;
-    const int dx_tiles = static_cast<int>(h.rows256 / 256) * ((K + tile_cols - 1) / tile_cols);
-    const int stages = (std::min(h.piece, N) + 63) / 64, slots = std::max(1, std::min((kBackwardPairs + dx_tiles / 2) / dx_tiles, stages));
+    const long long dx_tiles = h.rows256 / 256 * ((K + tile_cols - 1) / tile_cols);     // 2^34 for the largest sizes that can be asked about
+    const int stages = (std::min(h.piece, N) + 63) / 64;
+    const int slots = std::max(1, std::min(static_cast<int>((kBackwardPairs + dx_tiles / 2) / dx_tiles), stages));
     h.slot_stages = (stages + slots - 1) / slots;
     h.slots = (stages + h.slot_stages - 1) / h.slot_stages;             // all of them are written by the first piece
     return h;

@@ -20,7 +20,7 @@ namespace sbn {
 constexpr int kHeadMaxTop = 256;                  // teacher entries per token
 constexpr int kNoColumn = 0x7FFFFFFF;             // an event that is not there: behind every column
 
-// Per-row flags of a distillation (head_targets_kernel).
+// What is asked of a row, and what is wrong with it.
 constexpr int kRowDistill = 1, kRowLabel = 2, kRowBadTeacher = 4, kRowBadLabel = 8;
 
 // What a row's gradient or loss refers to.  Cross entropy: the label.  Distillation: `events` entries per row, sorted by

@@ -2,6 +2,9 @@
 the float64 oracle itself (closed forms, gradients against differences)."""
 import ctypes
 import math
+import subprocess
+import sys
+from pathlib import Path
 
 import pytest
 import torch
@@ -93,6 +96,22 @@ def test_workspace_sizes(L):
     assert b.sbn_head_workspace_bytes(T, 131072, K, top=64) < 0.15 * 4 * T * 131072
     # sizes past 32 bits are counted in 64
     assert b.sbn_head_workspace_bytes(1 << 20, 1 << 20, 4096, backward=True) > 1 << 34
+
+
+def test_workspace_sizes_at_the_largest_sizes(L):
+    # a child asks: an arithmetic fault would end the process
+    ask = """
+from paper_2603_05168_b200 import binding as b
+for T in (1, 17, 300, 1 << 20, (1 << 30) - 5, 1 << 30):
+    for N in (1, 1 << 20, 1 << 30):
+        for K in (128, 1 << 16, 1 << 20):
+            for top in (0, 256):
+                for backward in (False, True):
+                    n = b.sbn_head_workspace_bytes(T, N, K, top, backward)
+                    assert (4 * T * K if backward else 8 * T) <= n < 1 << 62, (T, N, K, top, backward, n)
+"""
+    done = subprocess.run([sys.executable, "-c", ask], cwd=Path(__file__).resolve().parent.parent, capture_output=True, text=True)
+    assert done.returncode == 0, done.stderr[-500:]
 
 
 def test_status_of_an_index_outside_the_vocabulary(L):
