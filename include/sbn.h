@@ -443,7 +443,7 @@ sbn_status sbn_tile_canonical(const int8_t *vals_plain, const uint8_t *meta_plai
  *   lse       device, fp32 [T], from the forward call with the same x, head and labels
  *   dloss     device, fp32 [T]; not read in rows left out
  *   dx_bf16   device out, bf16 [T][K], or NULL to skip;  dhead_bf16  device out, bf16 [N][K], or NULL to skip (both are
- *             overwritten, not accumulated; neither may be its input's buffer, SBN_ERR_UNSUPPORTED)
+ *             overwritten, not accumulated; neither may overlap x, head, the workspace or the other: SBN_ERR_UNSUPPORTED)
  *
  * sbn_head_distill: distillation from a teacher's `top` largest logits per token, over the whole vocabulary of the student:
  *   q_j = exp(top_logits[t][j] / tau) / sum over the entries that are there,   p_i = exp(z[t][i] / tau - lse[0][t]),
@@ -453,7 +453,7 @@ sbn_status sbn_tile_canonical(const int8_t *vals_plain, const uint8_t *meta_plai
  *               at); a row with none, or with none but logits of -infinity, is left out: loss 0, no gradient.  An index
  *               that comes twice counts twice.  An index >= N: distill_loss NaN, no gradient of it, SBN_ERR_INDEX as above
  *   top_logits  device, [T][top] of top_dtype (SBN_OUT_F32 or SBN_OUT_BF16);  top from 1 to 256, else SBN_ERR_UNSUPPORTED
- *   temperature tau, positive and finite, and so is 1 / tau (else SBN_ERR_UNSUPPORTED)
+ *   temperature tau, positive and finite, and so is 1.45 / tau (else SBN_ERR_UNSUPPORTED)
  *   labels, ce_loss  both or neither: the cross entropy of the same logits (at temperature 1) in the same pass over the
  *               head, as above; a row is left out of the products if neither loss asks for it
  *   lse         device out, fp32 [T], with labels [2][T]: lse[1] is that of temperature 1; 0 where its loss is left out

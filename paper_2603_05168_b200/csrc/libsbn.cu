@@ -1068,13 +1068,26 @@ static sbn_status head_call(HeadCall* c, bool backward, const void* x, int T, in
 static sbn_status head_distill_args(const int64_t* top_index, const void* top_logits, int top_dtype, int top, float tau) {
     if (!top_index || !top_logits) return SBN_ERR_NULL;
     if (top < 1 || top > kHeadMaxTop || (top_dtype != SBN_OUT_F32 && top_dtype != SBN_OUT_BF16)) return SBN_ERR_UNSUPPORTED;
-    if (!(tau > 0.0f) || !std::isfinite(tau) || !std::isfinite(static_cast<float>(1.4426950408889634 / static_cast<double>(tau)))) return SBN_ERR_UNSUPPORTED;
+    // 1.45: log2(e) with the factor that logits get (head_logit_scale, at most 1 + 2^-10)
+    if (!(tau > 0.0f) || !std::isfinite(tau) || !std::isfinite(static_cast<float>(1.45 / static_cast<double>(tau)))) return SBN_ERR_UNSUPPORTED;
     return SBN_OK;
 }
 static sbn_status head_gradient_args(const void* x, const void* head, const void* dx, const void* dhead) {
     if (!dx && !dhead) return SBN_ERR_NULL;
     if (dx == x || dhead == head) return SBN_ERR_UNSUPPORTED;
     if ((dx && misaligned(dx, 16)) || (dhead && misaligned(dhead, 16))) return SBN_ERR_ALIGN;
+    return SBN_OK;
+}
+// The gradients are written while the inputs are still read: nothing may lie on anything else.  Checked last.
+static sbn_status head_gradients_apart(const HeadCall& c, const void* dx, const void* dhead) {
+    const size_t rows = 2 * static_cast<size_t>(c.T) * c.K, words = 2 * static_cast<size_t>(c.N) * c.K;
+    const struct { const void* at; size_t bytes; } all[5] = {{dx, rows}, {dhead, words}, {c.x, rows}, {c.head, words}, {c.ws, sbn_head_workspace_bytes(1, c.T, c.N, c.K, c.top)}};
+    for (int i = 0; i < 2; ++i) {
+        for (int o = i + 1; o < 5; ++o) {
+            const uintptr_t a = reinterpret_cast<uintptr_t>(all[i].at), b = reinterpret_cast<uintptr_t>(all[o].at);
+            if (a && b && (a < b ? b - a < all[i].bytes : a - b < all[o].bytes)) return SBN_ERR_UNSUPPORTED;
+        }
+    }
     return SBN_OK;
 }
 
@@ -1096,6 +1109,8 @@ sbn_status sbn_head_cross_entropy_backward(const void* x_bf16, int T, int K, con
     if (st == SBN_OK) st = head_gradient_args(x_bf16, head_bf16, dx_bf16, dhead_bf16);
     if (st != SBN_OK) return st;
     if (misaligned(lse, 4) || misaligned(dloss, 4)) return SBN_ERR_ALIGN;
+    st = head_gradients_apart(c, dx_bf16, dhead_bf16);
+    if (st != SBN_OK) return st;
     return head_backward(c, lse, nullptr, dloss, nullptr, dx_bf16, dhead_bf16, static_cast<cudaStream_t>(stream));
 }
 
@@ -1122,6 +1137,8 @@ sbn_status sbn_head_distill_backward(const void* x_bf16, int T, int K, const voi
     if (st == SBN_OK) st = head_gradient_args(x_bf16, head_bf16, dx_bf16, dhead_bf16);
     if (st != SBN_OK) return st;
     if (misaligned(lse, 4) || misaligned(d_distill, 4) || (d_ce && misaligned(d_ce, 4))) return SBN_ERR_ALIGN;
+    st = head_gradients_apart(c, dx_bf16, dhead_bf16);
+    if (st != SBN_OK) return st;
     return head_backward(c, lse, labels ? lse + T : nullptr, d_distill, d_ce, dx_bf16, dhead_bf16, static_cast<cudaStream_t>(stream));
 }
 

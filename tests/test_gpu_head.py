@@ -391,8 +391,9 @@ def test_distill_with_one_entry_is_cross_entropy():
 
 
 @pytest.mark.parametrize("top", [0, 5])
-def test_either_gradient_alone(top):
-    c = make(140, 700, 256, seed=43, top=top)
+@pytest.mark.parametrize("T,N,K", [(140, 700, 256), (5, 3000, 384), (14, 2700, 1152), (400, 3000, 384), (1100, 20000, 640)])
+def test_either_gradient_alone(T, N, K, top):
+    c = make(T, N, K, seed=43, top=top)
     f = forward(c)
     dx, dhead = backward(c, f["lse"])
     only_dx, none = backward(c, f["lse"], dhead=False)
@@ -456,10 +457,11 @@ def test_calls_back_to_back_on_one_workspace():
 
 
 @pytest.mark.parametrize("top", [0, 6])
-def test_captured_into_a_graph(top):
+@pytest.mark.parametrize("T,N,K", [(200, 1500, 256), (7, 2000, 512), (900, 1500, 256), (1300, 9000, 1024)])
+def test_captured_into_a_graph(T, N, K, top):
     # a whole step in a graph, replayed on other inputs (other rows left out) in the same buffers
-    c = make(200, 1500, 256, seed=61, top=top)
-    ws = [b.alloc_head_ws(200, 1500, 256, top=top, backward=w) for w in (False, True)]
+    c = make(T, N, K, seed=61, top=top)
+    ws = [b.alloc_head_ws(T, N, K, top=top, backward=w) for w in (False, True)]
     f = forward(c, ws=ws[0])
     backward(c, f["lse"], ws=ws[1])
     g = torch.cuda.CUDAGraph()
@@ -467,7 +469,7 @@ def test_captured_into_a_graph(top):
         f = forward(c, ws=ws[0])
         dx, dhead = backward(c, f["lse"], ws=ws[1])
     for seed in (67, 71):
-        new = make(200, 1500, 256, seed=seed, top=top, ignored=0.6 if seed == 67 else 0.0)
+        new = make(T, N, K, seed=seed, top=top, ignored=0.6 if seed == 67 else 0.0)
         for k, v in new.items():
             if torch.is_tensor(v):
                 c[k].copy_(v)

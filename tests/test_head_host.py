@@ -81,6 +81,27 @@ def test_refusals_of_each_call(L):
     assert _kd(L, kd=odd) == ALIGN and _kd(L, ce=odd) == ALIGN and _kdb(L, dkd=odd) == ALIGN and _kdb(L, dce=odd) == ALIGN
 
 
+@pytest.mark.parametrize("call", [_ceb, _kdb])
+def test_gradients_that_overlap_are_refused(L, call):
+    # T x K and N x K values of 2 bytes: 2 KB and 500 KB
+    x, head, ws, dx, dhead = 0x1000000, 0x2000000, 0x3000000, 0x4000000, 0x5000000
+    at = ctypes.c_void_p
+
+    def run(**k):
+        return call(L, **{"x": at(x), "head": at(head), "ws": at(ws), "dx": at(dx), "dhead": at(dhead), **k})
+
+    for where in (x, x + 16, x + 2048 - 16, x - 2048 + 16, head + 16, head - 16, head + 512000 - 16, ws, ws - 16, dhead, dhead - 16, dhead + 511984):
+        assert run(dx=at(where)) == UNSUP, hex(where)
+    for where in (head, head - 512000 + 16, x, x - 16, x + 2032, ws + 256, dx, dx + 2032, dx - 511984):
+        assert run(dhead=at(where)) == UNSUP, hex(where)
+    assert run(dx=None, dhead=at(head + 16)) == UNSUP and run(dx=at(x + 16), dhead=None) == UNSUP
+
+
+def test_smallest_temperature(L):
+    for tau in (4.2e-39, 4.24e-39, 1e-45):                          # 1.45 / tau is no fp32 number
+        assert _kd(L, tau=tau) == UNSUP and _kdb(L, tau=tau) == UNSUP
+
+
 def test_workspace_sizes(L):
     from paper_2603_05168_b200 import binding as b
     for bad in ((0, 10, 128), (1, 0, 128), (1, 10, 100), (-1, 10, 128)):
