@@ -33,6 +33,7 @@
  *   - Inputs must be finite.  NaN/Inf give unspecified results.
  *   - Shape limits of the GPU path: N % 128 == 0, K % 128 == 0, T >= 1, K <= 2^20, pointers
  *     16-byte aligned (cudaMalloc alignment is always enough).
+ *     The calls at the output head (sbn_head_*) have rules of their own, given there.
  *
  * Compressed 2:4 layout (the paper leaves the layout to the kernel; this is the library's):
  *   groups are 4 consecutive columns of a row, aligned to column 0; group g of row n keeps the
