@@ -485,8 +485,9 @@ sbn_status sbn_head_distill_backward(const void *x_bf16, int T, int K, const voi
                                      void *dhead_bf16, void *ws, size_t ws_bytes, void *stream);
 
 /* Synchronises `stream`, returns SBN_ERR_TIMEOUT if any kernel since the last call gave up on a
- * bounded wait, SBN_ERR_INDEX if one met a label or a teacher's index outside the vocabulary (and
- * clears that record), SBN_ERR_CUDA if the stream reports an error, else SBN_OK. */
+ * bounded wait, otherwise SBN_ERR_INDEX if one met a label or a teacher's index outside the
+ * vocabulary (and clears the record: of both, the timeout is the one that is told), SBN_ERR_CUDA if
+ * the stream reports an error, else SBN_OK. */
 sbn_status sbn_check_status(void *stream);
 
 /* Static string for a status code. */

@@ -40,8 +40,9 @@ __device__ __forceinline__ int head_token_flags(const HeadTargets& tg, int t, in
     const long long y = tg.labels[t];
     return y < 0 ? 0 : (y < N ? kRowLabel : kRowBadLabel);
 }
+// Only where nothing is recorded: a wait that ran out is the graver fault (whole results, not a row) and overwrites this one.
 __device__ __forceinline__ void report_bad(int flags) {
-    if (flags & (kRowBadTeacher | kRowBadLabel)) atomicExch(&g_device_status, static_cast<int>(SBN_ERR_INDEX));
+    if (flags & (kRowBadTeacher | kRowBadLabel)) atomicCAS(&g_device_status, 0, static_cast<int>(SBN_ERR_INDEX));
 }
 // A token left out: the outputs of a forward call (any pointer may be null; distillation 0, label 1), and what is wrong with it.
 __device__ __forceinline__ void write_left_out(float* loss0, float* loss1, float* lse0, float* lse1, int t, int flags) {

@@ -15,7 +15,8 @@ constexpr int kNumSMs = 148;          // B200: 2 dies x 74 SMs
 constexpr float kEps = 1e-5f;         // Algorithm 2's clamp for both scales
 
 // Device status word: 0 = fine, otherwise an sbn_status written by a kernel whose bounded wait
-// ran out.  Read and cleared by sbn_check_status.
+// ran out, or (only if nothing is recorded yet) that met an index out of range.  Read and cleared by
+// sbn_check_status.
 __device__ int g_device_status = 0;
 
 // Limit of every bounded device-side wait, in ns (default 2 s).  Only the slow path of a wait reads it

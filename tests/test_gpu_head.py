@@ -587,3 +587,30 @@ def test_binding_refuses_wrong_tensors(change):
     with pytest.raises(ValueError):
         b.sbn_head_cross_entropy(x, head, labels, loss, lse, ws=ws)
     assert b.sbn_launch_count() == n
+
+
+@pytest.mark.parametrize("top", [0, 4])
+@pytest.mark.parametrize("T", [9, 100, 700])
+def test_a_bad_index_does_not_hide_a_timeout(T, top):
+    # a wait that ran out leaves results that are no results: that is what the status has to say, whichever came first
+    broken, bad = make(300, 700, 256, seed=113), make(T, 300, 128, seed=109, top=top, ignored=0.0, absent=0.0)
+    bad["top_index" if top else "labels"][T // 2] = 300
+
+    def time_out():
+        try:
+            b.sbn_set_wait_test(True, 1000)
+            forward(broken)
+        finally:
+            b.sbn_set_wait_test(False, 0)
+
+    for order in ((time_out, lambda: forward(bad)), (lambda: forward(bad), time_out)):
+        for call in order:
+            call()
+        with pytest.raises(b.SbnError) as err:
+            b.sbn_check_status()
+        assert err.value.code == 7
+        b.sbn_check_status()
+    forward(bad)
+    with pytest.raises(b.SbnError) as err:
+        b.sbn_check_status()
+    assert err.value.code == 9
