@@ -328,8 +328,9 @@ head_losses_kernel(const HeadLossJob j) {
                 w[q] = in && j.part1 != nullptr ? j.part1[p0 + i + q * kLossThreads] : 0.0f;
             }
             const float top = fmaxf(fmaxf(fmaxf(v[0].x, v[1].x), fmaxf(v[2].x, v[3].x)), m);
-            if (top == -INFINITY) {                           // nothing yet; a sum that is no number stays one
+            if (top == -INFINITY) {                           // nothing yet; sums that are no numbers stay so
                 s0 += (v[0].y + v[1].y) + (v[2].y + v[3].y);
+                s1 += (w[0] + w[1]) + (w[2] + w[3]);
                 continue;
             }
             s0 *= expf((m - top) * tau_f);
@@ -372,8 +373,9 @@ head_losses_kernel(const HeadLossJob j) {
         float top = s_f[0][0];
 #pragma unroll
         for (int w = 1; w < kWarps; ++w) top = fmaxf(top, s_f[0][w]);
-        const float down = m == -INFINITY ? 1.0f : expf((m - top) * tau_f);      // no part: s0 is 0 or no number
-        double sums[6] = {static_cast<double>(s0) * static_cast<double>(down), m == -INFINITY ? 0.0 : static_cast<double>(s1) * static_cast<double>(expf((m - top) * one_f)), q_sum, kd,
+        // no part: s0 and s1 are 0 or no numbers
+        const float down0 = m == -INFINITY ? 1.0f : expf((m - top) * tau_f), down1 = m == -INFINITY ? 1.0f : expf((m - top) * one_f);
+        double sums[6] = {static_cast<double>(s0) * static_cast<double>(down0), static_cast<double>(s1) * static_cast<double>(down1), q_sum, kd,
                           static_cast<double>(dot_top), static_cast<double>(q_top)};
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) {

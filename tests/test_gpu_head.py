@@ -614,3 +614,22 @@ def test_a_bad_index_does_not_hide_a_timeout(T, top):
     with pytest.raises(b.SbnError) as err:
         b.sbn_check_status()
     assert err.value.code == 9
+
+
+@pytest.mark.parametrize("T", [6, 16, 90, 400])
+def test_nan_shows_in_both_losses(T):
+    # a token that is no number, and words that are none: a whole share of the partial sums then has no maximum
+    N, K = 3000, 256
+    c = make(T, N, K, seed=127, top=5, ignored=0.0, absent=0.0)
+    clean = forward(c)
+    c["x"][3] = NAN
+    f = forward(c)
+    rest = torch.ones(T, dtype=torch.bool, device="cuda")
+    rest[3] = False
+    for name in ("distill", "ce", "lse_distill", "lse_ce"):
+        assert torch.isnan(f[name][3]) and torch.equal(f[name][rest], clean[name][rest]), name
+    c = make(T, N, K, seed=127, top=5, ignored=0.0, absent=0.0)
+    c["head"][512:1024] = NAN
+    f = forward(c)
+    for name in ("distill", "ce", "lse_distill", "lse_ce"):
+        assert torch.isnan(f[name]).all(), name
