@@ -164,6 +164,7 @@ head_few_forward_kernel(const HeadFewParams p) {
     // the word and token of this thread in every block
     const int tok = tid % kTok, slot = tid / kTok;
     const bool asked = slot < 16 && tok < p.T && (s_tg.flags[tok] & (kRowDistill | kRowLabel));
+    const int label = !LIST && asked ? static_cast<int>(p.tg.labels[tok]) : -1;
     float m = -INFINITY, s0 = 0.0f, s1 = 0.0f;
     FewCursor<NT, LIST> cursor(p, s_tg, tok, asked);
 
@@ -193,6 +194,7 @@ head_few_forward_kernel(const HeadFewParams p) {
             s0 = s0 * ex2_approx((m - m_new) * p.c0) + ex2_approx((z - m_new) * p.c0);
             if (DUAL) s1 = s1 * ex2_approx((m - m_new) * p.c1) + ex2_approx((z - m_new) * p.c1);
             m = m_new;
+            if (!LIST && n == label) p.z_ev[tok] = z;
             cursor.template visit<16>(p, s_tg, tok, nb * 16, n, [&](int e) { p.z_ev[static_cast<size_t>(tok) * p.tg.events + e] = z; });
         }
         __syncthreads();

@@ -81,7 +81,7 @@ struct HeadLogitsParams {
     // stats
     float2* part;                 // [rows][parts]
     float* part1;                 // [rows][parts], sums at temperature 1 (with labels)
-    float* z_ev;                  // [rows][events]
+    float* z_ev;                  // [rows][events]: logits at the targets
     int parts;
     // grad
     const float *lse0, *lse1;     // per token
@@ -128,12 +128,10 @@ struct HeadRow {
         }
     }
     __device__ const int* list(const HeadLogitsParams& p) const { return p.tg.ev_col + static_cast<size_t>(t) * p.tg.events; }
-    // To the first target at or behind column n.  Of the logits themselves only the teacher's entries are wanted (stats): the
-    // label's logit is a product of its own (head_losses_kernel).
-    static constexpr bool kTargets = LIST || MODE == 1;
+    // To the first target at or behind column n.
     __device__ void seek(const HeadLogitsParams& p, int n) {
         next_col = kNoColumn;
-        if (!kTargets || !here) return;
+        if (!here) return;
         if constexpr (LIST) {
             const int* col = list(p);
             int lo = 0, hi = p.tg.events;
@@ -159,18 +157,17 @@ struct HeadRow {
 
     // Writes down the row's logits at its targets among columns n .. n + 31; at(q) gives every lane of the warp its logit of column
     // n + q.  The whole warp takes part (picking a register by an index of the lane's own would put all 32 into local memory:
-    // 1 us per 32 columns).  A row has a handful of targets in the whole vocabulary.
+    // 1 us per 32 columns).  A row has a handful of targets in the whole vocabulary, the label's among them: head_losses_kernel
+    // takes its term out of the sum.
     template <class At>
     __device__ void note_targets(const HeadLogitsParams& p, int n, At&& at) {
-        if constexpr (LIST) {
-            while (next_col < n) step(p);
-            for (uint32_t who; (who = __ballot_sync(0xFFFFFFFFu, next_col < n + 32)) != 0u;) {
-                const int q = __shfl_sync(0xFFFFFFFFu, next_col - n, __ffs(who) - 1);
-                const float v = at(q);
-                if (next_col - n == q) {
-                    p.z_ev[static_cast<size_t>(r) * p.tg.events + e] = v;
-                    step(p);
-                }
+        while (next_col < n) step(p);
+        for (uint32_t who; (who = __ballot_sync(0xFFFFFFFFu, next_col < n + 32)) != 0u;) {
+            const int q = __shfl_sync(0xFFFFFFFFu, next_col - n, __ffs(who) - 1);
+            const float v = at(q);
+            if (next_col - n == q) {
+                p.z_ev[static_cast<size_t>(r) * p.tg.events + e] = v;
+                step(p);
             }
         }
     }

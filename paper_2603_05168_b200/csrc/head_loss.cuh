@@ -106,7 +106,7 @@ static HeadWs head_ws_layout(const HeadPlan& h, bool backward, int T, int K, int
     }
     if (!h.few && !(h.words && !backward)) w.xc = take(2 * static_cast<size_t>(h.rows64) * K);
     if (!backward) {
-        if (top) w.z_ev = take(4 * t * events);
+        w.z_ev = take(4 * t * events);
         w.part = take(8 * t * h.parts);
         if (top) w.part1 = take(4 * t * h.parts);
     } else {

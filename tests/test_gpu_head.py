@@ -633,3 +633,44 @@ def test_nan_shows_in_both_losses(T):
     f = forward(c)
     for name in ("distill", "ce", "lse_distill", "lse_ce"):
         assert torch.isnan(f[name]).all(), name
+
+
+def sure(T, N, K, seed, label_logit, top=0):
+    """Tokens that know their label: its logit is near `label_logit`, the others are N(0, 1).  The teacher is as sure."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    randn = lambda *s: torch.randn(*s, generator=g, device="cuda")
+    head = (randn(N, K) * 0.02).to(BF16)
+    y = torch.randint(0, N, (T,), generator=g, device="cuda")
+    rows = head[y].float()
+    x = (randn(T, K) + label_logit * rows / (rows * rows).sum(1, keepdim=True)).to(BF16)
+    c = dict(T=T, N=N, K=K, x=x, head=head, tau=1.0, labels=y, d_ce=torch.full((T,), 1.0 / T, device="cuda"))
+    if top:
+        index = (y[:, None] + torch.arange(top, device="cuda") * (N // top)) % N        # the label's entry is the first
+        c["top_index"], c["top_logits"] = index, torch.where(torch.arange(top, device="cuda") == 0, label_logit, 0.0) + randn(T, top)
+        c["d_distill"] = c["d_ce"]
+    return c
+
+
+@pytest.mark.parametrize("top", [0, 5])
+@pytest.mark.parametrize("label_logit", [20.0, 30.0, 40.0])
+@pytest.mark.parametrize("T,K", [(4, 2560), (16, 2560), (8, 4096), (40, 2560), (200, 4096), (300, 2560), (1100, 4096)])
+def test_losses_of_sure_tokens(T, K, label_logit, top):
+    """A sure token's loss is what the other words add to a sum of 1: with S = 1 + rest in fp32, each of at most 64 additions a thread's
+    and a row's sums go through once the label is in (40 for its 4 chunks of 32 words, 16 + 8 to put them together) is rounded by at
+    most 2^-24 of something below 2, so rest is off by 64 * 2^-23 = 7.7e-6 at worst.  Beside that only what the logits
+    themselves are off by, relative to the loss.  A cross entropy is never below 0; a divergence not by more than its q are rounded
+    (2^-24 per entry and one for log q)."""
+    c = sure(T, 5000, K, 131 + T, label_logit, top)
+    o, bd = reference(c)
+    bz = K * 2.0 ** -23 * (o["X"].abs() @ o["W"].abs().T).max(1).values            # as in oracle/head.py
+    f = forward(c)
+    b.sbn_check_status()
+    # exp(2 bz) - 1 of the loss, and ex2's and its argument's error of every term (2^-16)
+    tol = o["ce"] * (torch.expm1(2 * bz) + 2.0 ** -16) + 64 * 2.0 ** -23
+    assert float(f["ce"].min()) >= 0.0, float(f["ce"].min())
+    assert_near("ce", f["ce"], o["ce"], tol)
+    if top:
+        kd = o["distill"].abs() + (o["Q"] * (o["Z"] - o["Z"].max(1, keepdim=True).values).abs()).sum(1)
+        tol = kd * (torch.expm1(2 * bz) + 2.0 ** -16) + 64 * 2.0 ** -23 + (top + 2) * 2.0 ** -24
+        assert float(f["distill"].min()) >= -(top + 2) * 2.0 ** -24, float(f["distill"].min())
+        assert_near("distill", f["distill"], o["distill"], tol)
