@@ -299,10 +299,13 @@ __device__ __forceinline__ float head_logit_share(const HeadLossJob& j, int t, l
 // units of exp of the largest, with the word's as the products had it (`was`, relative to the largest); ahead: the largest less the exact logit.
 // The rest of the sum is at least 0 (a sum that holds the largest term is never rounded below it), and so is the result: with lse
 // and the logit from different sums, a sure token's loss was what their errors differed by, 4e-5 at 4096 columns and of either sign.
-__device__ __forceinline__ double surprise(double sum, double was, double ahead) {
-    double rest = sum - exp(was);
+// (expf: 1 exactly for the largest term, and where another one is the largest its error is beside a rest of at least 1.)
+__device__ __forceinline__ double surprise(double sum, float was, double ahead) {
+    double rest = sum - static_cast<double>(expf(was));
     rest = rest < 0.0 ? 0.0 : rest;                           // (a NaN stays)
-    return ahead < 700.0 ? log1p(rest * exp(ahead)) : ahead + log(rest);
+    if (ahead > 700.0) return ahead + log(rest);
+    const double y = rest * exp(ahead);
+    return y < 0x1p-10 ? y * (1.0 + y * (-1.0 / 2 + y * (1.0 / 3 - y * (1.0 / 4)))) : log(1.0 + y);      // log1p: off by less than 2^-42 of itself
 }
 
 // A CTA per row, everything it reads under way at once: a call with few rows waits for latencies only.  Sums in double: a loss
@@ -405,35 +408,41 @@ head_losses_kernel(const HeadLossJob j) {
             for (int k = 0; k < 6; ++k) s_d[k][warp] = sums[k];
         }
         __syncthreads();
-        if (tid == 0) {
+        // a warp per output: logarithms in double take their time one after another
+        if (lane == 0) {
+            dot = s_f[1][0];
+#pragma unroll
+            for (int k = 0; k < 6; ++k) sums[k] = s_d[k][0];
 #pragma unroll
             for (int w = 1; w < kWarps; ++w) {
                 dot += s_f[1][w];
 #pragma unroll
                 for (int k = 0; k < 6; ++k) sums[k] += s_d[k][w];
             }
-            const double m_z = static_cast<double>(top) * j.z_scale, lse0 = m_z * j.inv_tau + log(sums[0]);
-            if (j.tg.flags == nullptr) {                      // cross entropy
-                j.lse0[t] = static_cast<float>(lse0);
-                j.loss1[t] = static_cast<float>(surprise(sums[0], (static_cast<double>(s_was[1]) - top) * j.z_scale, m_z - dot));
-            } else {
-                const float bad = __uint_as_float(0x7FC00000u);
-                float loss0 = (flags & kRowBadTeacher) ? bad : 0.0f;
-                if (flags & kRowDistill) {
-                    // sum of q (log q - log p) with log p_j = (z_j - z_top) / tau - the heaviest's surprise
-                    const double z_top = sums[4] * j.inv_tau;
-                    loss0 = static_cast<float>(sums[3] + (sums[2] - sums[5]) * z_top +
-                                               sums[2] * surprise(sums[0], (static_cast<double>(s_was[0]) - top) * j.z_scale * j.inv_tau, m_z * j.inv_tau - z_top));
-                }
-                j.loss0[t] = loss0;
-                j.lse0[t] = (flags & kRowDistill) ? static_cast<float>(lse0) : 0.0f;
+            const double m_z = static_cast<double>(top) * j.z_scale;
+            const bool label_alone = j.tg.flags == nullptr;   // cross entropy: its sum is the first
+            const float bad = __uint_as_float(0x7FC00000u);
+            if (warp == 0) {
+                j.lse0[t] = label_alone || (flags & kRowDistill) ? static_cast<float>(m_z * j.inv_tau + log(sums[0])) : 0.0f;
+            } else if (warp == 1) {
                 if (j.loss1 != nullptr) {
-                    const double lse1 = m_z + log(sums[1]);
                     float loss1 = (flags & kRowBadLabel) ? bad : 0.0f;
-                    if (flags & kRowLabel) loss1 = static_cast<float>(surprise(sums[1], (static_cast<double>(s_was[1]) - top) * j.z_scale, m_z - dot));
+                    if (flags & kRowLabel) loss1 = static_cast<float>(surprise(label_alone ? sums[0] : sums[1], (s_was[1] - top) * one_f, m_z - dot));
                     j.loss1[t] = loss1;
-                    j.lse1[t] = (flags & kRowLabel) ? static_cast<float>(lse1) : 0.0f;
                 }
+            } else if (warp == 2) {
+                if (!label_alone) {
+                    float loss0 = (flags & kRowBadTeacher) ? bad : 0.0f;
+                    if (flags & kRowDistill) {
+                        // sum of q (log q - log p) with log p_j = (z_j - z_top) / tau - the heaviest's surprise
+                        const double z_top = sums[4] * j.inv_tau;
+                        loss0 = static_cast<float>(sums[3] + (sums[2] - sums[5]) * z_top +
+                                                   sums[2] * surprise(sums[0], (s_was[0] - top) * tau_f, m_z * j.inv_tau - z_top));
+                    }
+                    j.loss0[t] = loss0;
+                }
+            } else if (j.lse1 != nullptr) {
+                j.lse1[t] = (flags & kRowLabel) ? static_cast<float>(m_z + log(sums[1])) : 0.0f;
             }
         }
         __syncthreads();

@@ -18,7 +18,7 @@ namespace sbn {
 constexpr int kWordsTokens = 256;
 constexpr int kWordsSquare = 32 * 33;                                      // floats
 constexpr int kWordsTurnBytes = 8 * kWordsSquare * 4;
-constexpr int kWordsStateBytes = 8 * 3 * kWordsTokens * 4;                 // stats: [warp][m, s0, s1][token]; grad: the warps' boxes
+constexpr int kWordsStateBytes = 8 * 3 * kWordsTokens * 4;                 // stats: [warp][m, s0, s1 or label][token]; grad: the warps' boxes
 static_assert(kWordsTurnBytes % 1024 == 0 && kWordsStateBytes >= 8 * kWarpBoxBytes, "alignment and room of the boxes");
 
 // What a CTA has per stage: 128 words, half the tokens.
@@ -83,7 +83,7 @@ struct HeadWordsWork {
         const HeadWordsWork& w;
         int rank, quarter, sub, lane;
         float* square;
-        float* state;                                                       // stats: [m, s0, s1][token]
+        float* state;                                                       // stats: [m, s0, s1][token]; cross entropy has labels for s1
         uint32_t box;                                                       // grad
         float inv_scale;
         HeadRow<MODE, LIST, DUAL> row;
@@ -101,6 +101,10 @@ struct HeadWordsWork {
                 for (int t = lane; t < kWordsTokens; t += 32) {
                     state[t] = -INFINITY;
                     state[kWordsTokens + t] = state[2 * kWordsTokens + t] = 0.0f;
+                    if constexpr (!LIST) {                                  // read here, where it waits for nothing
+                        const bool there = t < p.T && (head_token_flags(p.tg, t, p.N) & kRowLabel);
+                        state[2 * kWordsTokens + t] = __int_as_float(there ? static_cast<int>(p.tg.labels[t]) : kNoColumn);
+                    }
                 }
             } else {
                 float largest = 0.0f;                                       // every warp for itself
@@ -140,9 +144,15 @@ struct HeadWordsWork {
 #pragma unroll 1
             for (int c = sub; c < all; c += 2) {
                 const int t = tile.t0 + c * 32 + lane;
-                const bool here = t < p.T && (head_token_flags(p.tg, t, p.N) & (kRowDistill | kRowLabel));
-                row.begin(p, t, here ? t : 0, here, inv_scale);
-                row.seek(p, n0);
+                if constexpr (MODE == 0 && !LIST) {
+                    const int label = __float_as_int(state[2 * kWordsTokens + t]);
+                    row.begin(p, t, t, label != kNoColumn);
+                    row.next_col = label >= n0 ? label : kNoColumn;
+                } else {
+                    const bool here = t < p.T && (head_token_flags(p.tg, t, p.N) & (kRowDistill | kRowLabel));
+                    row.begin(p, t, here ? t : 0, here, inv_scale);
+                    row.seek(p, n0);
+                }
                 uint32_t z[32];
                 __syncwarp();
                 // (behind the tile's tokens, but for less than 256 columns: whatever tensor memory holds, for nobody)
@@ -161,7 +171,11 @@ struct HeadWordsWork {
                         row.s0 = state[kWordsTokens + t];
                         if (DUAL) row.s1 = state[2 * kWordsTokens + t];
                     }
-                    row.note_targets(p, n0, [&](int q) { return square[lane * 33 + q]; });
+                    while (row.next_col < n0 + 32) {                        // a thread's token has its logits next to one another
+                        p.z_ev[static_cast<size_t>(t) * p.tg.events + row.e] = square[lane * 33 + row.next_col - n0];
+                        row.step(p);
+                    }
+                    __syncwarp();
                     row.stats(p, z, n0);
                     __syncwarp();
                     if (keep) {
