@@ -444,7 +444,7 @@ sbn_status sbn_tile_canonical(const int8_t *vals_plain, const uint8_t *meta_plai
  *   lse       device, fp32 [T], from the forward call with the same x, head and labels
  *   dloss     device, fp32 [T]; not read in rows left out
  *   dx_bf16   device out, bf16 [T][K], or NULL to skip;  dhead_bf16  device out, bf16 [N][K], or NULL to skip (both are
- *             overwritten, not accumulated; neither may overlap x, head, the workspace or the other: SBN_ERR_UNSUPPORTED)
+ *             overwritten, not accumulated)
  *
  * sbn_head_distill: distillation from a teacher's `top` largest logits per token, over the whole vocabulary of the student:
  *   q_j = exp(top_logits[t][j] / tau) / sum over the entries that are there,   p_i = exp(z[t][i] / tau - lse[0][t]),
@@ -464,6 +464,8 @@ sbn_status sbn_tile_canonical(const int8_t *vals_plain, const uint8_t *meta_plai
  *
  *   ws          device workspace of sbn_head_workspace_bytes(backward, T, N, K, top) bytes, 256-byte aligned, top = 0 for
  *               the cross entropy; contents need no initialisation; not to be shared by calls that may run concurrently
+ *   No output of the four calls may overlap an input, the workspace or another output, and the workspace no input
+ *   (SBN_ERR_UNSUPPORTED).
  * Results are the same, bit for bit, from call to call.  All four calls only enqueue; they may be captured into a graph.
  */
 size_t sbn_head_workspace_bytes(int backward, int T, int N, int K, int top);   /* 0 for sizes that the calls refuse */

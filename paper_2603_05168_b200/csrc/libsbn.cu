@@ -7,6 +7,7 @@
 #include <algorithm>
 #include <atomic>
 #include <cmath>
+#include <initializer_list>
 #include <mutex>
 #include <vector>
 
@@ -1078,14 +1079,27 @@ static sbn_status head_gradient_args(const void* x, const void* head, const void
     if ((dx && misaligned(dx, 16)) || (dhead && misaligned(dhead, 16))) return SBN_ERR_ALIGN;
     return SBN_OK;
 }
-// The gradients are written while the inputs are still read: nothing may lie on anything else.  Checked last.
-static sbn_status head_gradients_apart(const HeadCall& c, const void* dx, const void* dhead) {
-    const size_t rows = 2 * static_cast<size_t>(c.T) * c.K, words = 2 * static_cast<size_t>(c.N) * c.K;
-    const struct { const void* at; size_t bytes; } all[5] = {{dx, rows}, {dhead, words}, {c.x, rows}, {c.head, words}, {c.ws, sbn_head_workspace_bytes(1, c.T, c.N, c.K, c.top)}};
-    for (int i = 0; i < 2; ++i) {
-        for (int o = i + 1; o < 5; ++o) {
+// Outputs are written while inputs are still read, and the backward calls write all along: no output may lie on an input, the workspace
+// or another output, and the workspace on no input.  Checked last.
+struct HeadSpan { const void* at; size_t bytes; };
+static sbn_status head_apart(const HeadCall& c, bool backward, std::initializer_list<HeadSpan> outputs, std::initializer_list<HeadSpan> inputs) {
+    const size_t t = static_cast<size_t>(c.T), k = static_cast<size_t>(c.K);
+    HeadSpan all[12] = {};
+    int n = 0;
+    auto add = [&](const HeadSpan& s) { if (s.at) all[n++] = s; };
+    for (const HeadSpan& s : outputs) add(s);
+    add({c.ws, sbn_head_workspace_bytes(backward, c.T, c.N, c.K, c.top)});
+    const int written = n;
+    add({c.x, 2 * t * k});
+    add({c.head, 2 * static_cast<size_t>(c.N) * k});
+    add({c.labels, 8 * t});
+    add({c.top_index, 8 * t * c.top});
+    add({c.top_logits, (c.top_bf16 ? 2 : 4) * t * c.top});
+    for (const HeadSpan& s : inputs) add(s);
+    for (int i = 0; i < written; ++i) {
+        for (int o = i + 1; o < n; ++o) {
             const uintptr_t a = reinterpret_cast<uintptr_t>(all[i].at), b = reinterpret_cast<uintptr_t>(all[o].at);
-            if (a && b && (a < b ? b - a < all[i].bytes : a - b < all[o].bytes)) return SBN_ERR_UNSUPPORTED;
+            if (a < b ? b - a < all[i].bytes : a - b < all[o].bytes) return SBN_ERR_UNSUPPORTED;
         }
     }
     return SBN_OK;
@@ -1095,9 +1109,12 @@ sbn_status sbn_head_cross_entropy(const void* x_bf16, int T, int K, const void* 
                                   void* ws, size_t ws_bytes, void* stream) {
     if (!labels || !loss || !lse) return SBN_ERR_NULL;
     HeadCall c;
-    const sbn_status st = head_call(&c, false, x_bf16, T, K, head_bf16, N, labels, nullptr, nullptr, SBN_OUT_F32, 0, 1.0f, ws, ws_bytes);
+    sbn_status st = head_call(&c, false, x_bf16, T, K, head_bf16, N, labels, nullptr, nullptr, SBN_OUT_F32, 0, 1.0f, ws, ws_bytes);
     if (st != SBN_OK) return st;
     if (misaligned(loss, 4) || misaligned(lse, 4)) return SBN_ERR_ALIGN;
+    const size_t row = 4 * static_cast<size_t>(T);
+    st = head_apart(c, false, {{loss, row}, {lse, row}}, {});
+    if (st != SBN_OK) return st;
     return head_forward(c, nullptr, loss, lse, nullptr, static_cast<cudaStream_t>(stream));
 }
 
@@ -1109,7 +1126,8 @@ sbn_status sbn_head_cross_entropy_backward(const void* x_bf16, int T, int K, con
     if (st == SBN_OK) st = head_gradient_args(x_bf16, head_bf16, dx_bf16, dhead_bf16);
     if (st != SBN_OK) return st;
     if (misaligned(lse, 4) || misaligned(dloss, 4)) return SBN_ERR_ALIGN;
-    st = head_gradients_apart(c, dx_bf16, dhead_bf16);
+    const size_t row = 4 * static_cast<size_t>(T);
+    st = head_apart(c, true, {{dx_bf16, 2 * static_cast<size_t>(T) * K}, {dhead_bf16, 2 * static_cast<size_t>(N) * K}}, {{lse, row}, {dloss, row}});
     if (st != SBN_OK) return st;
     return head_backward(c, lse, nullptr, dloss, nullptr, dx_bf16, dhead_bf16, static_cast<cudaStream_t>(stream));
 }
@@ -1123,6 +1141,9 @@ sbn_status sbn_head_distill(const void* x_bf16, int T, int K, const void* head_b
     if (st == SBN_OK) st = head_call(&c, false, x_bf16, T, K, head_bf16, N, labels, top_index, top_logits, top_dtype, top, temperature, ws, ws_bytes);
     if (st != SBN_OK) return st;
     if (misaligned(distill_loss, 4) || misaligned(lse, 4) || (ce_loss && misaligned(ce_loss, 4))) return SBN_ERR_ALIGN;
+    const size_t row = 4 * static_cast<size_t>(T);
+    st = head_apart(c, false, {{distill_loss, row}, {ce_loss, row}, {lse, labels ? 2 * row : row}}, {});
+    if (st != SBN_OK) return st;
     return head_forward(c, distill_loss, ce_loss, lse, labels ? lse + T : nullptr, static_cast<cudaStream_t>(stream));
 }
 
@@ -1137,7 +1158,9 @@ sbn_status sbn_head_distill_backward(const void* x_bf16, int T, int K, const voi
     if (st == SBN_OK) st = head_gradient_args(x_bf16, head_bf16, dx_bf16, dhead_bf16);
     if (st != SBN_OK) return st;
     if (misaligned(lse, 4) || misaligned(d_distill, 4) || (d_ce && misaligned(d_ce, 4))) return SBN_ERR_ALIGN;
-    st = head_gradients_apart(c, dx_bf16, dhead_bf16);
+    const size_t row = 4 * static_cast<size_t>(T);
+    st = head_apart(c, true, {{dx_bf16, 2 * static_cast<size_t>(T) * K}, {dhead_bf16, 2 * static_cast<size_t>(N) * K}},
+                    {{lse, labels ? 2 * row : row}, {d_distill, row}, {d_ce, row}});
     if (st != SBN_OK) return st;
     return head_backward(c, lse, labels ? lse + T : nullptr, d_distill, d_ce, dx_bf16, dhead_bf16, static_cast<cudaStream_t>(stream));
 }

@@ -197,3 +197,28 @@ def test_oracle_gradients_against_differences():
             step[at] = h
             slope = (total(**{name: c[name] + step}) - total(**{name: c[name] - step})) / (2 * h)
             assert abs(slope - float(grad[at])) < 1e-8, (name, at)
+
+
+@pytest.mark.parametrize("call", [_ce, _ceb, _kd, _kdb])
+def test_nothing_written_may_lie_on_anything_else(L, call):
+    # T x K and N x K values of 2 bytes: 2 KB and 500 KB; per token 4 bytes (lse twice beside a teacher) or 8; 4 tokens x 8 entries
+    distill, back = call in (_kd, _kdb), call in (_ceb, _kdb)
+    size = dict(x=2048, head=512000, labels=32, lse=32 if distill else 16, ws=L.sbn_head_workspace_bytes(int(back), 4, 1000, 256, 8 if distill else 0))
+    if distill:
+        size.update(index=256, logits=128)
+    reads = {_ceb: ["lse", "dloss"], _kdb: ["lse", "dkd", "dce"]}.get(call, [])
+    writes = {_ce: ["loss", "lse"], _kd: ["kd", "ce", "lse"]}.get(call, ["dx", "dhead"])
+    for name in reads + writes:
+        size.setdefault(name, dict(dx=2048, dhead=512000).get(name, 16))
+    at = {name: (i + 1) << 28 for i, name in enumerate(size)}
+    inputs = [name for name in size if name not in writes and name != "ws"]
+
+    def run(**k):
+        return call(L, **{name: ctypes.c_void_p(k.get(name, where)) for name, where in at.items()})
+
+    pairs = [(w, o) for w in writes for o in size if o != w] + [("ws", o) for o in inputs]
+    for w, o in pairs:
+        step = 256 if "ws" in (w, o) else 16
+        for moved, still in ((w, o), (o, w)):
+            for where in (at[still], at[still] + (size[still] - 1) // step * step, at[still] - (size[moved] - 1) // step * step):
+                assert run(**{moved: where}) == UNSUP, (moved, still, hex(where))
