@@ -325,6 +325,8 @@ def sbn_bitlinear_backward(dY, xq, a_scale, vals, meta, w_scale, N: int, K: int,
 
 
 def sbn_head_workspace_bytes(T: int, N: int, K: int, top: int = 0, backward: bool = False) -> int:
+    if any(v < 0 or v > 1 << 30 for v in (T, N, K, top)):       # refused sizes; ctypes would keep the low 32 bits
+        return 0
     return int(lib().sbn_head_workspace_bytes(1 if backward else 0, T, N, K, top))
 
 

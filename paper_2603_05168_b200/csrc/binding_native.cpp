@@ -316,9 +316,10 @@ PyObject* py_head_workspace_bytes(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!expect(n, 5)) return nullptr;
     long long v[4];
     for (int i = 0; i < 4; ++i) {
-        v[i] = PyLong_AsLongLong(a[i]);
+        int past = 0;
+        v[i] = PyLong_AsLongLongAndOverflow(a[i], &past);
         if (v[i] == -1 && PyErr_Occurred()) return nullptr;
-        if (v[i] < 0 || v[i] > (1ll << 30)) return PyLong_FromLong(0);       // refused sizes
+        if (past != 0 || v[i] < 0 || v[i] > (1ll << 30)) return PyLong_FromLong(0);       // refused sizes
     }
     return PyLong_FromSize_t(f_head_workspace_bytes(PyObject_IsTrue(a[4]), static_cast<int>(v[0]), static_cast<int>(v[1]), static_cast<int>(v[2]), static_cast<int>(v[3])));
 }

@@ -222,3 +222,17 @@ def test_nothing_written_may_lie_on_anything_else(L, call):
         for moved, still in ((w, o), (o, w)):
             for where in (at[still], at[still] + (size[still] - 1) // step * step, at[still] - (size[moved] - 1) // step * step):
                 assert run(**{moved: where}) == UNSUP, (moved, still, hex(where))
+
+
+@pytest.mark.parametrize("big", [(1 << 32) + 4, (1 << 31) + 4, -(1 << 32) + 4, 1 << 70])
+def test_workspace_of_sizes_past_32_bits(L, big):
+    # no size that only its low 32 bits make look possible
+    from paper_2603_05168_b200 import binding as b
+    for at in range(3):
+        sizes = [4, 1000, 256]
+        sizes[at] = big
+        assert b.sbn_head_workspace_bytes(*sizes) == 0
+        assert b._load_native().head_workspace_bytes(*sizes, 0, False) == 0
+        with pytest.raises(ValueError):
+            b.alloc_head_ws(*sizes, device="cpu")
+    assert b.sbn_head_workspace_bytes(4, 1000, 256, top=big) == 0
