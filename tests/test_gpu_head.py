@@ -674,3 +674,13 @@ def test_losses_of_sure_tokens(T, K, label_logit, top):
         tol = kd * (torch.expm1(2 * bz) + 2.0 ** -16) + 64 * 2.0 ** -23 + (top + 2) * 2.0 ** -24
         assert float(f["distill"].min()) >= -(top + 2) * 2.0 ** -24, float(f["distill"].min())
         assert_near("distill", f["distill"], o["distill"], tol)
+
+
+@pytest.mark.parametrize("big", [(1 << 32) + 4, -(1 << 32) + 4, 1 << 70])
+def test_workspace_of_sizes_past_32_bits(big):
+    forward(make(4, 100, 128, seed=137))                    # the extension is there
+    for at in range(3):
+        sizes = [4, 1000, 256]
+        sizes[at] = big
+        with pytest.raises(ValueError):
+            b.alloc_head_ws(*sizes)

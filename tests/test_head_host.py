@@ -232,7 +232,6 @@ def test_workspace_of_sizes_past_32_bits(L, big):
         sizes = [4, 1000, 256]
         sizes[at] = big
         assert b.sbn_head_workspace_bytes(*sizes) == 0
-        assert b._load_native().head_workspace_bytes(*sizes, 0, False) == 0
         with pytest.raises(ValueError):
             b.alloc_head_ws(*sizes, device="cpu")
     assert b.sbn_head_workspace_bytes(4, 1000, 256, top=big) == 0
