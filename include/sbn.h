@@ -454,7 +454,8 @@ sbn_status sbn_tile_canonical(const int8_t *vals_plain, const uint8_t *meta_plai
  *               at); a row with none, or with none but logits of -infinity, is left out: loss 0, no gradient.  An index
  *               that comes twice counts twice.  An index >= N: distill_loss NaN, no gradient of it, SBN_ERR_INDEX as above
  *   top_logits  device, [T][top] of top_dtype (SBN_OUT_F32 or SBN_OUT_BF16);  top from 1 to 256, else SBN_ERR_UNSUPPORTED
- *   temperature tau, positive and finite, and so is 1.45 / tau (else SBN_ERR_UNSUPPORTED)
+ *   temperature tau, positive and finite, and so is 1.45 / tau; for the backward call at least 2^-10, since the p of its
+ *               gradient are off by about 2^-23 |z| / tau of themselves (else SBN_ERR_UNSUPPORTED)
  *   labels, ce_loss  both or neither: the cross entropy of the same logits (at temperature 1) in the same pass over the
  *               head, as above; a row is left out of the products if neither loss asks for it
  *   lse         device out, fp32 [T], with labels [2][T]: lse[1] is that of temperature 1; 0 where its loss is left out

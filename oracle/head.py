@@ -76,7 +76,8 @@ def bounds(o, tau=1.0, d_ce=None, d_distill=None):
              argument (relative 2^-23 of a difference of logits, in units of the logits' range) by less than
              2^-16 + 2^-21 range / tau; the result is rounded to fp32
       loss   the same and bz of the target's logit / tau
-      p      relative: (bz + max bz) / tau + 2^-16 + 2^-20 (|z| + |lse|) / tau (fma of z and lse in fp32)
+      p      relative: (bz + max bz) / tau + 2^-16 + 2^-20 (|z| + |lse|) / tau (fma of z and lse in fp32); and 2^-126: ex2 gives
+             0 for what is below the smallest normal number (the ftz of its name)
       dz     that share of g p, and 2^-8 |dz| for the rounding to bf16 (2^-7 |g q| where a target is taken off in fp32: its
              own rounding is 2^-24, covered)
       dx     sum |err dz| |w| + N 2^-23 sum |dz w| + 2^-8 |dx|;  dhead alike over the tokens"""
@@ -102,7 +103,7 @@ def bounds(o, tau=1.0, d_ce=None, d_distill=None):
             rel = (bz + mz[:, None]) / t + 2.0 ** -16 + 2.0 ** -20 * (Z.abs() / t + lse.abs())
             asked = o["lse_" + name] != 0
             gg = torch.where(asked, g.to(F64).abs() / t, 0.0)[:, None]
-            err += 1.01 * gg * p * rel
+            err += 1.01 * gg * p * rel + gg * 2.0 ** -126
             if name == "distill":
                 err += 2.0 ** -20 * gg * o["Q"]
         dz = o["dz"].abs()

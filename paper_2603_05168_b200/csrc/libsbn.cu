@@ -1066,10 +1066,16 @@ static sbn_status head_call(HeadCall* c, bool backward, const void* x, int T, in
                   top_dtype == SBN_OUT_BF16, top, tau, static_cast<char*>(ws)};
     return SBN_OK;
 }
-static sbn_status head_distill_args(const int64_t* top_index, const void* top_logits, int top_dtype, int top, float tau) {
+// The backward call has p = exp(z / tau - lse) with lse in fp32: what that rounds off, 2^-24 |z| / tau, is the relative error of p, and
+// with it of the gradient.  From 2^-10 on it is below bf16's own 2^-8 for logits up to 64; at 1e-6 gradients of ordinary logits were 15 % off,
+// at 1e-8 they overflowed.  The forward call takes differences of logits and is right at any temperature.
+constexpr float kHeadLeastBackwardTau = 0x1p-10f;
+
+static sbn_status head_distill_args(bool backward, const int64_t* top_index, const void* top_logits, int top_dtype, int top, float tau) {
     if (!top_index || !top_logits) return SBN_ERR_NULL;
     if (top < 1 || top > kHeadMaxTop || (top_dtype != SBN_OUT_F32 && top_dtype != SBN_OUT_BF16)) return SBN_ERR_UNSUPPORTED;
     // 1.45: log2(e) with the factor that logits get (head_logit_scale, at most 1 + 2^-10)
+    if (backward && tau < kHeadLeastBackwardTau) return SBN_ERR_UNSUPPORTED;
     if (!(tau > 0.0f) || !std::isfinite(tau) || !std::isfinite(static_cast<float>(1.45 / static_cast<double>(tau)))) return SBN_ERR_UNSUPPORTED;
     return SBN_OK;
 }
@@ -1137,7 +1143,7 @@ sbn_status sbn_head_distill(const void* x_bf16, int T, int K, const void* head_b
                             void* ws, size_t ws_bytes, void* stream) {
     if (!distill_loss || !lse || (labels != nullptr) != (ce_loss != nullptr)) return SBN_ERR_NULL;
     HeadCall c;
-    sbn_status st = head_distill_args(top_index, top_logits, top_dtype, top, temperature);
+    sbn_status st = head_distill_args(false, top_index, top_logits, top_dtype, top, temperature);
     if (st == SBN_OK) st = head_call(&c, false, x_bf16, T, K, head_bf16, N, labels, top_index, top_logits, top_dtype, top, temperature, ws, ws_bytes);
     if (st != SBN_OK) return st;
     if (misaligned(distill_loss, 4) || misaligned(lse, 4) || (ce_loss && misaligned(ce_loss, 4))) return SBN_ERR_ALIGN;
@@ -1153,7 +1159,7 @@ sbn_status sbn_head_distill_backward(const void* x_bf16, int T, int K, const voi
                                      void* stream) {
     if (!lse || !d_distill || (labels != nullptr) != (d_ce != nullptr)) return SBN_ERR_NULL;
     HeadCall c;
-    sbn_status st = head_distill_args(top_index, top_logits, top_dtype, top, temperature);
+    sbn_status st = head_distill_args(true, top_index, top_logits, top_dtype, top, temperature);
     if (st == SBN_OK) st = head_call(&c, true, x_bf16, T, K, head_bf16, N, labels, top_index, top_logits, top_dtype, top, temperature, ws, ws_bytes);
     if (st == SBN_OK) st = head_gradient_args(x_bf16, head_bf16, dx_bf16, dhead_bf16);
     if (st != SBN_OK) return st;

@@ -684,3 +684,28 @@ def test_workspace_of_sizes_past_32_bits(big):
         sizes[at] = big
         with pytest.raises(ValueError):
             b.alloc_head_ws(*sizes)
+
+
+@pytest.mark.parametrize("tau", [0.1, 0.01, 2.0 ** -10])
+@pytest.mark.parametrize("T", [6, 60, 400])
+def test_small_temperatures(T, tau):
+    # logits up to 8: z / tau up to 8192, and p 2^-24 * 8192 = 5e-4 off beside bf16's own roundings (2^-8 at most, each)
+    c = make(T, 700, 256, seed=5 + T, top=5, labels=False, ignored=0.0, scale=0.1)
+    c["tau"] = tau
+    o, _ = reference(c)
+    f, dx, dhead = check(c)
+    for got, want in ((dx, o["dx"]), (dhead, o["dhead"])):
+        assert float((got.double() - want).norm() / want.norm()) < 2 * 2.0 ** -8 + 2.0 ** -10
+
+
+@pytest.mark.parametrize("T", [6, 60, 400])
+def test_temperatures_that_only_the_loss_has(T):
+    c = make(T, 700, 256, seed=5 + T, top=5, labels=False, ignored=0.0, scale=0.1)
+    for tau in (1e-4, 1e-8):
+        c["tau"] = tau
+        o, bd = reference(dict(c, d_distill=None))
+        f = forward(c)
+        assert_near("distill", f["distill"], o["distill"], bd["distill"])
+        with pytest.raises(b.SbnError) as err:
+            backward(c, f["lse"])
+        assert err.value.code == 4

@@ -235,3 +235,10 @@ def test_workspace_of_sizes_past_32_bits(L, big):
         with pytest.raises(ValueError):
             b.alloc_head_ws(*sizes, device="cpu")
     assert b.sbn_head_workspace_bytes(4, 1000, 256, top=big) == 0
+
+
+def test_smallest_temperature_of_the_gradient(L):
+    # (the forward call goes on to the workspace, which is too small here)
+    for tau in (2.0 ** -10 * (1 - 2.0 ** -24), 1e-4, 1e-8, 1e-30):
+        assert _kdb(L, tau=tau) == UNSUP and _kd(L, tau=tau, wsb=100) == WS
+    assert _kdb(L, tau=2.0 ** -10, wsb=100) == WS
