@@ -709,3 +709,125 @@ def test_temperatures_that_only_the_loss_has(T):
         with pytest.raises(b.SbnError) as err:
             backward(c, f["lse"])
         assert err.value.code == 4
+
+
+# ---- how near the results are, beside the worst case that check() allows ----
+# T, N, K, tile: up to 16 tokens (dz in two parts where `two`), words on the lanes, row tiles with narrow and with wide gradients
+ACCURACY = [(8, 5003, 2560, 0, True), (8, 5003, 4096, 0, True), (16, 5003, 1024, 0, True), (16, 5003, 2560, 0, False), (40, 5003, 2560, 0, False),
+            (200, 9001, 2560, 0, False), (600, 9001, 2560, -256, False), (2100, 5003, 2560, -512, False), (300, 5003, 4096, 0, False)]
+# One rounding to bf16 is off by something even between -2^(e-8) and 2^(e-8) for values from 2^e to 2^(e+1): 2^-8 / sqrt(3) of the value in the
+# 2-norm at most (values just above a power of two).  5 % for what the logits' own errors and the small entries of dz add
+ONE_ROUNDING = 1.05 * 2.0 ** -8 / 3 ** 0.5
+
+
+def relative(got, want):
+    return float((got.double() - want).norm() / want.norm())
+
+
+@pytest.mark.parametrize("T,N,K,tile,two", ACCURACY)
+def test_gradients_of_a_mean_are_off_by_one_rounding(T, N, K, tile, two):
+    # no token knows its label: its dz is -d (1 - p), p around 1 / N.  All d alike, half way between two bf16 numbers: the unit that dz is
+    # kept in makes it -1, else every target would be off by 2^-8 in the same direction (2-norm 4e-3 instead of 1.7e-3)
+    b.sbn_set_gemm_tuning(tile, 0)
+    c = make(T, N, K, seed=139 + T, ignored=0.0, lean=0.0)
+    c["d_ce"].fill_((0.5 + 2.0 ** -9) / 1024)
+    o, _ = reference(c)
+    dx, dhead = backward(c, forward(c)["lse"])
+    b.sbn_check_status()
+    assert relative(dx, o["dx"]) < ONE_ROUNDING
+    assert relative(dhead, o["dhead"]) < ONE_ROUNDING
+
+
+@pytest.mark.parametrize("T,N,K,tile,two", ACCURACY)
+def test_gradients_with_weights_of_their_own(T, N, K, tile, two):
+    # every second token's weight is half way between two bf16 numbers even in the call's unit.  Two parts of dz: the results' own rounding is
+    # all there is.  One part: that and at most 2^-8 of every entry of dz, independent of each other and of it
+    b.sbn_set_gemm_tuning(tile, 0)
+    c = make(T, N, K, seed=149 + T, ignored=0.0, lean=0.0)
+    c["d_ce"].fill_(1.0 / 1024)
+    c["d_ce"][1::2] = (0.5 + 2.0 ** -9) / 1024
+    o, _ = reference(c)
+    dx, dhead = backward(c, forward(c)["lse"])
+    b.sbn_check_status()
+    tol = ONE_ROUNDING if two else 1.05 * 2.0 ** -8 * (4 / 3) ** 0.5
+    assert relative(dx, o["dx"]) < tol
+    assert relative(dhead, o["dhead"]) < tol
+    if two:                                                 # token by token: one part would be 4e-3 off in every second
+        rows = (dx.double() - o["dx"]).norm(dim=1) / o["dx"].norm(dim=1)
+        assert float(rows.max()) < tol, rows
+
+
+@pytest.mark.parametrize("top", [0, 7])
+@pytest.mark.parametrize("T,N,K,tile,two", ACCURACY)
+def test_losses_are_not_off_in_one_direction(T, N, K, tile, two, top):
+    # logits N(0, 3^2): what the tensor cores cut off would make lse, and with it every loss, K 2^-30 E_p[z] too small on average (2e-5 at
+    # 2560 columns); the factor that takes it back leaves a fifth of it or less.  Half of it is the line here, for the rounding of c0 and the losses (less than 2^-24 of lse each) besides
+    b.sbn_set_gemm_tuning(tile, 0)
+    c = make(T, N, K, seed=151 + T, ignored=0.0, lean=0.0, scale=3.0 / K ** 0.5, top=top, absent=0.0)
+    o, _ = reference(c)
+    f = forward(c)
+    b.sbn_check_status()
+    P = torch.softmax(o["Z"], 1)
+    bias = K * 2.0 ** -30 * float((P * o["Z"]).sum(1).mean())
+    for name in ("ce", "distill") if top else ("ce",):
+        err = f[name].double() - o[name]
+        assert abs(float(err.mean())) < 0.5 * bias + 2.0 ** -23 * float(o["lse_ce"].abs().mean()), (name, float(err.mean()), bias)
+        # a single loss: the bias once more, and the label's (or the entries') logit in fp32: sqrt(24) additions of at most |z| (12) / 2^24
+        assert float(err.pow(2).mean().sqrt()) < bias + 5 * 12 * 2.0 ** -24 + 2.0 ** -23 * float(o["lse_ce"].abs().mean()) + \
+            (K * 2.0 ** -30 * 3.0 if top else 0.0), name
+
+
+@pytest.mark.parametrize("kind", ["whole", "sparse", "steady"])
+@pytest.mark.parametrize("T,K,tile", [(8, 2560, 0), (16, 2560, 0), (60, 2560, 0), (256, 8192, 0), (300, 2560, 0), (700, 8192, -512)])
+def test_logits_that_nothing_or_much_is_cut_off(T, K, tile, kind):
+    """The factor is made for sums of changing sign.  Sums that fit 24 bits ("whole": small whole numbers; "sparse": a few entries that are not 0) lose
+    nothing and come out K 2^-30 too large; sums that only grow ("steady") lose more than it gives back: an MMA of 16 columns cuts off less
+    than 2^-23 of the running sum, which is half of the logit on average, K / 16 times: K 2^-28 of the logit at most."""
+    N = 3001
+    b.sbn_set_gemm_tuning(tile, 0)
+    g = torch.Generator(device="cuda").manual_seed(157 + T)
+    whole = lambda lo, hi, *s: torch.randint(lo, hi + 1, s, generator=g, device="cuda").float()
+    if kind == "whole":
+        x, head = whole(-3, 3, T, K), whole(-2, 2, N, K) / 64
+    elif kind == "sparse":
+        at = torch.randint(0, K, (T, 4), generator=g, device="cuda")
+        x, head = torch.zeros(T, K, device="cuda").scatter_(1, at, whole(-4, 4, T, 4) * 4), whole(-8, 8, N, K) / 16
+    else:
+        x, head = torch.rand(T, K, generator=g, device="cuda"), torch.rand(N, K, generator=g, device="cuda") * 80 / K
+    y = torch.randint(0, N, (T,), generator=g, device="cuda")
+    c = dict(T=T, N=N, K=K, x=x.to(BF16), head=head.to(BF16), tau=1.0, labels=y, d_ce=torch.full((T,), 1.0 / T, device="cuda"))
+    if kind == "sparse":
+        c["x"][::2, 5] = 24.0                               # tokens that know their label: its logit is 24, exactly
+        c["head"][:, 5] = 0.0
+        c["head"][y[::2], 5] = 1.0
+        c["x"][::2, :5] = 0.0
+        c["x"][::2, 6:] = 0.0
+    o, _ = reference(c)
+    f = forward(c)
+    b.sbn_check_status()
+    Z = o["Z"]
+    share = 2.0 ** -28 if kind == "steady" else 2.0 ** -30
+    # and what lse and loss have besides: 64 additions of the sum, ex2 (2^-22), c0 and its product (2^-24 of the logits' range each), the
+    # results' rounding and the label's logit in fp32 (5 of them)
+    rest = 64 * 2.0 ** -24 + 2.0 ** -22 + 2.0 ** -23 * (Z.max(1).values - Z.min(1).values) + 5 * 2.0 ** -24 * (o["lse_ce"].abs() + Z.abs().max(1).values)
+    tol = K * share * Z.abs().max(1).values + rest
+    assert_near("lse", f["lse"], o["lse_ce"], tol)
+    assert_near("ce", f["ce"], o["ce"], tol)
+    assert float(f["ce"].min()) >= 0.0
+
+
+@pytest.mark.parametrize("T,K,tile", [(8, 2560, 0), (16, 2560, 0), (60, 2560, 0), (256, 8192, 0), (300, 2560, 0), (700, 8192, -512)])
+def test_sure_tokens_whose_logits_are_exact(T, K, tile):
+    # one entry of x per token, in a column of its own where only the label's word is not 0: its logit is 24 exactly, all others are 0, and the loss
+    # is log(1 + 3000 exp(-24)) = 1.1e-7, up to 64 additions to a sum of 1 (see test_losses_of_sure_tokens)
+    N = 3001
+    b.sbn_set_gemm_tuning(tile, 0)
+    at = torch.arange(T, device="cuda")
+    y = (at * 7 + 3) % N
+    x, head = torch.zeros(T, K, device="cuda"), torch.zeros(N, K, device="cuda")
+    x[at, at * 3 + 5], head[y, at * 3 + 5] = 24.0, 1.0
+    f = forward(dict(T=T, N=N, K=K, x=x.to(BF16), head=head.to(BF16), labels=y))
+    b.sbn_check_status()
+    want = torch.full((T,), 3000.0, dtype=torch.float64, device="cuda").mul(torch.exp(torch.tensor(-24.0, dtype=torch.float64))).log1p()
+    assert float(f["ce"].min()) >= 0.0
+    assert_near("ce", f["ce"], want, torch.full_like(want, 64 * 2.0 ** -23))
