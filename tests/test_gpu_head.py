@@ -831,3 +831,33 @@ def test_sure_tokens_whose_logits_are_exact(T, K, tile):
     want = torch.full((T,), 3000.0, dtype=torch.float64, device="cuda").mul(torch.exp(torch.tensor(-24.0, dtype=torch.float64))).log1p()
     assert float(f["ce"].min()) >= 0.0
     assert_near("ce", f["ce"], want, torch.full_like(want, 64 * 2.0 ** -23))
+
+
+# 1 to 16 tokens with more columns than the register-fed kernels take; several groups of tokens, the last one with a token or a few
+@pytest.mark.parametrize("top", [0, 9])
+@pytest.mark.parametrize("T,N,K", [(1, 300, 4224), (3, 1, 5120), (8, 2000, 8192), (16, 1000, 4224), (97, 1000, 384), (225, 513, 256), (193, 4100, 128), (129, 9001, 256)])
+def test_words_on_the_lanes_in_groups(T, N, K, top):
+    check(make(T, N, K, seed=T + N + K, top=top))
+
+
+# tokens of a whole batch: pieces of the vocabulary at their narrowest (1024 words), many row tiles, dx added up piece by piece
+@pytest.mark.parametrize("T,N,K,top", [(20011, 5000, 256, 0), (66001, 2100, 128, 0), (9001, 4200, 384, 3)])
+def test_tokens_of_a_whole_batch(T, N, K, top):
+    check(make(T, N, K, seed=163, top=top))
+
+
+@pytest.mark.parametrize("T,tile", [(100, 0), (256, 0), (600, -512)])
+def test_waits_are_bounded_with_words_on_the_lanes_and_wide_tiles(T, tile):
+    b.sbn_set_gemm_tuning(tile, 0)
+    c = make(T, 1700, 640, seed=167, top=3)
+    f = forward(c)
+    try:
+        b.sbn_set_wait_test(True, 1000)
+        for call in (lambda: forward(c), lambda: backward(c, f["lse"]), lambda: backward(c, f["lse"], dx=False), lambda: backward(c, f["lse"], dhead=False)):
+            call()
+            with pytest.raises(b.SbnError) as err:
+                b.sbn_check_status()
+            assert err.value.code == 7
+    finally:
+        b.sbn_set_wait_test(False, 0)
+    check(c)
