@@ -71,9 +71,9 @@ typedef enum {
     SBN_OK = 0,
     SBN_ERR_NULL = 1,        /* a required pointer is NULL */
     SBN_ERR_SHAPE = 2,       /* a dimension is <= 0 or breaks the divisibility rules above */
-    SBN_ERR_ALIGN = 3,       /* a pointer is not 16-byte aligned */
-    SBN_ERR_UNSUPPORTED = 4, /* pattern other than 2:4 / 6:8, unknown dtype or op */
-    SBN_ERR_WORKSPACE = 5,   /* workspace missing or smaller than sbn_workspace_bytes() */
+    SBN_ERR_ALIGN = 3,       /* a pointer is not aligned: 16 bytes, or what its argument says */
+    SBN_ERR_UNSUPPORTED = 4, /* pattern other than 2:4 / 6:8, unknown dtype or op, overlapping buffers */
+    SBN_ERR_WORKSPACE = 5,   /* workspace missing or smaller than sbn_workspace_bytes() resp. sbn_head_workspace_bytes() */
     SBN_ERR_CUDA = 6,        /* a CUDA runtime/driver call failed (launch, tensor map, ...) */
     SBN_ERR_TIMEOUT = 7,     /* a bounded device-side wait ran out (see sbn_check_status) */
     SBN_ERR_TOO_LARGE = 8,   /* problem exceeds what the library's built-in scratch can serve */

@@ -1187,9 +1187,9 @@ const char* sbn_status_string(sbn_status s) {
     switch (s) {
         case SBN_OK: return "ok";
         case SBN_ERR_NULL: return "a required pointer is NULL";
-        case SBN_ERR_SHAPE: return "bad shape (need T >= 1, N % 128 == 0, K % 128 == 0)";
-        case SBN_ERR_ALIGN: return "pointer not 16-byte aligned";
-        case SBN_ERR_UNSUPPORTED: return "unsupported pattern, dtype or op";
+        case SBN_ERR_SHAPE: return "bad shape (need T >= 1, K % 128 == 0 and, but at the output head, N % 128 == 0)";
+        case SBN_ERR_ALIGN: return "pointer not aligned as its argument asks (16 bytes where nothing else is said)";
+        case SBN_ERR_UNSUPPORTED: return "unsupported pattern, dtype, op or argument, or buffers that overlap";
         case SBN_ERR_WORKSPACE: return "workspace missing or too small";
         case SBN_ERR_CUDA: return "CUDA call failed";
         case SBN_ERR_TIMEOUT: return "a bounded device-side wait ran out";

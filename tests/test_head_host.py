@@ -242,3 +242,10 @@ def test_smallest_temperature_of_the_gradient(L):
     for tau in (2.0 ** -10 * (1 - 2.0 ** -24), 1e-4, 1e-8, 1e-30):
         assert _kdb(L, tau=tau) == UNSUP and _kd(L, tau=tau, wsb=100) == WS
     assert _kdb(L, tau=2.0 ** -10, wsb=100) == WS
+
+
+def test_messages_fit_the_calls_at_the_head(L):
+    # any N is right there, a workspace starts on 256 bytes, overlapping buffers are unsupported
+    from paper_2603_05168_b200 import binding as b
+    assert "output head" in b.status_string(SHAPE)
+    assert not b.status_string(ALIGN).startswith("pointer not 16-byte") and "overlap" in b.status_string(UNSUP)
