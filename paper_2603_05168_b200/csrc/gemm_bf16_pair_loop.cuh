@@ -45,8 +45,7 @@ struct PairLoop {
     static_assert(kSmemBytes <= 232448 && Work::kStagingBytes % 1024 == 0, "shared memory overflow");
 };
 
-// Barrier of the epilogue warps of a CTA (narrow tiles).
-__device__ __forceinline__ void epilogue_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+// Whether all epilogue warps of a CTA say yes (narrow tiles).
 __device__ __forceinline__ bool epilogue_all(bool ok) {
     uint32_t all;
     asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.and.pred q, 1, 256, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"

@@ -43,9 +43,10 @@ static std::atomic<unsigned long long> g_launch_count{0ull};
 // kernel has already left, instead of after a full launch round trip.  The signal comes first, so
 // in a chain of short kernels (quantiser, GEMM, quantiser, GEMM, ...) a kernel is resident while
 // the one TWO places ahead still runs: its own wait keeps it correct, and a GEMM uses the time to
-// fetch weights.  All kernels here are
+// fetch weights.  Most kernels here are
 // persistent with every CTA resident from the start, so an early dependent only ever takes
-// resources nobody else is waiting for.  SBN_DISABLE_PDL=1 in the environment turns the
+// resources nobody else is waiting for.  (Kernels with more CTAs than fit at once, head_losses_kernel and head_dx_kernel, are safe for another
+// reason: the signal of a grid is given when its last CTA has started, and none of them waits for another.)  SBN_DISABLE_PDL=1 in the environment turns the
 // attribute off (the two instructions are then no-ops).
 // One exception in each direction, which belong together: the few-token GEMM kernel fetches its
 // first stages of WEIGHTS before pdl_wait (they do not depend on the kernel right before it in a

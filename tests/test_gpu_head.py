@@ -133,7 +133,7 @@ def test_few_tokens(T, N, K, top):
     check(make(T, N, K, seed=T + N + K, top=top))
 
 
-# up to 256 tokens words are on the lanes: token groups of 16 and 32, tiles of 128 words, more tiles than SMs
+# up to 256 tokens words are on the lanes: token groups of 32 and more, tiles of 256 words, more tiles than CTA pairs; sizes beyond that, too
 @pytest.mark.parametrize("top", [0, 11])
 @pytest.mark.parametrize("T,N,K", [(17, 129, 128), (32, 20001, 256), (47, 1000, 2560), (49, 19007, 384), (96, 128, 1024), (161, 5000, 128), (192, 301, 4224),
                                    (250, 38500, 128), (256, 2049, 640), (257, 2049, 640), (320, 19001, 256), (333, 900, 384), (385, 38500, 128), (448, 3000, 512), (449, 700, 256)])
