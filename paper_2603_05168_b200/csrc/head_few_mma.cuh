@@ -48,10 +48,6 @@ __device__ __forceinline__ void mma_bf16_k16(float (&d)[4], uint32_t a0, uint32_
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ void mma_bf16_k8(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t b0) {
-    asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5}, {%6}, {%0, %1, %2, %3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(b0));
-}
 __device__ __forceinline__ uint32_t transpose_8x8(uint32_t v) {
     uint32_t r;
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
@@ -240,6 +236,8 @@ static inline int head_few_shares(int K) { return K <= 1024 ? 2 : (K <= 2560 ? 5
 __host__ __device__ constexpr int few_backward_words(int kbw, int nt) { return kbw * (8 + 8 * nt) <= 100 ? 16 : 8; }    // dx and words: 4 bytes x this per thread
 static inline int head_few_words(int T, int K) { return few_backward_words(head_few_shares(K), T <= 8 ? 1 : 2); }
 
+constexpr float kFewLarge = 0x1p-6f;              // an entry of dz whose second bf16 part matters, in the call's unit
+
 // Words per step: 16 where the registers hold them beside dx (a 16-row MMA is full then, and a step's barriers are spread over twice
 // the words), else 8.
 template <int KBW, int NT, bool LIST, bool DUAL>
@@ -256,9 +254,12 @@ head_few_backward_kernel(const HeadFewParams p) {
     __shared__ int s_label[kTok];
     __shared__ int2 s_cursor[kFewHeadWarps];                        // a warp's token's next target and its word
     // dz in bf16, and what that leaves off as well, in bf16 again: with few tokens a value of dW is a few products, and a gradient's
-    // own rounding to bf16 should be the only one that shows (1.7e-3 instead of 1.7e-3 to 3.6e-3 in the 2-norm; 8 tokens leave
-    // half of an MMA's indices free for it, 4 % of the time of a step).  Not for 16 tokens of more than 1024 columns: no registers
-    constexpr int kSplit = NT == 1 || KBW == 2 ? 2 : 1;
+    // own rounding to bf16 should be the only one that shows (1.7e-3 instead of 1.7e-3 to 3.7e-3 in the 2-norm; 8 tokens leave
+    // half of an MMA's indices free for it, 4 % of the time of a step).  For 16 tokens of more than 1024 columns dW gets the second part only in
+    // steps where an entry of dz is at least kFewLarge in the call's unit, that is where targets are: what smaller entries leave off adds
+    // less than 1 % to a gradient's own rounding, and in every step it took 30 % longer (16 x 2560 x 32000 143 us; now 121, 111 without)
+    constexpr bool kSome = NT == 2 && KBW > 2;
+    constexpr int kSplit = 2, kAlways = kSome ? 1 : 2;
     __shared__ __align__(16) uint16_t s_dz[kSplit][kTok][kWords];   // B operand of dx: pairs of words of a token
     __shared__ __align__(16) uint16_t s_dzt[kSplit][kWords][kTok];  // A operand of dW: pairs of tokens of a word
     extern __shared__ __align__(16) uint8_t s_x[];
@@ -343,6 +344,7 @@ head_few_backward_kernel(const HeadFewParams p) {
             if (NT == 2) *reinterpret_cast<float2*>(to + 8 * kRow) = make_float2(d[h][0][2] + d[h][1][2], d[h][0][3] + d[h][1][3]);
         }
         __syncthreads();
+        bool large = false;
         if (tid < kTok * kWords * kParts) {                         // whole warps, a token each
             const int tok = tid / (kWords * kParts), slot = tid / kParts % kWords, part = tid % kParts;
             const int n = nb * kWords + slot;
@@ -373,6 +375,7 @@ head_few_backward_kernel(const HeadFewParams p) {
                 v -= k.y;
             }
             if (n >= p.N || (k.y == 0.0f && k.w == 0.0f)) v = 0.0f;   // behind the vocabulary; nothing asked (z may be anything)
+            large = fabsf(v) >= kFewLarge;
 #pragma unroll
             for (int q = 0; q < kSplit; ++q) {
                 unsigned short o;
@@ -384,8 +387,41 @@ head_few_backward_kernel(const HeadFewParams p) {
                 v -= __uint_as_float(static_cast<uint32_t>(o) << 16);
             }
         }
-        __syncthreads();
-        uint32_t dz[kSplit][NT][H], dzt[kSplit][NT][2] = {};
+        if constexpr (kSome) large = __syncthreads_or(large);
+        else __syncthreads();
+        if constexpr (kSome) {
+            static_assert(!kSome || H == 1, "one row of words per lane");
+            if (large && p.dw != nullptr) {
+                // dW of this step, with both parts
+                uint32_t t_dz[2][NT];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    t_dz[0][nt] = *reinterpret_cast<const uint32_t*>(&s_dzt[0][g][nt * 8 + 2 * t4]);
+                    t_dz[1][nt] = *reinterpret_cast<const uint32_t*>(&s_dzt[1][g][nt * 8 + 2 * t4]);
+                }
+                const int n = nb * kWords + g;
+#pragma unroll
+                for (int i = 0; i < KBW; ++i) {
+                    const int kb = warp + kFewHeadWarps * i;
+                    if (kb < kbs) {
+                        uint32_t lo[4], hi[4], o[4];
+                        ldmatrix_x4<true>(lo, x_lane + kb * 64);
+                        ldmatrix_x4<true>(hi, x_lane + 8 * pitch + kb * 64);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            float e[4] = {};
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) mma_bf16_k16(e, t_dz[k][0], 0u, t_dz[k][NT - 1], 0u, lo[j], hi[j]);
+                            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[j]) : "f"(e[1] * unit), "f"(e[0] * unit));
+                        }
+                        if (n < p.N) *reinterpret_cast<uint4*>(p.dw + static_cast<size_t>(n) * p.K + kb * 32 + t4 * 8) = make_uint4(o[0], o[1], o[2], o[3]);
+                        __syncwarp();
+                    }
+                }
+            }
+        }
+        const bool write_dw = p.dw != nullptr && !(kSome && large);
+        uint32_t dz[kSplit][NT][H], dzt[kAlways][NT][2] = {};
 #pragma unroll
         for (int q = 0; q < kSplit; ++q)
 #pragma unroll
@@ -393,7 +429,7 @@ head_few_backward_kernel(const HeadFewParams p) {
 #pragma unroll
                 for (int h = 0; h < H; ++h) {
                     dz[q][nt][h] = *reinterpret_cast<const uint32_t*>(&s_dz[q][nt * 8 + g][h * 8 + 2 * t4]);
-                    dzt[q][nt][h] = *reinterpret_cast<const uint32_t*>(&s_dzt[q][h * 8 + g][nt * 8 + 2 * t4]);
+                    if (q < kAlways) dzt[q < kAlways ? q : 0][nt][h] = *reinterpret_cast<const uint32_t*>(&s_dzt[q][h * 8 + g][nt * 8 + 2 * t4]);
                 }
 #pragma unroll
         for (int i = 0; i < KBW; ++i) {
@@ -414,14 +450,13 @@ head_few_backward_kernel(const HeadFewParams p) {
                         } else {
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt) {
-                                if constexpr (kSplit == 2) mma_bf16_k16(acc[i][q][nt], a0, a1, a0, a1, dz[0][nt][0], dz[kSplit - 1][nt][0]);
-                                else mma_bf16_k8(acc[i][q][nt], a0, a1, dz[0][nt][0]);
+                                mma_bf16_k16(acc[i][q][nt], a0, a1, a0, a1, dz[0][nt][0], dz[1][nt][0]);
                             }
                         }
                     }
                 }
                 load_block(i, nb + static_cast<int>(gridDim.x));
-                if (p.dw != nullptr) {
+                if (write_dw) {
                     uint32_t lo[4], hi[4];
                     ldmatrix_x4<true>(lo, x_lane + kb * 64);
                     if (NT == 2) ldmatrix_x4<true>(hi, x_lane + 8 * pitch + kb * 64);
@@ -430,10 +465,10 @@ head_few_backward_kernel(const HeadFewParams p) {
                     for (int j = 0; j < 4; ++j) {
                         float e[4] = {};
                         if constexpr (NT == 1) {
-                            mma_bf16_k16(e, dzt[0][0][0], dzt[0][0][1], dzt[kSplit - 1][0][0], dzt[kSplit - 1][0][1], lo[j], lo[j]);
+                            mma_bf16_k16(e, dzt[0][0][0], dzt[0][0][1], dzt[kAlways - 1][0][0], dzt[kAlways - 1][0][1], lo[j], lo[j]);
                         } else {
 #pragma unroll
-                            for (int k = 0; k < kSplit; ++k) mma_bf16_k16(e, dzt[k][0][0], dzt[k][0][1], dzt[k][NT - 1][0], dzt[k][NT - 1][1], lo[j], hi[j]);
+                            for (int k = 0; k < kAlways; ++k) mma_bf16_k16(e, dzt[k][0][0], dzt[k][0][1], dzt[k][NT - 1][0], dzt[k][NT - 1][1], lo[j], hi[j]);
                         }
 #pragma unroll
                         for (int h = 0; h < H; ++h)

@@ -861,3 +861,21 @@ def test_waits_are_bounded_with_words_on_the_lanes_and_wide_tiles(T, tile):
     finally:
         b.sbn_set_wait_test(False, 0)
     check(c)
+
+
+@pytest.mark.parametrize("top", [0, 3])
+@pytest.mark.parametrize("T,N,K", [(9, 2003, 1152), (12, 5003, 2048), (16, 5003, 2560)])
+def test_gradients_of_few_tokens_are_off_by_their_own_rounding(T, N, K, top):
+    # as test_gradients_with_weights_of_their_own, token by token and for the labels' words: dz in one part is 4e-3 off there
+    c = make(T, N, K, seed=173 + T, ignored=0.0, lean=0.0, top=top, absent=0.0)
+    c["labels"] = torch.arange(T, device="cuda") * (N // T) + 5
+    c["d_ce"].fill_(1.0 / 1024)
+    c["d_ce"][1::2] = (0.5 + 2.0 ** -9) / 1024
+    if top:
+        c["d_distill"] = c["d_ce"] / 2
+    o, _ = reference(c)
+    dx, dhead = backward(c, forward(c)["lse"])
+    b.sbn_check_status()
+    for got, want in ((dx, o["dx"]), (dhead[c["labels"]], o["dhead"][c["labels"]])):
+        rows = (got.double() - want).norm(dim=1) / want.norm(dim=1)
+        assert float(rows.max()) < ONE_ROUNDING, rows
