@@ -236,7 +236,7 @@ static inline int head_few_shares(int K) { return K <= 1024 ? 2 : (K <= 2560 ? 5
 __host__ __device__ constexpr int few_backward_words(int kbw, int nt) { return kbw * (8 + 8 * nt) <= 100 ? 16 : 8; }    // dx and words: 4 bytes x this per thread
 static inline int head_few_words(int T, int K) { return few_backward_words(head_few_shares(K), T <= 8 ? 1 : 2); }
 
-constexpr float kFewLarge = 0x1p-6f;              // an entry of dz whose second bf16 part matters, in the call's unit
+constexpr float kFewLarge = 0x1p-9f;              // an entry of dz whose second bf16 part matters, in the call's unit
 
 // Words per step: 16 where the registers hold them beside dx (a 16-row MMA is full then, and a step's barriers are spread over twice
 // the words), else 8.
@@ -256,8 +256,8 @@ head_few_backward_kernel(const HeadFewParams p) {
     // dz in bf16, and what that leaves off as well, in bf16 again: with few tokens a value of dW is a few products, and a gradient's
     // own rounding to bf16 should be the only one that shows (1.7e-3 instead of 1.7e-3 to 3.7e-3 in the 2-norm; 8 tokens leave
     // half of an MMA's indices free for it, 4 % of the time of a step).  For 16 tokens of more than 1024 columns dW gets the second part only in
-    // steps where an entry of dz is at least kFewLarge in the call's unit, that is where targets are: what smaller entries leave off adds
-    // less than 1 % to a gradient's own rounding, and in every step it took 30 % longer (16 x 2560 x 32000 143 us; now 121, 111 without)
+    // steps where an entry of dz is at least kFewLarge in the call's unit, that is where targets are: smaller ones make a gradient by the hundreds, and
+    // what they leave off averages out.  In every step it took 30 % longer (16 x 2560 x 32000 143 us; now 121, 111 without)
     constexpr bool kSome = NT == 2 && KBW > 2;
     constexpr int kSplit = 2, kAlways = kSome ? 1 : 2;
     __shared__ __align__(16) uint16_t s_dz[kSplit][kTok][kWords];   // B operand of dx: pairs of words of a token
