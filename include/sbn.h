@@ -435,7 +435,7 @@ sbn_status sbn_tile_canonical(const int8_t *vals_plain, const uint8_t *meta_plai
  * it, is given back.  A sum that is exact in 24 bits comes out that much too large (2.4e-6 of the logit at K = 2560), one whose
  * terms have all the same sign up to 5 K 2^-30 too small.  The gradient of the logits is rounded to bf16 (as a bf16 run holds it)
  * before it is multiplied with x and head: dx and dhead are 1.9e-3 to 2.6e-3 off in the 2-norm, of which their own bf16 is
- * 1.7e-3; up to 8 tokens of at most 4096 columns, and up to 16 of at most 2560, two bf16 parts leave that alone.
+ * 1.7e-3; up to 128 tokens it is taken in two bf16 parts, which leave that alone.
  *
  * sbn_head_cross_entropy: softmax cross entropy of every token,
  *   lse[t] = log sum_i exp z[t][i],   loss[t] = lse[t] - z[t][labels[t]]

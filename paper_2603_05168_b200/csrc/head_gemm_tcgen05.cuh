@@ -202,8 +202,10 @@ struct HeadRow {
         if (DUAL) p.part1[at] = s1;
     }
 
-    // Columns n .. n + 31 of dz in bf16, zeros in rows that nothing is asked of and behind the vocabulary.
-    __device__ void grad(const HeadLogitsParams& p, const uint32_t (&z)[32], int n, uint32_t (&o)[16]) {
+    // Columns n .. n + 31 of dz in bf16, zeros in rows that nothing is asked of and behind the vocabulary; SPLIT: and what bf16 leaves off,
+    // in bf16 again.
+    template <bool SPLIT = false>
+    __device__ void grad(const HeadLogitsParams& p, const uint32_t (&z)[32], int n, uint32_t (&o)[16], uint32_t* rest = nullptr) {
         while (next_col < n) step(p);
         float v[32];
 #pragma unroll
@@ -227,6 +229,11 @@ struct HeadRow {
         }
 #pragma unroll
         for (int q = 0; q < 16; ++q) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[q]) : "f"(v[2 * q + 1]), "f"(v[2 * q]));
+        if constexpr (SPLIT) {
+#pragma unroll
+            for (int q = 0; q < 16; ++q)
+                asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(rest[q]) : "f"(v[2 * q + 1] - bf16hi_to_f32(o[q])), "f"(v[2 * q] - bf16lo_to_f32(o[q])));
+        }
     }
 };
 

@@ -15,7 +15,9 @@ struct HeadPlan {
     int bn_piece;                 // columns per tile of the pieces' logits
     bool wide_grads;              // gradients in tiles of 512 columns, else 256
     int slots, slot_stages;       // slices of dx's contraction over a piece, and 64-column stages of each
-    long long rows64, rows256;    // T up to a multiple
+    int rest;                     // dz in two parts: rows from a token's to its second part's (kWordsTwoParts), else 0
+    int grad_rows;                // rows that the gradients' products have: the tokens, or both parts
+    long long rows64, rows256;    // grad_rows up to a multiple
 };
 
 static inline long long head_up(long long v, long long to) { return (v + to - 1) / to * to; }
@@ -39,15 +41,20 @@ static int head_tile_columns(int T, int cols, int K) {
 
 static HeadPlan head_plan(int T, int N, int K) {
     HeadPlan h{};
+    h.grad_rows = T;
     h.few = head_few_takes(T, K);
     if (h.few) {
         h.parts = std::min((N + 15) / 16, kNumSMs);
         h.slots = std::min((N + head_few_words(T, K) - 1) / head_few_words(T, K), kNumSMs);
         return h;
     }
-    h.rows64 = head_up(T, 64);
-    h.rows256 = head_up(T, 256);
     h.words = T <= kWordsTokens;
+    if (T <= kWordsTwoParts) {
+        h.rest = static_cast<int>(head_up(T, 64));
+        h.grad_rows = 2 * h.rest;
+    }
+    h.rows64 = head_up(h.grad_rows, 64);
+    h.rows256 = head_up(h.grad_rows, 256);
     if (h.words) {
         const int tiles = (N + 255) / 256;
         h.groups = std::max(1, std::min(kBackwardPairs / tiles, (T + 31) / 32));
@@ -111,7 +118,7 @@ static HeadWs head_ws_layout(const HeadPlan& h, bool backward, int T, int K, int
         if (top) w.part1 = take(4 * t * h.parts);
     } else {
         if (!h.few) w.dz = take(2 * static_cast<size_t>(h.rows256) * h.piece);
-        w.acc = take(4 * static_cast<size_t>(h.slots) * t * K);
+        w.acc = take(4 * static_cast<size_t>(h.slots) * h.grad_rows * K);
     }
     w.total = at;
     return w;
@@ -170,19 +177,25 @@ static sbn_status launch_head_logits(const HeadMaps& maps, const HeadLogitsParam
     return dual ? launch_head_logits_as<MODE, true, true>(maps, p, stream) : launch_head_logits_as<MODE, true, false>(maps, p, stream);
 }
 
-template <int MODE, bool LIST, bool DUAL>
+template <int MODE, bool LIST, bool DUAL, bool REST>
 static sbn_status launch_head_words_as(const HeadMaps& maps, const HeadWordsParams& p, cudaStream_t stream) {
-    using Loop = PairLoop<HeadWordsWork<MODE, LIST, DUAL>>;
-    if (!ensure_dynamic_smem<head_words_kernel<MODE, LIST, DUAL>>(232448)) return SBN_ERR_CUDA;
-    if (launch_kernel(head_words_kernel<MODE, LIST, DUAL>, dim3(2 * p.pairs), dim3(Loop::kThreads), words_smem_bytes(p.tokens), stream, maps, p) != cudaSuccess)
+    using Loop = PairLoop<HeadWordsWork<MODE, LIST, DUAL, REST>>;
+    if (!ensure_dynamic_smem<head_words_kernel<MODE, LIST, DUAL, REST>>(232448)) return SBN_ERR_CUDA;
+    if (launch_kernel(head_words_kernel<MODE, LIST, DUAL, REST>, dim3(2 * p.pairs), dim3(Loop::kThreads), words_smem_bytes(p.tokens), stream, maps, p) != cudaSuccess)
         return SBN_ERR_CUDA;
     ++g_launch_count;
     return SBN_OK;
 }
+template <int MODE, bool LIST, bool DUAL>
+static sbn_status launch_head_words_of(const HeadMaps& maps, const HeadWordsParams& p, cudaStream_t stream) {
+    if constexpr (MODE == 1)
+        if (p.rest != 0) return launch_head_words_as<MODE, LIST, DUAL, true>(maps, p, stream);
+    return launch_head_words_as<MODE, LIST, DUAL, false>(maps, p, stream);
+}
 template <int MODE>
 static sbn_status launch_head_words(const HeadMaps& maps, const HeadWordsParams& p, bool list, bool dual, cudaStream_t stream) {
-    if (!list) return launch_head_words_as<MODE, false, false>(maps, p, stream);
-    return dual ? launch_head_words_as<MODE, true, true>(maps, p, stream) : launch_head_words_as<MODE, true, false>(maps, p, stream);
+    if (!list) return launch_head_words_of<MODE, false, false>(maps, p, stream);
+    return dual ? launch_head_words_of<MODE, true, true>(maps, p, stream) : launch_head_words_of<MODE, true, false>(maps, p, stream);
 }
 
 // What is asked of the tokens: the labels themselves, or for a distillation the sorted targets of every token.
@@ -225,17 +238,18 @@ static sbn_status launch_head_losses(const HeadLossJob& j, cudaStream_t stream) 
     ++g_launch_count;
     return SBN_OK;
 }
-template <int GROUPS>
+template <int GROUPS, bool REST>
 static sbn_status launch_head_dx_as(const HeadDxJob& j, cudaStream_t stream) {
     constexpr int vecs = kDxThreads / GROUPS;
     const long long steps = (static_cast<long long>(j.T) * (j.K / 4) + vecs - 1) / vecs;
     const int blocks = static_cast<int>(std::min<long long>(steps, 16ll * device_sm_count()));
-    if (launch_kernel(head_dx_kernel<GROUPS>, dim3(blocks), dim3(kDxThreads), 0, stream, j) != cudaSuccess) return SBN_ERR_CUDA;
+    if (launch_kernel(head_dx_kernel<GROUPS, REST>, dim3(blocks), dim3(kDxThreads), 0, stream, j) != cudaSuccess) return SBN_ERR_CUDA;
     ++g_launch_count;
     return SBN_OK;
 }
 static sbn_status launch_head_dx(const HeadDxJob& j, cudaStream_t stream) {
-    return j.slots > 4 ? launch_head_dx_as<8>(j, stream) : launch_head_dx_as<1>(j, stream);
+    if (j.rest != 0) return j.slots > 4 ? launch_head_dx_as<8, true>(j, stream) : launch_head_dx_as<1, true>(j, stream);
+    return j.slots > 4 ? launch_head_dx_as<8, false>(j, stream) : launch_head_dx_as<1, false>(j, stream);
 }
 
 // ---- few tokens ------------------------------------------------------------------------------------
@@ -315,7 +329,7 @@ static sbn_status head_few_backward(const HeadCall& c, const HeadPlan& h, const 
     p.acc = dx ? reinterpret_cast<float*>(c.ws + w.acc) : nullptr;
     st = launch_head_few<true>(p, h.slots, list, dual, stream);
     if (st != SBN_OK) return st;
-    return dx ? launch_head_dx(HeadDxJob{nullptr, p.acc, h.slots, c.T, c.K, p.scale.out, static_cast<uint16_t*>(dx)}, stream) : SBN_OK;
+    return dx ? launch_head_dx(HeadDxJob{nullptr, p.acc, h.slots, c.T, c.K, c.T, 0, p.scale.out, static_cast<uint16_t*>(dx)}, stream) : SBN_OK;
 }
 
 // ---- any number of tokens --------------------------------------------------------------------------
@@ -346,7 +360,7 @@ static sbn_status head_forward(const HeadCall& c, float* loss0, float* loss1, fl
     p.z_ev = reinterpret_cast<float*>(c.ws + w.z_ev);
     p.parts = h.parts;
     p.skip_loads = g_test_break_waits;
-    st = h.words ? launch_head_words<0>(maps, HeadWordsParams{p, words_stages(h.tokens), h.tokens, h.groups, h.word_pairs, nullptr, nullptr, HeadScale{}}, list, dual, stream)
+    st = h.words ? launch_head_words<0>(maps, HeadWordsParams{p, words_stages(h.tokens), h.tokens, h.groups, h.word_pairs, nullptr, nullptr, HeadScale{}, 0}, list, dual, stream)
                  : launch_head_logits<0>(maps, p, list, dual, stream);
     if (st != SBN_OK) return st;
     return launch_head_losses(HeadLossJob{p.tg, p.count, p.row_src, c.T, c.N, p.part, p.part1, p.z_ev, static_cast<const uint16_t*>(c.x),
@@ -369,7 +383,7 @@ static sbn_status head_backward(const HeadCall& c, const float* lse0, const floa
     const HeadPlan h = head_plan(c.T, c.N, c.K);
     if (h.few) return head_few_backward(c, h, lse0, lse1, g0, g1, dx, dhead, stream);
     const HeadWs w = head_ws_layout(h, true, c.T, c.K, c.top);
-    const uint64_t k = static_cast<uint64_t>(c.K), t = static_cast<uint64_t>(c.T);
+    const uint64_t k = static_cast<uint64_t>(c.K), t = static_cast<uint64_t>(c.T), grad_rows = static_cast<uint64_t>(h.grad_rows);
     HeadMaps maps;
     HeadGradMaps gm;
     if (!head_encode(c, h, w, h.bn_piece, &maps) || !encode_out(&maps.dz, c.ws + w.dz, true, h.piece, h.rows256, 1)) return SBN_ERR_CUDA;
@@ -377,7 +391,7 @@ static sbn_status head_backward(const HeadCall& c, const float* lse0, const floa
     bool ok = encode_3d_bf16_blocks(&gm.aw, c.ws + w.dz, h.piece, h.rows256, 2) && encode_2d_bf16_sw128(&gm.ax, c.ws + w.dz, h.piece, h.rows256, h.piece, 128);
     for (int half = 0; ok && half < 2; ++half)
         ok = (h.words || encode_3d_bf16_blocks(&gm.bx[half], c.x, k, t, blocks >> half)) && encode_3d_bf16_blocks(&gm.bxc[half], c.ws + w.xc, k, h.rows64, blocks >> half);
-    ok = ok && (!dx || encode_out(&gm.acc, c.ws + w.acc, false, k, t, h.slots));
+    ok = ok && (!dx || encode_out(&gm.acc, c.ws + w.acc, false, k, grad_rows, h.slots));
     if (!ok) return SBN_ERR_CUDA;
     HeadRowsJob rows{};
     if (!h.words) rows.row_of = reinterpret_cast<int*>(c.ws + w.row_of);
@@ -403,7 +417,7 @@ static sbn_status head_backward(const HeadCall& c, const float* lse0, const floa
     HeadGradParams q{};
     q.count = p.count;
     q.scale = p.scale;
-    q.T = c.T; q.K = c.K;
+    q.T = h.grad_rows; q.K = c.K;
     q.slot_stages = h.slot_stages;
     q.want_dx = dx != nullptr;
     q.want_dw = dhead != nullptr;
@@ -412,7 +426,7 @@ static sbn_status head_backward(const HeadCall& c, const float* lse0, const floa
     for (int v0 = 0; v0 < c.N; v0 += h.piece) {
         const int cols = std::min(h.piece, c.N - v0);
         p.v0 = v0; p.v1 = v0 + cols;
-        st = h.words ? launch_head_words<1>(maps, HeadWordsParams{p, words_stages(h.tokens), h.tokens, h.groups, h.word_pairs, static_cast<const uint16_t*>(c.x), reinterpret_cast<uint16_t*>(c.ws + w.xc), rows.scale},
+        st = h.words ? launch_head_words<1>(maps, HeadWordsParams{p, words_stages(h.tokens), h.tokens, h.groups, h.word_pairs, static_cast<const uint16_t*>(c.x), reinterpret_cast<uint16_t*>(c.ws + w.xc), rows.scale, h.rest},
                                             list, dual, stream)
                      : launch_head_logits<1>(maps, p, list, dual, stream);
         if (st != SBN_OK) return st;
@@ -425,12 +439,12 @@ static sbn_status head_backward(const HeadCall& c, const float* lse0, const floa
         q.add = v0 > 0;
         const int slices = (all_stages + h.slot_stages - 1) / h.slot_stages;     // fewer in a short last piece
         const int tiles[2] = {dhead ? (cols + 255) / 256 * tiles_k : 0, dx ? static_cast<int>(h.rows256 / 256) * tiles_k * slices : 0};
-        const int stages[2] = {(c.T + 63) / 64, h.slot_stages};
+        const int stages[2] = {(h.grad_rows + 63) / 64, h.slot_stages};
         q.plan = plan_backward(tiles, stages, -1, 7.5);
         st = h.wide_grads ? launch_head_grads<true>(gm, q, stream) : launch_head_grads<false>(gm, q, stream);
         if (st != SBN_OK) return st;
     }
-    return dx ? launch_head_dx(HeadDxJob{rows.row_of, reinterpret_cast<const float*>(c.ws + w.acc), h.slots, c.T, c.K, p.scale, static_cast<uint16_t*>(dx)}, stream) : SBN_OK;
+    return dx ? launch_head_dx(HeadDxJob{rows.row_of, reinterpret_cast<const float*>(c.ws + w.acc), h.slots, c.T, c.K, h.grad_rows, h.rest, p.scale, static_cast<uint16_t*>(dx)}, stream) : SBN_OK;
 }
 
 }  // namespace sbn

@@ -451,16 +451,17 @@ head_losses_kernel(const HeadLossJob j) {
 
 struct HeadDxJob {
     const int* row_of;                            // null (few tokens): every token has its row
-    const float* acc;                             // [slots][T][K]
+    const float* acc;                             // [slots][rows][K]
     int slots, T, K;
+    int rows, rest;                               // rest: rows from a token's to its second part's (dz in two parts), 0: there is none
     const float* scale;                           // the unit of dz
     uint16_t* dx;                                 // [T][K]
 };
 
 constexpr int kDxThreads = 256;
 
-// GROUPS threads per 4 values, each with every GROUPS-th slot; their sums are added in the groups' order.
-template <int GROUPS>
+// GROUPS threads per 4 values, each with every GROUPS-th slot; their sums are added in the groups' order.  REST: dz in two parts.
+template <int GROUPS, bool REST>
 __global__ void __launch_bounds__(kDxThreads)
 head_dx_kernel(const HeadDxJob j) {
     constexpr int kVecs = kDxThreads / GROUPS;    // of a CTA and step
@@ -469,7 +470,7 @@ head_dx_kernel(const HeadDxJob j) {
     pdl_wait();
     const int vecs = j.K >> 2, group = threadIdx.x / kVecs, mine = threadIdx.x % kVecs;
     const long long all = static_cast<long long>(j.T) * vecs;
-    const size_t slot = static_cast<size_t>(j.T) * j.K;
+    const size_t slot = static_cast<size_t>(j.rows) * j.K, rest = static_cast<size_t>(j.rest) * j.K;
     const float scale = *j.scale;
     for (long long first = static_cast<long long>(blockIdx.x) * kVecs; first < all; first += static_cast<long long>(gridDim.x) * kVecs) {
         const long long i = first + mine;
@@ -481,7 +482,11 @@ head_dx_kernel(const HeadDxJob j) {
                 const float* a = j.acc + static_cast<size_t>(r) * j.K + 4 * c;
 #pragma unroll 8
                 for (int s = group; s < j.slots; s += GROUPS) {
-                    const float4 o = *reinterpret_cast<const float4*>(a + s * slot);
+                    float4 o = *reinterpret_cast<const float4*>(a + s * slot);
+                    if constexpr (REST) {
+                        const float4 r = *reinterpret_cast<const float4*>(a + s * slot + rest);
+                        o.x += r.x; o.y += r.y; o.z += r.z; o.w += r.w;
+                    }
                     v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
                 }
             }

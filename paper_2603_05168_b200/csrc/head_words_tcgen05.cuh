@@ -16,6 +16,11 @@
 namespace sbn {
 
 constexpr int kWordsTokens = 256;
+// Up to this many tokens dz is kept in two bf16 parts, the second as further rows behind the first's (and x twice, one below the other).  The
+// fewer the tokens, the fewer the entries that make a gradient, and the less their roundings average out: with one part 1.7 % of steps of up to
+// 128 tokens had gradients 2.5e-3 to 3.7e-3 off in the 2-norm, where their own rounding is 1.7e-3; above that 0.2 % do, 2.6e-3 at most.  Both parts fit the
+// one tile of 256 rows that dx has, so this costs 3 % (64 x 4096 x 131072 745 -> 770 us) to 8 % (128 x 2560 x 32000 146 -> 159 us) of a backward call.
+constexpr int kWordsTwoParts = 128;
 constexpr int kWordsSquare = 32 * 33;                                      // floats
 constexpr int kWordsTurnBytes = 8 * kWordsSquare * 4;
 constexpr int kWordsStateBytes = 8 * 3 * kWordsTokens * 4;                 // stats: [warp][m, s0, s1 or label][token]; grad: the warps' boxes
@@ -38,9 +43,11 @@ struct HeadWordsParams {
     const uint16_t* x;            // grad: copied to xc [T up to a multiple of 64][K]
     uint16_t* xc;
     HeadScale scale;              // grad
+    int rest;                     // grad: rows of dz and xc from a token's to its second part's, 0: there is none
 };
 
-template <int MODE, bool LIST, bool DUAL>
+// REST: dz in two parts (grad).
+template <int MODE, bool LIST, bool DUAL, bool REST>
 struct HeadWordsWork {
     static constexpr bool kWide = false;
     static constexpr int kStages = 5, kStagingBytes = kWordsTurnBytes + kWordsStateBytes;    // (at 256 tokens)
@@ -124,7 +131,11 @@ struct HeadWordsWork {
                     if (!LIST && tid == 0) report_bad(flags);
                     const uint4* from = reinterpret_cast<const uint4*>(w.wp.x + static_cast<size_t>(t) * p.K);
                     uint4* to = reinterpret_cast<uint4*>(w.wp.xc + static_cast<size_t>(t) * p.K);
-                    for (int v = tid; v < vecs; v += 256) to[v] = there ? __ldg(from + v) : make_uint4(0u, 0u, 0u, 0u);
+                    for (int v = tid; v < vecs; v += 256) {
+                        const uint4 value = there ? __ldg(from + v) : make_uint4(0u, 0u, 0u, 0u);
+                        to[v] = value;
+                        if constexpr (REST) to[static_cast<size_t>(w.wp.rest) * vecs + v] = value;
+                    }
                 }
             }
         }
@@ -185,8 +196,15 @@ struct HeadWordsWork {
                     }
                 } else {
                     uint32_t o[16];
-                    row.grad(p, z, n0, o);
-                    store_warp_box(box, lane, o, [&] { tma_store_2d(&w.maps.dz, n0 - p.v0, tile.t0 + c * 32, box); });
+                    if constexpr (REST) {
+                        uint32_t rest[16];
+                        row.template grad<true>(p, z, n0, o, rest);
+                        store_warp_box(box, lane, o, [&] { tma_store_2d(&w.maps.dz, n0 - p.v0, tile.t0 + c * 32, box); });
+                        store_warp_box(box, lane, rest, [&] { tma_store_2d(&w.maps.dz, n0 - p.v0, w.wp.rest + tile.t0 + c * 32, box); });
+                    } else {
+                        row.grad(p, z, n0, o);
+                        store_warp_box(box, lane, o, [&] { tma_store_2d(&w.maps.dz, n0 - p.v0, tile.t0 + c * 32, box); });
+                    }
                 }
             }
         }
@@ -214,11 +232,11 @@ struct HeadWordsWork {
     };
 };
 
-template <int MODE, bool LIST, bool DUAL>
+template <int MODE, bool LIST, bool DUAL, bool REST>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(320, 1)
 head_words_kernel(const __grid_constant__ HeadMaps maps, const __grid_constant__ HeadWordsParams p) {
     pdl_launch_dependents();
-    HeadWordsWork<MODE, LIST, DUAL> work(maps, p);
+    HeadWordsWork<MODE, LIST, DUAL, REST> work(maps, p);
     bf16_pair_loop(work, p.p.skip_loads != 0);
 }
 

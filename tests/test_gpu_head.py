@@ -879,3 +879,29 @@ def test_gradients_of_few_tokens_are_off_by_their_own_rounding(T, N, K, top):
     for got, want in ((dx, o["dx"]), (dhead[c["labels"]], o["dhead"][c["labels"]])):
         rows = (got.double() - want).norm(dim=1) / want.norm(dim=1)
         assert float(rows.max()) < ONE_ROUNDING, rows
+
+
+@pytest.mark.parametrize("top", [0, 3])
+@pytest.mark.parametrize("T,N,K", [(9, 2003, 2688), (17, 2003, 1152), (33, 5003, 2560), (64, 1300, 1024), (65, 1300, 1024), (97, 5003, 512), (128, 19001, 384)])
+def test_gradients_of_up_to_128_tokens_are_off_by_their_own_rounding(T, N, K, top):
+    c = make(T, N, K, seed=179 + T, ignored=0.0, lean=0.0, top=top, absent=0.0)
+    c["labels"] = torch.arange(T, device="cuda") * (N // T) + 5
+    c["d_ce"].fill_(1.0 / 1024)
+    c["d_ce"][1::2] = (0.5 + 2.0 ** -9) / 1024
+    if top:
+        c["d_distill"] = c["d_ce"] / 2
+    o, _ = reference(c)
+    dx, dhead = backward(c, forward(c)["lse"])
+    b.sbn_check_status()
+    for got, want in ((dx, o["dx"]), (dhead[c["labels"]], o["dhead"][c["labels"]])):
+        rows = (got.double() - want).norm(dim=1) / want.norm(dim=1)
+        assert float(rows.max()) < ONE_ROUNDING * 1.03, rows       # (a row of 384 values: 3 % more than its expectation)
+
+
+@pytest.mark.parametrize("T", [20, 64, 65, 128, 129])
+def test_rows_left_out_of_both_parts(T):
+    # tokens that nothing is asked of in every place of a 64, gradients of either kind alone, and NaN in them
+    c = make(T, 900, 384, seed=181 + T, ignored=0.5)
+    c["x"][c["labels"] < 0] = NAN
+    f, dx, dhead = check(c)
+    assert torch.equal(backward(c, f["lse"], dhead=False)[0], dx) and torch.equal(backward(c, f["lse"], dx=False)[1], dhead)
