@@ -905,3 +905,45 @@ def test_rows_left_out_of_both_parts(T):
     c["x"][c["labels"] < 0] = NAN
     f, dx, dhead = check(c)
     assert torch.equal(backward(c, f["lse"], dhead=False)[0], dx) and torch.equal(backward(c, f["lse"], dx=False)[1], dhead)
+
+
+@pytest.mark.parametrize("top", [0, 6])
+@pytest.mark.parametrize("T,N,K", [(12, 2000, 1152), (50, 700, 384), (64, 1500, 256), (128, 1500, 256)])
+def test_two_parts_captured_and_within_their_buffers(T, N, K, top):
+    # a step in a graph, replayed on other inputs; outputs and workspaces between guards
+    c, pad = make(T, N, K, seed=191, top=top), 4096
+    n = [b.sbn_head_workspace_bytes(T, N, K, top, w) for w in (False, True)]
+    held = [torch.full((m + 2 * pad,), 0x5A, dtype=torch.uint8, device="cuda") for m in n]
+    ws = [h[pad:pad + m] for h, m in zip(held, n)]
+    outs = {k: torch.full((m * K + 2 * pad,), 7.0, dtype=BF16, device="cuda") for k, m in (("dx", T), ("dhead", N))}
+    dx, dhead = outs["dx"][pad:pad + T * K].view(T, K), outs["dhead"][pad:pad + N * K].view(N, K)
+
+    def step():
+        f = forward(c, ws=ws[0], dirty=False)
+        if top:
+            b.sbn_head_distill_backward(c["x"], c["head"], c["top_index"], c["top_logits"], c["tau"], f["lse"], c["d_distill"], labels=c["labels"],
+                                        d_ce=c["d_ce"], dx=dx, dhead=dhead, ws=ws[1])
+        else:
+            b.sbn_head_cross_entropy_backward(c["x"], c["head"], c["labels"], f["lse"], c["d_ce"], dx=dx, dhead=dhead, ws=ws[1])
+        return f
+
+    step()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        f = step()
+    for seed in (193, 197):
+        new = make(T, N, K, seed=seed, top=top, ignored=0.6 if seed == 193 else 0.0)
+        for k, v in new.items():
+            if torch.is_tensor(v):
+                c[k].copy_(v)
+        g.replay()
+        o, bd = reference(c)
+        for name in ("ce", "distill"):
+            if name in f and name in o:
+                assert_near(name, f[name], o[name], bd[name])
+        assert_near("dx", dx, o["dx"], bd["dx"])
+        assert_near("dhead", dhead, o["dhead"], bd["dhead"])
+    for h, m in zip(held, n):
+        assert bool((h[:pad] == 0x5A).all()) and bool((h[pad + m:] == 0x5A).all())
+    for k, m in (("dx", T), ("dhead", N)):
+        assert bool((outs[k][:pad] == 7).all()) and bool((outs[k][pad + m * K:] == 7).all()), k
