@@ -298,7 +298,7 @@ __device__ __forceinline__ float head_logit_share(const HeadLossJob& j, int t, l
 // lse - z of one word: log(sum / term), with the term itself taken from the word's exact logit.  sum: of exp of all logits in
 // units of exp of the largest, with the word's as the products had it (`was`, relative to the largest); ahead: the largest less the exact logit.
 // The rest of the sum is at least 0 (a sum that holds the largest term is never rounded below it), and so is the result: with lse
-// and the logit from different sums, a sure token's loss was what their errors differed by, 4e-5 at 4096 columns and of either sign.
+// and the logit from different sums, a sure token's loss was what their errors differed by: up to 1.1e-4 at 4096 columns, mostly below 0.
 // (expf: 1 exactly for the largest term, and where another one is the largest its error is beside a rest of at least 1.)
 __device__ __forceinline__ double surprise(double sum, float was, double ahead) {
     double rest = sum - static_cast<double>(expf(was));
